@@ -569,6 +569,102 @@ int eep_get_dedup_view(eep_ctx* ctx, eep_dedup_view* out);
 /* Copies the first n ints of a field to the host after synchronising `stream`. */
 int eep_read_dedup(eep_ctx* ctx, int32_t field, int32_t* host_dst, int64_t n, void* stream);
 
+/* ---- the layer around dispatch and combine: the norm that makes the payload rows, the
+ * router's choice, the experts' products (paper Sec. 4.1 and Fig. 4: the expert kernels and the
+ * router sit in the same captured graph as dispatch and combine; it leaves them to prior
+ * work).  None of these needs a context: what they read of a step is topk_idx, topk_w,
+ * x and x_scale, which go into the per-step calls above, and eep_view.offset, which comes
+ * from them.  Graph-capturable; grids depend only on T or rows. */
+
+/* Residual addition, root-mean-square norm, 8-bit codes: row by row of H = hidden elements,
+ *   h = x + residual (x alone where residual is NULL), in fp32
+ *   sum  = round(h)                                 (in_dtype; not written where NULL)
+ *   v = h / sqrt(mean(h * h) + epsilon) * gain, in fp32, from the unrounded h
+ *   y    = round(v)                                 (out_dtype; not written where NULL)
+ *   code_scale = max|v| / 448 of scale_group channels (1 if they are all zero),
+ *   code = e4m3fn(v / code_scale), as eep_dispatch_quant (from the unrounded v; not written
+ *          where NULL): the x and x_scale of an eep_dispatch with fp8 payloads.
+ * x, residual, sum: device [T, H] in_dtype; gain: device [H] gain_dtype; y: device [T, H];
+ * code: device bytes [T, H]; code_scale: device float [T, H/scale_group].  sum may be x or
+ * residual itself, and so may y where the types agree.
+ * hidden: 8 to 65536, a multiple of 8; scale_group: a power of two from 16 to 512 that divides
+ * hidden, or 0 without codes.  A row with an infinity or a NaN gives what the formulas give. */
+typedef struct {
+  int32_t hidden;
+  int32_t in_dtype, gain_dtype, out_dtype; /* EEP_F32 or EEP_BF16 */
+  int32_t scale_group;
+  float epsilon;
+} eep_norm_shape;
+int eep_residual_norm(const eep_norm_shape* shape, const void* x, const void* residual,
+                      const void* gain, void* sum, void* y, void* code, float* code_scale,
+                      int32_t T, void* stream);
+
+/* The router's choice: for every token the topk largest of its num_logical logits, in descending
+ * order, equal ones by ascending index (paper Sec. 2.1: top-k routing), and their weights,
+ *   topk_w[t, j] = exp(logit_j - largest) / sum of exp(logit_i - largest) over
+ *                  the chosen i (over_all == 0), or over all i (over_all != 0).
+ * Logits of -infinity and NaN are never chosen and weigh nothing; where fewer than topk are
+ * left, topk_idx is -1 (which eep_dispatch_layout masks) and topk_w is 0.  Logits of +infinity
+ * share the weight among them.  logits: device [T, num_logical] in_dtype (EEP_F32 or EEP_BF16),
+ * aligned to its elements; topk_idx: device int32 [T, topk]; topk_w: device float [T, topk].
+ * num_logical: 1 to 4096; topk: 1 to 32, at most num_logical. */
+typedef struct {
+  int32_t num_logical, topk, in_dtype, over_all;
+} eep_router_shape;
+int eep_route(const eep_router_shape* shape, const void* logits, int32_t* topk_idx, float* topk_w,
+              int32_t T, void* stream);
+
+/* The experts' product: the rows of every slot times the slot's own weights, grouped as
+ * eep_dispatch_layout left them (paper Fig. 4: the expert kernels read the receive rows
+ * that dispatch wrote),
+ *   s[i, n] = sum over k of x[i, k] * w[p][n, k]      for offset[p] <= i < offset[p+1]
+ *   gate EEP_GATE_NONE: y[i, n] = round(s[i, n]), out_features rows n of w
+ *   gate EEP_GATE_SILU: y[i, n] = round(silu(s[i, n]) * s[i, out_features + n]), 2 * out_features
+ *                       rows of w: the gate's, then the other factor's.  silu(v) = v / (1 + exp(-v))
+ * with sums in fp32 and one rounding at the end.  Rows of y outside every slot are left untouched.
+ *   x        device [rows, in_features] x_dtype: the receive rows
+ *   offset   device int32 [num_slots + 1], read on the device (eep_view.offset); NULL: one slot
+ *            with all the rows (num_slots must be 1): an ordinary product, such as that of an
+ *            expert that every token goes to
+ *   w        device; slot p's weights begin p * slot_stride bytes in, [n][in_features] of
+ *            x_dtype; the slot-major store that eep_apply_repair moves is one such
+ *   y        device [rows, out_features] y_dtype
+ * x_dtype EEP_FP8_E4M3: codes with a scale for each block of 128 channels,
+ *   x_scale  device float [rows, in_features / 128] (eep_dispatch's recv_scale)
+ *   w_scale  device float, slot p's begin p * scale_stride bytes in: [ceil(n / 128)][in_features / 128],
+ *            one for 128 rows by 128 channels
+ *   (both NULL for the other types); products of a block are summed in fp32 by the matrix cores, then
+ *   multiplied by the two scales and summed in fp32.
+ * y_dtype EEP_FP8_E4M3 (with the gate): codes, and y_scale device float [rows, out_features / 128], from
+ *   the unrounded fp32 values as eep_residual_norm makes them: the second product's x and x_scale.
+ *
+ * eep_product_create checks a shape and allocates what the product needs beside its operands (a
+ * workspace for few rows; hipMalloc on the current device).  Calls with one handle share the
+ * workspace: their kernels may not overlap (one stream, or events between); handles are
+ * independent.  eep_product_destroy waits for the device.
+ *   num_slots      1 to 65536;  max_rows  0 to 2^30: the most that a call may pass
+ *   in_features    rows of x and w must be multiples of 16 bytes (EEP_ERR_ALIGN), and whole scale
+ *                  blocks for fp8 (EEP_ERR_INVALID_ARG)
+ *   out_features   rows of y must be multiples of 16 bytes; a multiple of 128 where y is fp8 or
+ *                  where fp8 weights are gated
+ *   slot_stride, scale_stride   0: packed; else multiples of 16 and of 4, at least packed
+ * eep_expert_product: rows of the call, at most max_rows (T*k of the step: rows from offset's end on are not
+ * read).  Offsets are taken as they are clamped to [0, rows]; y may not overlap an operand. */
+typedef enum { EEP_GATE_NONE = 0, EEP_GATE_SILU = 1 } eep_gate;
+typedef struct {
+  int32_t num_slots, in_features, out_features;
+  int32_t x_dtype, y_dtype;
+  int32_t gate;
+  int32_t max_rows;
+  int64_t slot_stride, scale_stride;
+} eep_product_config;
+typedef struct eep_product eep_product;
+int eep_product_create(const eep_product_config* cfg, eep_product** out);
+int eep_product_destroy(eep_product* product);
+int eep_expert_product(eep_product* product, const void* x, const float* x_scale, const void* w,
+                       const float* w_scale, const int32_t* offset, void* y, float* y_scale,
+                       int32_t rows, void* stream);
+
 /* ---- hipGraph helper (Sec. 2.3, Fig. 4: capture once, replay, patch table
  * contents only) ------------------------------------------------------------
  * eep_graph_begin puts `stream` (not the default stream) into capture mode;

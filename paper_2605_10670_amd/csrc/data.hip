@@ -10,15 +10,10 @@
 #include <type_traits>
 
 #include "eep_internal.hpp"
+#include "numbers.hpp"
 #include "rows.hpp"
 
 namespace eep {
-
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 // ---------------------------------------------------------------------------
 // pack: recv[row_of[t, j]] = x[t].  One wavefront per token reads the row once
@@ -537,17 +532,6 @@ hipError_t launch_expand(eep_ctx* c, const void* recv_dedup, void* recv_x, int T
 // ---------------------------------------------------------------------------
 // number formats
 // ---------------------------------------------------------------------------
-__device__ inline float bf16_lo(uint32_t u) { return __uint_as_float(u << 16); }
-__device__ inline float bf16_hi(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
-
-// Two binary32 -> two bfloat16 in one dword, round to nearest even, NaN stays (quiet) NaN: one
-// v_cvt_pk_bf16_f32.  Compared with the integer form of the rule (add 0x7fff and the kept
-// bit, shift) over all 2^32 inputs, NaNs and subnormals included: no difference.
-__device__ inline uint32_t pack_bf16x2(float lo, float hi) {
-  const f32x2 v = {lo, hi};
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
-}
-
 // binary32 -> OCP e4m3fn byte, round to nearest even, saturating at +-448
 // (NaN -> 0x7f).  Normal results round the 23-bit significand to 3 bits with an
 // integer add so that a carry moves into the exponent; results below 2^-6 are
@@ -600,17 +584,6 @@ __device__ inline uint32_t f32_to_e4m3(float f) {
 // ---------------------------------------------------------------------------
 constexpr int kQuantVecs = 7;           // 16-channel vectors per lane per pass (7 * 64 * 16 = 7168)
 constexpr int kQuantSplitBelow = 1024;  // batches below this many tokens split a row over wavefronts
-
-// Maximum over aligned groups of n lanes (n a power of two <= 64), in every lane of the group.
-__device__ __forceinline__ uint32_t group_max(uint32_t v, int n) {
-  auto larger = [](uint32_t a, uint32_t b) { return a > b ? a : b; };
-  if (n > 1) v = larger(v, __builtin_amdgcn_update_dpp(0u, v, 0xB1, 0xf, 0xf, false));   // lane ^ 1
-  if (n > 2) v = larger(v, __builtin_amdgcn_update_dpp(0u, v, 0x4E, 0xf, 0xf, false));   // lane ^ 2
-  if (n > 4) v = larger(v, __builtin_amdgcn_update_dpp(0u, v, 0x141, 0xf, 0xf, false));  // half row mirrored
-  if (n > 8) v = larger(v, __builtin_amdgcn_update_dpp(0u, v, 0x140, 0xf, 0xf, false));  // row mirrored
-  for (int m = 16; m < n; m <<= 1) v = larger(v, __shfl_xor(v, m, 64));
-  return v;
-}
 
 __device__ __forceinline__ uint32_t quant4(const uint32_t (&d)[2], float scale, float y) {
   float q[4];

@@ -1,0 +1,420 @@
+// The experts' product: the rows of every slot times the slot's weights, grouped by the offsets that the layout
+// left in device memory.
+//
+// All kernels work on the transposed product: the matrix cores' rows are rows of the weights (features of y), their
+// columns are tokens.  A lane then holds four neighbouring features of ONE token: it needs one scale of x and one of w
+// per block, and stores 8 or 16 bytes of a row of y.  Whatever the type, a step is 128 bytes along in_features, of which lane
+// l takes 16 bytes of row l % 16 at 16 * (l / 16) and 16 more 64 bytes on, of both operands alike: a product of sums
+// does not ask in which order its terms come, so the matrix cores' own order of k plays no part.
+#include <new>
+
+#include "eep_internal.hpp"
+#include "numbers.hpp"
+#include "rows.hpp"
+
+struct eep_product {
+  eep_product_config cfg;
+  int64_t slot_stride, scale_stride;  // bytes
+};
+
+namespace eep {
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kStepBytes = 128;  // along in_features
+constexpr int kScaleBlock = 128;
+
+struct ProductArgs {
+  const uint8_t *x, *w;
+  const float *x_scale, *w_scale;
+  const int32_t* offset;
+  uint8_t* y;
+  float* y_scale;
+  int rows, slots;
+  int row_bytes;  // of x and w
+  int features;   // of y
+  int feature_tiles;
+  int64_t slot_stride, scale_stride;
+};
+
+// 32 bytes a lane of a 16-row operand: two chunks of 16.
+struct Frag {
+  u32x4 c[2];
+};
+
+// 16 e4m3 codes as bf16, which holds them exactly.
+__device__ __forceinline__ void widen(const u32x4& c, bf16x8 (&out)[2]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[i], 1.0f, false);
+    const bf16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[i], 1.0f, true);
+    out[i >> 1][4 * (i & 1)] = lo[0];
+    out[i >> 1][4 * (i & 1) + 1] = lo[1];
+    out[i >> 1][4 * (i & 1) + 2] = hi[0];
+    out[i >> 1][4 * (i & 1) + 3] = hi[1];
+  }
+}
+
+// acc + a * b over the 128 bytes of a step.
+//
+// Codes are multiplied as bf16, of which the matrix cores keep every product: their 8-bit forms line the products of
+// 8 neighbouring k up with the largest of them and keep 13 bits below its first (measured with single products
+// beside a large one; across the eights nothing is lost).  On normally distributed rows a sum of 128 then is
+// 1.3e-5 off (2-norm), and 5.4e-5 with wider ones; as bf16 1e-8 and 7e-8.
+template <int DT>
+__device__ __forceinline__ f32x4 mma(const Frag& a, const Frag& b, f32x4 acc) {
+  if constexpr (DT == EEP_FP8_E4M3) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      bf16x8 av[2], bv[2];
+      widen(a.c[j], av);
+      widen(b.c[j], bv);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[i], bv[i], acc, 0, 0, 0);
+    }
+    return acc;
+  } else if constexpr (DT == EEP_BF16) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a.c[j]),
+                                                    __builtin_bit_cast(bf16x8, b.c[j]), acc, 0, 0, 0);
+    return acc;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.c[j][i]), __uint_as_float(b.c[j][i]), acc, 0, 0, 0);
+    return acc;
+  }
+}
+
+// v / (1 + exp(-v)) * u
+__device__ __forceinline__ float silu_times(float v, float u) { return v / (1.0f + expf(-v)) * u; }
+
+// Where the `tile`-th tile of TOKENS rows lies: its slot, its first row and the end of the slot's rows.  false: there are
+// fewer.  A lane counts the tiles of a run of slots, a wavefront adds them up; all lanes get the answer.
+template <int TOKENS>
+__device__ __forceinline__ bool find_tile(const ProductArgs& a, int64_t tile, int* slot, int* first, int* end) {
+  if (a.offset == nullptr) {
+    *slot = 0;
+    *first = (int)(tile * TOKENS);
+    *end = a.rows;
+    return tile * TOKENS < a.rows;
+  }
+  const int lane = threadIdx.x & 63;
+  const int run = (a.slots + 63) / 64;
+  const int p0 = lane * run, p1 = p0 + run < a.slots ? p0 + run : a.slots;
+  auto bound = [&](int p) {
+    const int o = a.offset[p];
+    return o < 0 ? 0 : o > a.rows ? a.rows : o;
+  };
+  int mine = 0;
+  if (p0 < p1) {
+    int lo = bound(p0);
+    for (int p = p0; p < p1; ++p) {
+      const int hi = bound(p + 1);
+      if (hi > lo) mine += (hi - lo + TOKENS - 1) / TOKENS;
+      lo = hi;
+    }
+  }
+  int upto = mine;  // inclusive sum over the lanes
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int v = __shfl_up(upto, d, 64);
+    if (lane >= d) upto += v;
+  }
+  const uint64_t behind = __ballot((int64_t)upto > tile);
+  if (behind == 0) return false;
+  const int owner = __builtin_ctzll(behind);
+  int found[3] = {0, 0, 0};
+  if (lane == owner) {
+    int64_t left = tile - (upto - mine);
+    int lo = bound(p0);
+    for (int p = p0; p < p1; ++p) {
+      const int hi = bound(p + 1);
+      const int n = hi > lo ? (hi - lo + TOKENS - 1) / TOKENS : 0;
+      if (left < n) {
+        found[0] = p;
+        found[1] = lo + (int)left * TOKENS;
+        found[2] = hi;
+        break;
+      }
+      left -= n;
+      lo = hi;
+    }
+  }
+  *slot = __builtin_amdgcn_readlane(found[0], owner);
+  *first = __builtin_amdgcn_readlane(found[1], owner);
+  *end = __builtin_amdgcn_readlane(found[2], owner);
+  return true;
+}
+
+// Stores four neighbouring features of one token.
+template <int YT>
+__device__ __forceinline__ void store4(uint8_t* y, int64_t element, const float (&v)[4]) {
+  if constexpr (YT == EEP_F32)
+    *(f32x4*)(y + element * 4) = f32x4{v[0], v[1], v[2], v[3]};
+  else
+    *(u32x2*)(y + element * 2) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+}
+
+// ---------------------------------------------------------------------------
+// few rows a slot: the weights go straight to registers.
+//
+// A workgroup of 8 wavefronts has 16 rows of one slot and 128 features of y with the gate, 256 without: each wavefront two
+// matrix-core tiles of 16 weight rows, with the gate the two factors of 16 features.  No weight is used by two
+// wavefronts, so nothing of them goes through LDS; the rows of x come from the caches.
+// ---------------------------------------------------------------------------
+constexpr int kThinTokens = 16, kThinWaves = 8;
+
+template <int DT, int YT, bool GATE>
+__global__ __launch_bounds__(64 * kThinWaves) void k_product_thin(ProductArgs a, int64_t first_tile) {
+  constexpr int U = 2;  // steps of loads in flight ahead of the ones that are multiplied
+  __shared__ uint32_t s_top[kThinWaves][16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int col = lane & 15, part = lane >> 4;
+  const int64_t work = first_tile + blockIdx.x;
+  const int64_t row_tile = work / a.feature_tiles;
+  const int feature_tile = (int)(work - row_tile * a.feature_tiles);
+  int slot, row0, end;
+  if (!find_tile<kThinTokens>(a, row_tile, &slot, &row0, &end)) return;
+
+  const int weight_rows = GATE ? 2 * a.features : a.features;
+  int n0[2];  // first weight row of the wavefront's two tiles
+  if constexpr (GATE) {
+    n0[0] = (feature_tile * kThinWaves + wave) * 16;
+    n0[1] = n0[0] + a.features;
+  } else {
+    n0[0] = (feature_tile * kThinWaves + wave) * 32;
+    n0[1] = n0[0] + 16;
+  }
+  // rows past the end are read as the last one; their results are not stored
+  const uint8_t* slot_w = a.w + slot * a.slot_stride;
+  const uint8_t* from[3];
+#pragma unroll
+  for (int m = 0; m < 2; ++m) {
+    const int n = n0[m] + col < weight_rows ? n0[m] + col : weight_rows - 1;
+    from[m] = slot_w + (int64_t)n * a.row_bytes + part * 16;
+  }
+  const int token = row0 + col < end ? row0 + col : end - 1;
+  from[2] = a.x + (int64_t)token * a.row_bytes + part * 16;
+  const int steps = a.row_bytes / kStepBytes;
+  const int tail = a.row_bytes - steps * kStepBytes;  // bytes, a multiple of 16; 0 for fp8
+  const float* sx = nullptr;
+  const float* sw[2] = {nullptr, nullptr};
+  if constexpr (DT == EEP_FP8_E4M3) {
+    sx = a.x_scale + (int64_t)token * steps;
+    const float* slot_scale = (const float*)((const uint8_t*)a.w_scale + slot * a.scale_stride);
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      const int n = n0[m] < weight_rows ? n0[m] : weight_rows - 1;
+      sw[m] = slot_scale + (int64_t)(n / kScaleBlock) * steps;
+    }
+  }
+
+  f32x4 acc[2] = {};
+  Frag f[2][U][3];
+  float xs[2][U], ws[2][U][2];
+  auto load = [&](int buffer, int step) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int s = step + u < steps ? step + u : steps - 1;
+#pragma unroll
+      for (int m = 0; m < 3; ++m)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          f[buffer][u][m].c[j] = *(const u32x4*)(from[m] + (int64_t)s * kStepBytes + j * 64);
+      if constexpr (DT == EEP_FP8_E4M3) {
+        xs[buffer][u] = sx[s];
+#pragma unroll
+        for (int m = 0; m < 2; ++m) ws[buffer][u][m] = sw[m][s];
+      }
+    }
+  };
+  auto multiply = [&](int buffer, int step) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (step + u >= steps) break;
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        if constexpr (DT == EEP_FP8_E4M3) {
+          const f32x4 p = mma<DT>(f[buffer][u][m], f[buffer][u][2], f32x4{0, 0, 0, 0});
+          const float scale = xs[buffer][u] * ws[buffer][u][m];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[m][i] = fmaf(p[i], scale, acc[m][i]);
+        } else {
+          acc[m] = mma<DT>(f[buffer][u][m], f[buffer][u][2], acc[m]);
+        }
+      }
+    }
+  };
+  if (steps > 0) {
+    load(0, 0);
+    for (int s = 0; s < steps; s += 2 * U) {
+      load(1, s + U);
+      multiply(0, s);
+      load(0, s + 2 * U);
+      multiply(1, s + U);
+    }
+  }
+  if (tail != 0) {
+    Frag t[3];
+#pragma unroll
+    for (int m = 0; m < 3; ++m)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        t[m].c[j] = u32x4{0, 0, 0, 0};
+        if (j * 64 + part * 16 < tail) t[m].c[j] = *(const u32x4*)(from[m] + (int64_t)steps * kStepBytes + j * 64);
+      }
+#pragma unroll
+    for (int m = 0; m < 2; ++m) acc[m] = mma<DT>(t[m], t[2], acc[m]);
+  }
+
+  const int64_t out_row = (int64_t)(row0 + col) * a.features;
+  const bool in_rows = row0 + col < end;
+  if constexpr (GATE) {
+    const int n = n0[0] + part * 4;
+    float v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = silu_times(acc[0][i], acc[1][i]);
+    if constexpr (YT == EEP_FP8_E4M3) {
+      uint32_t top = top_magnitude<4>(v);
+      top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
+      top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
+      if (part == 0) s_top[wave][col] = top;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < kThinWaves; ++w) top = max(top, s_top[w][col]);
+      const float scale = scale_of(top);
+      if (in_rows) {
+        *(uint32_t*)(a.y + out_row + n) = codes4(v[0], v[1], v[2], v[3], scale);
+        if (wave == 0 && part == 0) a.y_scale[(int64_t)(row0 + col) * a.feature_tiles + feature_tile] = scale;
+      }
+    } else {
+      if (in_rows && n < a.features) store4<YT>(a.y, out_row + n, v);
+    }
+  } else {
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      const int n = n0[m] + part * 4;
+      const float v[4] = {acc[m][0], acc[m][1], acc[m][2], acc[m][3]};
+      if (in_rows && n < a.features) store4<YT>(a.y, out_row + n, v);
+    }
+  }
+}
+
+// Tiles of `tokens` rows that the slots may have at most.
+int64_t most_tiles(int rows, int slots, int tokens) {
+  const int64_t touched = rows < slots ? rows : slots;
+  return (rows + touched * (tokens - 1)) / tokens;
+}
+
+template <int DT, int YT, bool GATE>
+hipError_t launch_product(ProductArgs a, hipStream_t st) {
+  const int features = GATE ? 16 * kThinWaves : 32 * kThinWaves;
+  a.feature_tiles = (a.features + features - 1) / features;
+  const int64_t work = most_tiles(a.rows, a.slots, kThinTokens) * a.feature_tiles;
+  return in_launches(work, max_blocks(64 * kThinWaves), [&](int64_t first, int64_t n) {
+    hipLaunchKernelGGL((k_product_thin<DT, YT, GATE>), dim3((unsigned)n), dim3(64 * kThinWaves), 0, st, a, first);
+    return hipGetLastError();
+  });
+}
+
+template <int DT>
+hipError_t launch_product(const ProductArgs& a, int y_dtype, bool gate, hipStream_t st) {
+  if (gate) {
+    if (y_dtype == EEP_FP8_E4M3) return launch_product<DT, EEP_FP8_E4M3, true>(a, st);
+    if (y_dtype == EEP_BF16) return launch_product<DT, EEP_BF16, true>(a, st);
+    return launch_product<DT, EEP_F32, true>(a, st);
+  }
+  if (y_dtype == EEP_BF16) return launch_product<DT, EEP_BF16, false>(a, st);
+  return launch_product<DT, EEP_F32, false>(a, st);
+}
+
+}  // namespace eep
+
+using namespace eep;
+
+extern "C" {
+
+int eep_product_create(const eep_product_config* cfg, eep_product** out) {
+  if (!out) return EEP_ERR_INVALID_ARG;
+  *out = nullptr;
+  if (!cfg) return EEP_ERR_INVALID_ARG;
+  const eep_product_config& f = *cfg;
+  const bool fp8 = f.x_dtype == EEP_FP8_E4M3, gated = f.gate == EEP_GATE_SILU;
+  if (f.num_slots < 1 || f.num_slots > 65536 || f.in_features < 1 || f.out_features < 1 ||
+      f.in_features > (1 << 24) || f.out_features > (1 << 24) || f.max_rows < 0 || f.max_rows > (1 << 30))
+    return EEP_ERR_INVALID_ARG;
+  if ((f.x_dtype != EEP_F32 && f.x_dtype != EEP_BF16 && !fp8) ||
+      (f.y_dtype != EEP_F32 && f.y_dtype != EEP_BF16 && f.y_dtype != EEP_FP8_E4M3) ||
+      (!gated && f.gate != EEP_GATE_NONE) || (f.y_dtype == EEP_FP8_E4M3 && !gated))
+    return EEP_ERR_INVALID_ARG;
+  const int64_t in_bytes = (int64_t)f.in_features * dtype_bytes(f.x_dtype);
+  if (in_bytes % 16 || (int64_t)f.out_features * dtype_bytes(f.y_dtype) % 16) return EEP_ERR_ALIGN;
+  if ((fp8 && f.in_features % kScaleBlock != 0) ||
+      ((f.y_dtype == EEP_FP8_E4M3 || (fp8 && gated)) && f.out_features % kScaleBlock != 0))
+    return EEP_ERR_INVALID_ARG;
+  const int64_t weight_rows = (int64_t)f.out_features * (gated ? 2 : 1);
+  const int64_t packed = weight_rows * in_bytes;
+  const int64_t packed_scale =
+      fp8 ? (weight_rows + kScaleBlock - 1) / kScaleBlock * (f.in_features / kScaleBlock) * (int64_t)sizeof(float) : 0;
+  if (f.slot_stride < 0 || f.scale_stride < 0 || (f.slot_stride != 0 && f.slot_stride < packed) ||
+      (f.scale_stride != 0 && f.scale_stride < packed_scale))
+    return EEP_ERR_INVALID_ARG;
+  if (f.slot_stride % 16 || f.scale_stride % 4) return EEP_ERR_ALIGN;
+  eep_product* p = new (std::nothrow) eep_product();
+  if (!p) return EEP_ERR_INVALID_ARG;
+  p->cfg = f;
+  p->slot_stride = f.slot_stride ? f.slot_stride : packed;
+  p->scale_stride = f.scale_stride ? f.scale_stride : packed_scale;
+  *out = p;
+  return EEP_OK;
+}
+
+int eep_product_destroy(eep_product* product) {
+  if (!product) return EEP_OK;
+  const hipError_t e = hipDeviceSynchronize();
+  delete product;
+  return e == hipSuccess ? EEP_OK : EEP_ERR_HIP;
+}
+
+int eep_expert_product(eep_product* product, const void* x, const float* x_scale, const void* w, const float* w_scale,
+                       const int32_t* offset, void* y, float* y_scale, int32_t rows, void* stream) {
+  if (!product || rows < 0 || rows > product->cfg.max_rows) return EEP_ERR_INVALID_ARG;
+  const eep_product_config& f = product->cfg;
+  const bool fp8 = f.x_dtype == EEP_FP8_E4M3;
+  if (rows == 0) return EEP_OK;
+  if (!x || !w || !y || (x_scale != nullptr) != fp8 || (w_scale != nullptr) != fp8 || (y_scale != nullptr) != (f.y_dtype == EEP_FP8_E4M3) ||
+      (offset == nullptr && f.num_slots != 1))
+    return EEP_ERR_INVALID_ARG;
+  if (((uintptr_t)x & 15u) || ((uintptr_t)w & 15u) || ((uintptr_t)y & 15u) || ((uintptr_t)x_scale & 3u) ||
+      ((uintptr_t)w_scale & 3u) || ((uintptr_t)offset & 3u) || ((uintptr_t)y_scale & 3u))
+    return EEP_ERR_ALIGN;
+  ProductArgs a = {};
+  a.x = (const uint8_t*)x;
+  a.w = (const uint8_t*)w;
+  a.x_scale = x_scale;
+  a.w_scale = w_scale;
+  a.offset = offset;
+  a.y = (uint8_t*)y;
+  a.y_scale = y_scale;
+  a.rows = rows;
+  a.slots = f.num_slots;
+  a.row_bytes = f.in_features * dtype_bytes(f.x_dtype);
+  a.features = f.out_features;
+  a.slot_stride = product->slot_stride;
+  a.scale_stride = product->scale_stride;
+  const bool gate = f.gate == EEP_GATE_SILU;
+  hipError_t e;
+  switch (f.x_dtype) {
+    case EEP_FP8_E4M3: e = launch_product<EEP_FP8_E4M3>(a, f.y_dtype, gate, (hipStream_t)stream); break;
+    case EEP_BF16: e = launch_product<EEP_BF16>(a, f.y_dtype, gate, (hipStream_t)stream); break;
+    default: e = launch_product<EEP_F32>(a, f.y_dtype, gate, (hipStream_t)stream);
+  }
+  return e == hipSuccess ? EEP_OK : EEP_ERR_HIP;
+}
+
+}  // extern "C"

@@ -53,17 +53,18 @@ bool stream_of(PyObject* o, uint64_t* out) {
 // call(entry point's address, "kinds of its arguments", arguments...) -> its return code.  Kinds: p a device
 // address (tensor, int or None), i an int32, h a handle as an int, s the stream.  Every argument is of the
 // integer class, so it travels in a 64-bit register or stack slot whatever its width.
-constexpr int kMost = 9;
+// (MOST: how many an entry point may take, so that the ones of few are not handed more.)
+template <int MOST>
 PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   Py_ssize_t n = 0;
   const char* kinds = nargs >= 2 ? PyUnicode_AsUTF8AndSize(args[1], &n) : nullptr;
-  if (kinds == nullptr || n != nargs - 2 || n < 1 || n > kMost) {
+  if (kinds == nullptr || n != nargs - 2 || n < 1 || n > MOST) {
     if (!PyErr_Occurred()) PyErr_SetString(PyExc_TypeError, "call(address, kinds, arguments...)");
     return nullptr;
   }
   const uint64_t entry = PyLong_AsUnsignedLongLong(args[0]);
   if (entry == (uint64_t)-1 && PyErr_Occurred()) return nullptr;
-  uint64_t a[kMost] = {};
+  uint64_t a[MOST] = {};
   for (Py_ssize_t i = 0; i < n; ++i) {
     PyObject* o = args[i + 2];
     bool ok = true;
@@ -81,16 +82,22 @@ PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     if (!ok) return nullptr;
   }
   int code;
-  typedef int (*Entry)(uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t,
-                       uint64_t);
+  typedef uint64_t U;
+  typedef int (*Entry)(U, U, U, U, U, U, U, U, U);
+  typedef int (*LongEntry)(U, U, U, U, U, U, U, U, U, U);
   Py_BEGIN_ALLOW_THREADS  // (arguments past the entry point's own are not looked at)
-  code = reinterpret_cast<Entry>(entry)(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8]);
+  if constexpr (MOST == 9)
+    code = reinterpret_cast<Entry>(entry)(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8]);
+  else
+    code = reinterpret_cast<LongEntry>(entry)(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9]);
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(code);
 }
 
-PyMethodDef methods[] = {{"call", (PyCFunction)(void (*)(void))call, METH_FASTCALL,
+PyMethodDef methods[] = {{"call", (PyCFunction)(void (*)(void))call<9>, METH_FASTCALL,
                           "call(address, kinds, arguments...) -> return code"},
+                         {"call_ten", (PyCFunction)(void (*)(void))call<10>, METH_FASTCALL,
+                          "call, for entry points of up to ten arguments"},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
