@@ -643,6 +643,7 @@ int eep_route(const eep_router_shape* shape, const void* logits, int32_t* topk_i
  * workspace: their kernels may not overlap (one stream, or events between); handles are
  * independent.  eep_product_destroy waits for the device.
  *   num_slots      1 to 65536;  max_rows  0 to 2^30: the most that a call may pass
+ *   in_features, out_features   1 to 2^21
  *   in_features    rows of x and w must be multiples of 16 bytes (EEP_ERR_ALIGN), and whole scale
  *                  blocks for fp8 (EEP_ERR_INVALID_ARG)
  *   out_features   rows of y must be multiples of 16 bytes; a multiple of 128 where y is fp8 or

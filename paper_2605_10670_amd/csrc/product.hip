@@ -7,6 +7,7 @@
 // l takes 16 bytes of row l % 16 at 16 * (l / 16) and 16 more 64 bytes on, of both operands alike: a product of sums
 // does not ask in which order its terms come, so the matrix cores' own order of k plays no part.
 #include <new>
+#include <type_traits>
 
 #include "eep_internal.hpp"
 #include "numbers.hpp"
@@ -15,6 +16,7 @@
 struct eep_product {
   eep_product_config cfg;
   int64_t slot_stride, scale_stride;  // bytes
+  int cus;                            // of the device
 };
 
 namespace eep {
@@ -89,6 +91,43 @@ __device__ __forceinline__ f32x4 mma(const Frag& a, const Frag& b, f32x4 acc) {
     return acc;
   }
 }
+
+// An operand of mma, ready to be used several times.  WIDE: e4m3 codes are widened to bf16 (once), see above; else they are
+// multiplied as they are, where the sums are rounded to 16 or 8 bits anyway.
+template <int DT, bool WIDE>
+struct Operand {
+  Frag f;
+  __device__ __forceinline__ void set(const Frag& v) { f = v; }
+  __device__ __forceinline__ f32x4 times(const Operand& b, f32x4 acc) const {
+    if constexpr (DT == EEP_FP8_E4M3) {
+      i32x8 av, bv;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        av[i] = (int)f.c[0][i];
+        av[4 + i] = (int)f.c[1][i];
+        bv[i] = (int)b.f.c[0][i];
+        bv[4 + i] = (int)b.f.c[1][i];
+      }
+      return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(av, bv, acc, 0, 0, 0, 0, 0, 0);
+    } else {
+      return mma<DT>(f, b.f, acc);
+    }
+  }
+};
+template <>
+struct Operand<EEP_FP8_E4M3, true> {
+  bf16x8 v[2][2];
+  __device__ __forceinline__ void set(const Frag& f) {
+    widen(f.c[0], v[0]);
+    widen(f.c[1], v[1]);
+  }
+  __device__ __forceinline__ f32x4 times(const Operand& b, f32x4 acc) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[i >> 1][i & 1], b.v[i >> 1][i & 1], acc, 0, 0, 0);
+    return acc;
+  }
+};
 
 // v / (1 + exp(-v)) * u
 __device__ __forceinline__ float silu_times(float v, float u) { return v / (1.0f + expf(-v)) * u; }
@@ -305,6 +344,371 @@ __global__ __launch_bounds__(64 * kThinWaves) void k_product_thin(ProductArgs a,
   }
 }
 
+// ---------------------------------------------------------------------------
+// many rows a slot: tiles through LDS.
+//
+// A workgroup of 8 wavefronts has 256 weight rows (with the gate 128 of each factor) by 64 * TT tokens; two wavefronts share
+// the weight rows, four the tokens, so that one holds 128 by 16 * TT sums and reads 128 + 16 * TT rows of a step for
+// them.  A step's rows go from memory to LDS without passing through registers, STAGES - 1 steps ahead; a row's eight
+// 16-byte chunks lie in LDS at their number XOR the row's, so that the 16 rows of a tile are read without bank
+// conflicts although each begins at the same bank.
+//
+// The workgroups stay: each goes through its share of the work items, an item being a tile.  Workgroups of one XCD
+// (every eighth) have neighbouring items, those of one slot with the row tiles innermost: what runs at a time
+// shares weights and rows in that XCD's L2.
+// ---------------------------------------------------------------------------
+constexpr int kTiledWaves = 8, kTiledRows = 256;
+constexpr int kTiledThreads = 64 * kTiledWaves;
+__host__ __device__ constexpr int tiled_stages(int tt) { return tt == 4 ? 2 : 3; }
+__host__ __device__ constexpr int tiled_stage_bytes(int tt) { return (kTiledRows + 64 * tt) * kStepBytes; }
+
+typedef __attribute__((address_space(3))) void lds_void;
+typedef const __attribute__((address_space(1))) void global_void;
+
+// The tiles of the slots: what one wavefront has to remember to find any of them.
+template <int TOKENS>
+struct TileMap {
+  int run;   // slots a lane counts
+  int upto;  // tiles of the slots up to the end of this lane's run
+  int total;
+
+  __device__ __forceinline__ static int tiles_of(int lo, int hi) { return hi > lo ? (hi - lo + TOKENS - 1) / TOKENS : 0; }
+  __device__ __forceinline__ static int bound(const ProductArgs& a, int p) {
+    const int o = a.offset[p];
+    return o < 0 ? 0 : o > a.rows ? a.rows : o;
+  }
+  __device__ __forceinline__ static int running_sum(int v) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int other = __shfl_up(v, d, 64);
+      if (lane >= d) v += other;
+    }
+    return v;
+  }
+
+  __device__ __forceinline__ void make(const ProductArgs& a) {
+    if (a.offset == nullptr) {
+      total = tiles_of(0, a.rows);
+      return;
+    }
+    const int lane = threadIdx.x & 63;
+    run = (a.slots + 63) / 64;
+    const int p0 = lane * run, p1 = p0 + run < a.slots ? p0 + run : a.slots;
+    int mine = 0;
+    if (p0 < p1) {
+      int lo = bound(a, p0);
+      for (int p = p0; p < p1; ++p) {
+        const int hi = bound(a, p + 1);
+        mine += tiles_of(lo, hi);
+        lo = hi;
+      }
+    }
+    upto = running_sum(mine);
+    total = __builtin_amdgcn_readlane(upto, 63);
+  }
+
+  // Item `item` of total * feature_tiles: slot, feature tile, first row and the end of the slot's rows.
+  __device__ __forceinline__ void find(const ProductArgs& a, int64_t item, int* slot, int* feature_tile, int* first,
+                                       int* end) const {
+    if (a.offset == nullptr) {
+      *slot = 0;
+      *feature_tile = (int)(item / total);
+      *first = (int)(item - (int64_t)*feature_tile * total) * TOKENS;
+      *end = a.rows;
+      return;
+    }
+    const int lane = threadIdx.x & 63;
+    const int owner = __builtin_ctzll(__ballot((int64_t)upto * a.feature_tiles > item));
+    int before = owner > 0 ? __builtin_amdgcn_readlane(upto, owner - 1) : 0;
+    for (int p0 = owner * run;; p0 += 64) {
+      // the lanes look at 64 slots of the run; the item is in one of the run's
+      const int p = p0 + lane;
+      const bool in = p < (owner + 1) * run && p < a.slots;
+      const int lo = in ? bound(a, p) : 0, hi = in ? bound(a, p + 1) : 0;
+      const int tiles = tiles_of(lo, hi);
+      const int sum = before + running_sum(tiles);
+      const uint64_t behind = __ballot((int64_t)sum * a.feature_tiles > item);
+      if (behind != 0) {
+        const int who = __builtin_ctzll(behind);
+        const int n = __builtin_amdgcn_readlane(tiles, who);
+        const int left = (int)(item - (int64_t)(__builtin_amdgcn_readlane(sum, who) - n) * a.feature_tiles);
+        *slot = p0 + who;
+        *feature_tile = left / n;
+        *first = __builtin_amdgcn_readlane(lo, who) + (left - *feature_tile * n) * TOKENS;
+        *end = __builtin_amdgcn_readlane(hi, who);
+        return;
+      }
+      if (p0 + 64 >= (owner + 1) * run) {  // (offsets that changed while the kernel ran)
+        *slot = *feature_tile = *first = *end = 0;
+        return;
+      }
+      before = __builtin_amdgcn_readlane(sum, 63);
+    }
+  }
+};
+
+template <int DT, bool WIDE, int YT, bool GATE, int TT>
+__global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs a) {
+  constexpr int kStages = tiled_stages(TT), kTokens = 64 * TT, kStage = tiled_stage_bytes(TT);
+  constexpr int kLoads = (kTiledRows + kTokens) / 8 / kTiledWaves;  // of 8 rows each, a wavefront and step
+  constexpr int kWeightLoads = kTiledRows / 8 / kTiledWaves;
+  extern __shared__ __align__(1024) uint8_t lds[];
+  uint32_t* s_top = (uint32_t*)(lds + kStages * kStage);  // [2][kTokens]
+
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave & 1, wn = wave >> 1;
+  const int col = lane & 15, part = lane >> 4;
+
+  TileMap<kTokens> map;
+  map.make(a);
+  const int64_t items = (int64_t)map.total * a.feature_tiles;
+  // the items of this workgroup: those of its XCD, every so manieth
+  const int xcds = gridDim.x % 8 == 0 ? 8 : 1;
+  const int xcd = blockIdx.x % xcds, seat = blockIdx.x / xcds, seats = gridDim.x / xcds;
+  const int64_t from = items * xcd / xcds, to = items * (xcd + 1) / xcds;
+
+  const int weight_rows = GATE ? 2 * a.features : a.features;
+  const int full_steps = a.row_bytes / kStepBytes;
+  const int tail = a.row_bytes - full_steps * kStepBytes;
+  const int steps = full_steps + (tail != 0 ? 1 : 0);
+
+  // what the lane loads: 16 bytes of row `lane / 8` of eight
+  const int load_row = lane >> 3, load_chunk = (lane & 7) ^ load_row;
+  const int tail_chunk = load_chunk * 16 < tail ? load_chunk : 0;  // past the row's end: anything of it
+  // what it reads of a tile of 16 rows: two chunks
+  const int read_at = col * kStepBytes + ((part ^ (col & 7)) << 4);
+
+  struct Tile {
+    int slot, feature_tile, first, end;
+  };
+  Tile t = {}, next = {};
+  const uint8_t *w_base, *x_base;      // of the tile whose rows are loaded
+  uint32_t row_at[kLoads];             // first byte of the lane's rows from there
+  auto aim = [&](const Tile& tile) {
+    const int half = GATE ? 128 : 256;  // weight rows in one piece
+    const int n0 = tile.feature_tile * half;
+    const int piece = GATE && wave >= kTiledWaves / 2 ? 1 : 0;
+    w_base = a.w + tile.slot * a.slot_stride + (int64_t)(n0 + piece * a.features) * a.row_bytes;
+    x_base = a.x + (int64_t)tile.first * a.row_bytes;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      int r;
+      if (i < kWeightLoads) {
+        r = (wave * kWeightLoads + i) * 8 + load_row - piece * half;
+        r = n0 + r < a.features ? r : a.features - 1 - n0;
+      } else {
+        r = (wave * (kLoads - kWeightLoads) + i - kWeightLoads) * 8 + load_row;
+        r = tile.first + r < tile.end ? r : tile.end - 1 - tile.first;
+        r = r > 0 ? r : 0;
+      }
+      row_at[i] = (uint32_t)r * (uint32_t)a.row_bytes;
+    }
+  };
+  auto fetch = [&](int step, int stage) {
+    const uint32_t at = (uint32_t)(step * kStepBytes + (step < full_steps ? load_chunk : tail_chunk) * 16);
+    uint8_t* to_lds = lds + stage * kStage;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int group = i < kWeightLoads ? wave * kWeightLoads + i
+                                         : kTiledRows / 8 + wave * (kLoads - kWeightLoads) + i - kWeightLoads;
+      const uint8_t* base = i < kWeightLoads ? w_base : x_base;
+      __builtin_amdgcn_global_load_lds((global_void*)(base + (row_at[i] + at)), (lds_void*)(to_lds + group * 8 * kStepBytes),
+                                       16, 0, 0);
+    }
+  };
+
+  int64_t item = from + seat;
+  if (item >= to) return;
+  map.find(a, item, &t.slot, &t.feature_tile, &t.first, &t.end);
+  aim(t);
+#pragma unroll
+  for (int s = 0; s < kStages - 1; ++s)
+    if (s < steps) fetch(s, s);
+
+  for (;;) {
+    const bool more = item + seats < to;
+    if (more) map.find(a, item + seats, &next.slot, &next.feature_tile, &next.first, &next.end);
+
+    // scales: of the lane's token of each tile, and of the wavefront's weight rows (a block of 128 or, gated, one of each factor)
+    const float *x_scale = nullptr, *w_scale = nullptr;
+    uint32_t sx[TT];
+    float sx_now[TT], sw_now[2];
+    const int up = GATE ? a.features / kScaleBlock * steps : 0;
+    if constexpr (DT == EEP_FP8_E4M3) {
+      x_scale = a.x_scale + (int64_t)t.first * steps;
+#pragma unroll
+      for (int j = 0; j < TT; ++j) {
+        int r = (wn * TT + j) * 16 + col;
+        r = t.first + r < t.end ? r : t.end - 1 - t.first;
+        sx[j] = (uint32_t)(r > 0 ? r : 0) * (uint32_t)steps;
+        sx_now[j] = x_scale[sx[j]];
+      }
+      int block = GATE ? t.feature_tile : 2 * t.feature_tile + wm;
+      const int last = (weight_rows - 1) / kScaleBlock;
+      block = block < last ? block : last;
+      w_scale = (const float*)((const uint8_t*)a.w_scale + t.slot * a.scale_stride) + (int64_t)block * steps;
+      sw_now[0] = w_scale[0];
+      sw_now[1] = w_scale[up];
+    }
+
+    f32x4 acc[8][TT];
+#pragma unroll
+    for (int f = 0; f < 8; ++f)
+#pragma unroll
+      for (int j = 0; j < TT; ++j) acc[f][j] = f32x4{0, 0, 0, 0};
+
+    auto step = [&](int s, auto is_cut) {
+      constexpr bool kCut = decltype(is_cut)::value;  // the last step of rows that end within it
+      // this step's rows are there once no more than the steps behind it are under way; and all wavefronts have read the
+      // stage that is filled next
+      if (kStages > 2 && s + 1 < steps)
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kStages - 2) * kLoads) : "memory");
+      else
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      float sx_next[TT], sw_next[2];
+      if constexpr (DT == EEP_FP8_E4M3) {
+        const int n = s + 1 < steps ? s + 1 : s;
+#pragma unroll
+        for (int j = 0; j < TT; ++j) sx_next[j] = x_scale[sx[j] + (uint32_t)n];
+        sw_next[0] = w_scale[n];
+        sw_next[1] = w_scale[up + n];
+      }
+      if (s + kStages - 1 < steps) fetch(s + kStages - 1, (s + kStages - 1) % kStages);
+
+      const uint8_t* stage = lds + (s % kStages) * kStage;
+      auto read = [&](int tile_row) {
+        Frag f;
+        const uint8_t* at = stage + tile_row * kStepBytes + read_at;
+        f.c[0] = *(const u32x4*)at;
+        f.c[1] = *(const u32x4*)(stage + tile_row * kStepBytes + (read_at ^ 64));
+        if constexpr (kCut) {
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+            if (j * 64 + part * 16 >= tail) f.c[j] = u32x4{0, 0, 0, 0};
+        }
+        return f;
+      };
+      Operand<DT, WIDE> b[TT];
+#pragma unroll
+      for (int j = 0; j < TT; ++j) b[j].set(read(kTiledRows + (wn * TT + j) * 16));
+      auto row_of_tile = [&](int f) {
+        return GATE ? (f < 4 ? wm * 64 + f * 16 : 128 + wm * 64 + (f - 4) * 16) : wm * 128 + f * 16;
+      };
+      Frag ahead = read(row_of_tile(0));
+#pragma unroll
+      for (int f = 0; f < 8; ++f) {
+        Operand<DT, WIDE> av;
+        av.set(ahead);
+        if (f < 7) ahead = read(row_of_tile(f + 1));
+        if constexpr (DT == EEP_FP8_E4M3) {
+          f32x4 p[TT];
+#pragma unroll
+          for (int j = 0; j < TT; ++j) p[j] = av.times(b[j], f32x4{0, 0, 0, 0});
+#pragma unroll
+          for (int j = 0; j < TT; ++j) {
+            const float scale = sx_now[j] * sw_now[GATE ? f / 4 : 0];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[f][j][i] = fmaf(p[j][i], scale, acc[f][j][i]);
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < TT; ++j) acc[f][j] = av.times(b[j], acc[f][j]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if constexpr (DT == EEP_FP8_E4M3) {
+#pragma unroll
+        for (int j = 0; j < TT; ++j) sx_now[j] = sx_next[j];
+        sw_now[0] = sw_next[0];
+        sw_now[1] = sw_next[1];
+      }
+    };
+    for (int s = 0; s < full_steps; ++s) step(s, std::false_type());
+    if constexpr (DT != EEP_FP8_E4M3)
+      if (tail != 0) step(full_steps, std::true_type());
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    // the next tile's first rows are on their way while this one's results are stored
+    if (more) {
+      aim(next);
+#pragma unroll
+      for (int s = 0; s < kStages - 1; ++s)
+        if (s < steps) fetch(s, s);
+    }
+
+    if constexpr (GATE) {
+      const int n0 = t.feature_tile * 128 + wm * 64 + part * 4;
+      uint32_t top[TT];
+#pragma unroll
+      for (int j = 0; j < TT; ++j) {
+        top[j] = 0;
+#pragma unroll
+        for (int f = 0; f < 4; ++f) {
+          float v[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[f][j][i] = v[i] = silu_times(acc[f][j][i], acc[f + 4][j][i]);
+          const uint32_t m = top_magnitude<4>(v);
+          top[j] = m > top[j] ? m : top[j];
+        }
+      }
+      if constexpr (YT == EEP_FP8_E4M3) {
+#pragma unroll
+        for (int j = 0; j < TT; ++j) {
+          top[j] = max(top[j], (uint32_t)__shfl_xor((int)top[j], 16, 64));
+          top[j] = max(top[j], (uint32_t)__shfl_xor((int)top[j], 32, 64));
+          if (part == 0) s_top[wm * kTokens + (wn * TT + j) * 16 + col] = top[j];
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int j = 0; j < TT; ++j) {
+          const int at = (wn * TT + j) * 16 + col;
+          const uint32_t other = s_top[(wm ^ 1) * kTokens + at];
+          const float scale = scale_of(max(top[j], other));
+          const int64_t row = t.first + at;
+          if (row < t.end) {
+#pragma unroll
+            for (int f = 0; f < 4; ++f)
+              *(uint32_t*)(a.y + row * a.features + n0 + f * 16) =
+                  codes4(acc[f][j][0], acc[f][j][1], acc[f][j][2], acc[f][j][3], scale);
+            if (wm == 0 && part == 0) a.y_scale[row * a.feature_tiles + t.feature_tile] = scale;
+          }
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < TT; ++j) {
+          const int64_t row = t.first + (wn * TT + j) * 16 + col;
+#pragma unroll
+          for (int f = 0; f < 4; ++f) {
+            const float v[4] = {acc[f][j][0], acc[f][j][1], acc[f][j][2], acc[f][j][3]};
+            if (row < t.end && n0 + f * 16 < a.features) store4<YT>(a.y, row * a.features + n0 + f * 16, v);
+          }
+        }
+      }
+    } else {
+      const int n0 = t.feature_tile * 256 + wm * 128 + part * 4;
+#pragma unroll
+      for (int j = 0; j < TT; ++j) {
+        const int64_t row = t.first + (wn * TT + j) * 16 + col;
+#pragma unroll
+        for (int f = 0; f < 8; ++f) {
+          const float v[4] = {acc[f][j][0], acc[f][j][1], acc[f][j][2], acc[f][j][3]};
+          if (row < t.end && n0 + f * 16 < a.features) store4<YT>(a.y, row * a.features + n0 + f * 16, v);
+        }
+      }
+    }
+    if (!more) return;
+    item += seats;
+    t = next;
+  }
+}
+
 // Tiles of `tokens` rows that the slots may have at most.
 int64_t most_tiles(int rows, int slots, int tokens) {
   const int64_t touched = rows < slots ? rows : slots;
@@ -312,7 +716,7 @@ int64_t most_tiles(int rows, int slots, int tokens) {
 }
 
 template <int DT, int YT, bool GATE>
-hipError_t launch_product(ProductArgs a, hipStream_t st) {
+hipError_t launch_thin(ProductArgs a, hipStream_t st) {
   const int features = GATE ? 16 * kThinWaves : 32 * kThinWaves;
   a.feature_tiles = (a.features + features - 1) / features;
   const int64_t work = most_tiles(a.rows, a.slots, kThinTokens) * a.feature_tiles;
@@ -322,15 +726,39 @@ hipError_t launch_product(ProductArgs a, hipStream_t st) {
   });
 }
 
+template <int DT, int YT, bool GATE, int TT>
+hipError_t launch_tiled(ProductArgs a, int cus, hipStream_t st) {
+  constexpr bool kWide = DT == EEP_FP8_E4M3 && YT == EEP_F32;
+  constexpr int kLds = tiled_stages(TT) * tiled_stage_bytes(TT) + 2 * 64 * TT * (int)sizeof(uint32_t);
+  const auto kernel = k_product_tiled<DT, kWide, YT, GATE, TT>;
+  static const hipError_t allowed =
+      hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+  if (allowed != hipSuccess) return allowed;
+  const int features = GATE ? kTiledRows / 2 : kTiledRows;
+  a.feature_tiles = (a.features + features - 1) / features;
+  const int64_t work = most_tiles(a.rows, a.slots, 64 * TT) * a.feature_tiles;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(work < cus ? work : cus)), dim3(kTiledThreads), kLds, st, a);
+  return hipGetLastError();
+}
+
+template <int DT, int YT, bool GATE>
+hipError_t launch_product(const ProductArgs& a, int cus, hipStream_t st) {
+  const int mean = (a.rows + a.slots - 1) / a.slots;  // rows a slot
+  if (mean <= 16) return launch_thin<DT, YT, GATE>(a, st);
+  if (mean <= 64) return launch_tiled<DT, YT, GATE, 1>(a, cus, st);
+  if (mean <= 160) return launch_tiled<DT, YT, GATE, 2>(a, cus, st);
+  return launch_tiled<DT, YT, GATE, 4>(a, cus, st);
+}
+
 template <int DT>
-hipError_t launch_product(const ProductArgs& a, int y_dtype, bool gate, hipStream_t st) {
+hipError_t launch_product(const ProductArgs& a, int y_dtype, bool gate, int cus, hipStream_t st) {
   if (gate) {
-    if (y_dtype == EEP_FP8_E4M3) return launch_product<DT, EEP_FP8_E4M3, true>(a, st);
-    if (y_dtype == EEP_BF16) return launch_product<DT, EEP_BF16, true>(a, st);
-    return launch_product<DT, EEP_F32, true>(a, st);
+    if (y_dtype == EEP_FP8_E4M3) return launch_product<DT, EEP_FP8_E4M3, true>(a, cus, st);
+    if (y_dtype == EEP_BF16) return launch_product<DT, EEP_BF16, true>(a, cus, st);
+    return launch_product<DT, EEP_F32, true>(a, cus, st);
   }
-  if (y_dtype == EEP_BF16) return launch_product<DT, EEP_BF16, false>(a, st);
-  return launch_product<DT, EEP_F32, false>(a, st);
+  if (y_dtype == EEP_BF16) return launch_product<DT, EEP_BF16, false>(a, cus, st);
+  return launch_product<DT, EEP_F32, false>(a, cus, st);
 }
 
 }  // namespace eep
@@ -346,7 +774,7 @@ int eep_product_create(const eep_product_config* cfg, eep_product** out) {
   const eep_product_config& f = *cfg;
   const bool fp8 = f.x_dtype == EEP_FP8_E4M3, gated = f.gate == EEP_GATE_SILU;
   if (f.num_slots < 1 || f.num_slots > 65536 || f.in_features < 1 || f.out_features < 1 ||
-      f.in_features > (1 << 24) || f.out_features > (1 << 24) || f.max_rows < 0 || f.max_rows > (1 << 30))
+      f.in_features > (1 << 21) || f.out_features > (1 << 21) || f.max_rows < 0 || f.max_rows > (1 << 30))
     return EEP_ERR_INVALID_ARG;
   if ((f.x_dtype != EEP_F32 && f.x_dtype != EEP_BF16 && !fp8) ||
       (f.y_dtype != EEP_F32 && f.y_dtype != EEP_BF16 && f.y_dtype != EEP_FP8_E4M3) ||
@@ -368,6 +796,13 @@ int eep_product_create(const eep_product_config* cfg, eep_product** out) {
   eep_product* p = new (std::nothrow) eep_product();
   if (!p) return EEP_ERR_INVALID_ARG;
   p->cfg = f;
+  int device = 0;
+  if (hipGetDevice(&device) != hipSuccess ||
+      hipDeviceGetAttribute(&p->cus, hipDeviceAttributeMultiprocessorCount, device) != hipSuccess) {
+    (void)hipGetLastError();
+    delete p;
+    return EEP_ERR_HIP;
+  }
   p->slot_stride = f.slot_stride ? f.slot_stride : packed;
   p->scale_stride = f.scale_stride ? f.scale_stride : packed_scale;
   *out = p;
@@ -410,9 +845,9 @@ int eep_expert_product(eep_product* product, const void* x, const float* x_scale
   const bool gate = f.gate == EEP_GATE_SILU;
   hipError_t e;
   switch (f.x_dtype) {
-    case EEP_FP8_E4M3: e = launch_product<EEP_FP8_E4M3>(a, f.y_dtype, gate, (hipStream_t)stream); break;
-    case EEP_BF16: e = launch_product<EEP_BF16>(a, f.y_dtype, gate, (hipStream_t)stream); break;
-    default: e = launch_product<EEP_F32>(a, f.y_dtype, gate, (hipStream_t)stream);
+    case EEP_FP8_E4M3: e = launch_product<EEP_FP8_E4M3>(a, f.y_dtype, gate, product->cus, (hipStream_t)stream); break;
+    case EEP_BF16: e = launch_product<EEP_BF16>(a, f.y_dtype, gate, product->cus, (hipStream_t)stream); break;
+    default: e = launch_product<EEP_F32>(a, f.y_dtype, gate, product->cus, (hipStream_t)stream);
   }
   return e == hipSuccess ? EEP_OK : EEP_ERR_HIP;
 }

@@ -68,7 +68,7 @@ def check_rounded(y, exact, err):
 
 
 def product_case(seed, counts, K, N, x="bf16", gate=False, spare=0):
-    """Inputs on the CPU and the exact result: rows of every slot in counts, `spare` rows behind the last."""
+    """Inputs on the CPU and the exact sums: rows of every slot in counts, `spare` rows behind the last."""
     g = gen(seed)
     P, rows = len(counts), sum(counts) + spare
     weight_rows = N * (2 if gate else 1)
@@ -88,9 +88,9 @@ def product_case(seed, counts, K, N, x="bf16", gate=False, spare=0):
 
 
 def exact(c, xd, wd):
-    """c["want"] and c["err"]: the result in 64 bits, and what K additions in fp32 (in any order, each term and each
-    sum rounded, or cut off by a matrix core's alignment) may be off: K * 2^-23 of the sum of magnitudes."""
-    N, K = c["N"], c["K"]
+    """c["sums"] in 64 bits, and c["sum_err"], what K additions in fp32 (in any order, each term and each sum rounded,
+    or cut off by a matrix core's alignment) may be off: K * 2^-23 of the sum of magnitudes."""
+    K = c["K"]
     s = torch.zeros((c["rows"], wd.shape[1]), dtype=torch.float64)
     m = torch.zeros_like(s)
     off = c["offset"].tolist()
@@ -98,16 +98,35 @@ def exact(c, xd, wd):
         lo, hi = off[p], off[p + 1]
         s[lo:hi] = xd[lo:hi] @ wd[p].t()
         m[lo:hi] = xd[lo:hi].abs() @ wd[p].abs().t()
-    e = m * (K + 8) * 2.0 ** -23
-    if c["gate"]:
-        a, u = s[:, :N], s[:, N:]
-        act = a * torch.sigmoid(a)
-        # |silu'| < 1.1; the exponential, the quotient and the product round a few times each
-        err = 1.1 * e[:, :N] * (u.abs() + e[:, N:]) + act.abs() * e[:, N:] + (act * u).abs() * 16 * 2.0 ** -23
-        c["want"], c["err"] = act * u, err
-    else:
-        c["want"], c["err"] = s, e
-    c["routed"] = off[-1]
+    c["sums"], c["sum_err"] = s, m * (K + 8) * 2.0 ** -23
+    c["xd"], c["wd"], c["routed"] = xd, wd, off[-1]
+
+
+def lost_by_alignment(c):
+    """What the matrix cores' 8-bit forms may lose: of every 8 neighbouring products each keeps the bits down to 2^-13 of
+    the largest."""
+    lost = torch.zeros_like(c["sums"])
+    off = c["offset"].tolist()
+    for p in range(c["P"]):
+        x, w = c["xd"][off[p]:off[p + 1]].cuda().float(), c["wd"][p].cuda().float()
+        if x.shape[0]:
+            part = sum((x[:, None, k:k + 8] * w[None, :, k:k + 8]).abs().amax(dim=2).double() for k in range(0, c["K"], 8))
+            lost[off[p]:off[p + 1]] = part.cpu() * 8 * 2.0 ** -13 * (1 + 2.0 ** -22)
+    return lost
+
+
+def result(c, y):
+    """(the product in 64 bits, what it may be off before it is rounded to y)."""
+    N, s, e = c["N"], c["sums"], c["sum_err"]
+    if c["xt"] == "fp8" and y != "f32":
+        e = e + lost_by_alignment(c)
+    if not c["gate"]:
+        return s, e
+    a, u = s[:, :N], s[:, N:]
+    act = a * torch.sigmoid(a)
+    # |silu'| < 1.1; the exponential, the quotient and the product round a few times each
+    err = 1.1 * e[:, :N] * (u.abs() + e[:, N:]) + act.abs() * e[:, N:] + (act * u).abs() * 16 * 2.0 ** -23
+    return act * u, err
 
 
 SENTINEL = 77.0
@@ -134,7 +153,7 @@ def run_product(c, y="bf16", product=None, dense=False, stream=None):
 def check_product(c, y, out, y_scale):
     n = c["routed"]
     assert (out[n:].float() == torch.tensor(SENTINEL).to(out.dtype).float()).all(), "rows outside the slots were written"
-    want, err = c["want"][:n], c["err"][:n]
+    want, err = (t[:n] for t in result(c, y))
     if y == "fp8":
         assert (y_scale[n:] == SENTINEL).all()
         check_codes(out[:n], y_scale[:n], want, err)
