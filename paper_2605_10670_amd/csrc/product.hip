@@ -360,7 +360,10 @@ __global__ __launch_bounds__(64 * kThinWaves) void k_product_thin(ProductArgs a,
 constexpr int kTiledWaves = 8, kTiledRows = 256;
 constexpr int kTiledThreads = 64 * kTiledWaves;
 __host__ __device__ constexpr int tiled_stages(int tt) { return tt == 4 ? 2 : 3; }
-__host__ __device__ constexpr int tiled_stage_bytes(int tt) { return (kTiledRows + 64 * tt) * kStepBytes; }
+// A stage: the weight rows of a step, the tokens' rows, and for codes the tokens' scales and two of the weights'.
+__host__ __device__ constexpr int tiled_stage_bytes(bool codes, int tt) {
+  return (kTiledRows + 64 * tt) * kStepBytes + (codes ? 64 * tt * 4 + 128 : 0);
+}
 
 typedef __attribute__((address_space(3))) void lds_void;
 typedef const __attribute__((address_space(1))) void global_void;
@@ -450,8 +453,12 @@ struct TileMap {
 
 template <int DT, bool WIDE, int YT, bool GATE, int TT>
 __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs a) {
-  constexpr int kStages = tiled_stages(TT), kTokens = 64 * TT, kStage = tiled_stage_bytes(TT);
+  constexpr int kStages = tiled_stages(TT), kTokens = 64 * TT;
+  constexpr bool kCodes = DT == EEP_FP8_E4M3;
+  constexpr int kStage = tiled_stage_bytes(kCodes, TT);
   constexpr int kLoads = (kTiledRows + kTokens) / 8 / kTiledWaves;  // of 8 rows each, a wavefront and step
+  constexpr int kScales = (kTiledRows + kTokens) * kStepBytes;      // where a stage has them: tokens', weights'
+  constexpr int kScaleLanes = kTokens / kTiledWaves;                 // tokens whose scales a wavefront loads
   constexpr int kWeightLoads = kTiledRows / 8 / kTiledWaves;
   extern __shared__ __align__(1024) uint8_t lds[];
   uint32_t* s_top = (uint32_t*)(lds + kStages * kStage);  // [2][kTokens]
@@ -486,6 +493,8 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
   Tile t = {}, next = {};
   const uint8_t *w_base, *x_base;      // of the tile whose rows are loaded
   uint32_t row_at[kLoads];             // first byte of the lane's rows from there
+  const float* scale_base = nullptr;   // and the scale that it loads, if any, of a step
+  const bool loads_scale = kCodes && lane < kScaleLanes + (wave == kTiledWaves - 1 ? 2 : 0);
   auto aim = [&](const Tile& tile) {
     const int half = GATE ? 128 : 256;  // weight rows in one piece
     const int n0 = tile.feature_tile * half;
@@ -505,6 +514,20 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
       }
       row_at[i] = (uint32_t)r * (uint32_t)a.row_bytes;
     }
+    if constexpr (kCodes) {
+      // a token's; behind the last wavefront's those of the two blocks of 128 weight rows
+      if (lane < kScaleLanes) {
+        int r = wave * kScaleLanes + lane;
+        r = tile.first + r < tile.end ? r : tile.end - 1 - tile.first;
+        scale_base = a.x_scale + (tile.first + (int64_t)(r > 0 ? r : 0)) * steps;
+      } else {
+        const int second = lane == kScaleLanes ? 0 : 1;
+        int block = GATE ? tile.feature_tile + second * (a.features / kScaleBlock) : 2 * tile.feature_tile + second;
+        const int last = (weight_rows - 1) / kScaleBlock;
+        block = block < last ? block : last;
+        scale_base = (const float*)((const uint8_t*)a.w_scale + tile.slot * a.scale_stride) + (int64_t)block * steps;
+      }
+    }
   };
   auto fetch = [&](int step, int stage) {
     const uint32_t at = (uint32_t)(step * kStepBytes + (step < full_steps ? load_chunk : tail_chunk) * 16);
@@ -516,6 +539,11 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
       const uint8_t* base = i < kWeightLoads ? w_base : x_base;
       __builtin_amdgcn_global_load_lds((global_void*)(base + (row_at[i] + at)), (lds_void*)(to_lds + group * 8 * kStepBytes),
                                        16, 0, 0);
+    }
+    if constexpr (kCodes) {
+      if (loads_scale)
+        __builtin_amdgcn_global_load_lds((global_void*)(scale_base + step),
+                                         (lds_void*)(to_lds + kScales + wave * kScaleLanes * 4), 4, 0, 0);
     }
   };
 
@@ -531,28 +559,6 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
     const bool more = item + seats < to;
     if (more) map.find(a, item + seats, &next.slot, &next.feature_tile, &next.first, &next.end);
 
-    // scales: of the lane's token of each tile, and of the wavefront's weight rows (a block of 128 or, gated, one of each factor)
-    const float *x_scale = nullptr, *w_scale = nullptr;
-    uint32_t sx[TT];
-    float sx_now[TT], sw_now[2];
-    const int up = GATE ? a.features / kScaleBlock * steps : 0;
-    if constexpr (DT == EEP_FP8_E4M3) {
-      x_scale = a.x_scale + (int64_t)t.first * steps;
-#pragma unroll
-      for (int j = 0; j < TT; ++j) {
-        int r = (wn * TT + j) * 16 + col;
-        r = t.first + r < t.end ? r : t.end - 1 - t.first;
-        sx[j] = (uint32_t)(r > 0 ? r : 0) * (uint32_t)steps;
-        sx_now[j] = x_scale[sx[j]];
-      }
-      int block = GATE ? t.feature_tile : 2 * t.feature_tile + wm;
-      const int last = (weight_rows - 1) / kScaleBlock;
-      block = block < last ? block : last;
-      w_scale = (const float*)((const uint8_t*)a.w_scale + t.slot * a.scale_stride) + (int64_t)block * steps;
-      sw_now[0] = w_scale[0];
-      sw_now[1] = w_scale[up];
-    }
-
     f32x4 acc[8][TT];
 #pragma unroll
     for (int f = 0; f < 8; ++f)
@@ -564,19 +570,11 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
       // this step's rows are there once no more than the steps behind it are under way; and all wavefronts have read the
       // stage that is filled next
       if (kStages > 2 && s + 1 < steps)
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kStages - 2) * kLoads) : "memory");
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kStages - 2) * (kLoads + (kCodes ? 1 : 0))) : "memory");
       else
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
-      float sx_next[TT], sw_next[2];
-      if constexpr (DT == EEP_FP8_E4M3) {
-        const int n = s + 1 < steps ? s + 1 : s;
-#pragma unroll
-        for (int j = 0; j < TT; ++j) sx_next[j] = x_scale[sx[j] + (uint32_t)n];
-        sw_next[0] = w_scale[n];
-        sw_next[1] = w_scale[up + n];
-      }
       if (s + kStages - 1 < steps) fetch(s + kStages - 1, (s + kStages - 1) % kStages);
 
       const uint8_t* stage = lds + (s % kStages) * kStage;
@@ -598,33 +596,49 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
       auto row_of_tile = [&](int f) {
         return GATE ? (f < 4 ? wm * 64 + f * 16 : 128 + wm * 64 + (f - 4) * 16) : wm * 128 + f * 16;
       };
+      [[maybe_unused]] float scale[GATE ? 2 : 1][TT];
+      if constexpr (kCodes) {
+        const float* scales = (const float*)(stage + kScales);
+#pragma unroll
+        for (int j = 0; j < TT; ++j) {
+          const float token = scales[(wn * TT + j) * 16 + col];
+          scale[0][j] = token * scales[kTokens + (GATE ? 0 : wm)];
+          if constexpr (GATE) scale[1][j] = token * scales[kTokens + 1];
+        }
+      }
+      // codes: the block's sums of a tile are multiplied by the scales and added while the next ones are multiplied
+      constexpr int kBehind = 3;
+      [[maybe_unused]] f32x4 block[kBehind + 1];
+      auto add_block = [&](int i) {
+        if constexpr (kCodes) {
+          const int f = i / TT, j = i % TT;
+#pragma unroll
+          for (int n = 0; n < 4; ++n)
+            acc[f][j][n] = fmaf(block[i % (kBehind + 1)][n], scale[GATE ? f / 4 : 0][j], acc[f][j][n]);
+        }
+      };
       Frag ahead = read(row_of_tile(0));
 #pragma unroll
       for (int f = 0; f < 8; ++f) {
         Operand<DT, WIDE> av;
         av.set(ahead);
         if (f < 7) ahead = read(row_of_tile(f + 1));
-        if constexpr (DT == EEP_FP8_E4M3) {
-          f32x4 p[TT];
 #pragma unroll
-          for (int j = 0; j < TT; ++j) p[j] = av.times(b[j], f32x4{0, 0, 0, 0});
-#pragma unroll
-          for (int j = 0; j < TT; ++j) {
-            const float scale = sx_now[j] * sw_now[GATE ? f / 4 : 0];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[f][j][i] = fmaf(p[j][i], scale, acc[f][j][i]);
+        for (int j = 0; j < TT; ++j) {
+          if constexpr (kCodes) {
+            const int i = f * TT + j;
+            block[i % (kBehind + 1)] = av.times(b[j], f32x4{0, 0, 0, 0});
+            if (i >= kBehind) add_block(i - kBehind);
+            __builtin_amdgcn_sched_barrier(0);
+          } else {
+            acc[f][j] = av.times(b[j], acc[f][j]);
           }
-        } else {
-#pragma unroll
-          for (int j = 0; j < TT; ++j) acc[f][j] = av.times(b[j], acc[f][j]);
         }
-        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (!kCodes) __builtin_amdgcn_sched_barrier(0);
       }
-      if constexpr (DT == EEP_FP8_E4M3) {
+      if constexpr (kCodes) {
 #pragma unroll
-        for (int j = 0; j < TT; ++j) sx_now[j] = sx_next[j];
-        sw_now[0] = sw_next[0];
-        sw_now[1] = sw_next[1];
+        for (int i = 8 * TT - kBehind; i < 8 * TT; ++i) add_block(i);
       }
     };
     for (int s = 0; s < full_steps; ++s) step(s, std::false_type());
@@ -729,7 +743,7 @@ hipError_t launch_thin(ProductArgs a, hipStream_t st) {
 template <int DT, int YT, bool GATE, int TT>
 hipError_t launch_tiled(ProductArgs a, int cus, hipStream_t st) {
   constexpr bool kWide = DT == EEP_FP8_E4M3 && YT == EEP_F32;
-  constexpr int kLds = tiled_stages(TT) * tiled_stage_bytes(TT) + 2 * 64 * TT * (int)sizeof(uint32_t);
+  constexpr int kLds = tiled_stages(TT) * tiled_stage_bytes(DT == EEP_FP8_E4M3, TT) + 2 * 64 * TT * (int)sizeof(uint32_t);
   const auto kernel = k_product_tiled<DT, kWide, YT, GATE, TT>;
   static const hipError_t allowed =
       hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
