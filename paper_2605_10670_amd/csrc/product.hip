@@ -360,9 +360,13 @@ __global__ __launch_bounds__(64 * kThinWaves) void k_product_thin(ProductArgs a,
 constexpr int kTiledWaves = 8, kTiledRows = 256;
 constexpr int kTiledThreads = 64 * kTiledWaves;
 __host__ __device__ constexpr int tiled_stages(int tt) { return tt == 4 ? 2 : 3; }
-// A stage: the weight rows of a step, the tokens' rows, and for codes the tokens' scales and two of the weights'.
-__host__ __device__ constexpr int tiled_stage_bytes(bool codes, int tt) {
-  return (kTiledRows + 64 * tt) * kStepBytes + (codes ? 64 * tt * 4 + 128 : 0);
+// A stage: the weight rows and the tokens' rows of a step.  Codes' scales come four steps at a time: a token's side by side, behind
+// them those of two blocks of weight rows.
+constexpr int kScaleSteps = 4, kScaleBuffers = 3;
+__host__ __device__ constexpr int tiled_stage_bytes(int tt) { return (kTiledRows + 64 * tt) * kStepBytes; }
+__host__ __device__ constexpr int tiled_scale_bytes(int tt) { return 64 * tt * kScaleSteps * 4 + 256; }
+__host__ __device__ constexpr int tiled_lds_bytes(bool codes, int tt) {
+  return tiled_stages(tt) * tiled_stage_bytes(tt) + (codes ? kScaleBuffers * tiled_scale_bytes(tt) : 0) + 2 * 64 * tt * 4;
 }
 
 typedef __attribute__((address_space(3))) void lds_void;
@@ -455,13 +459,13 @@ template <int DT, bool WIDE, int YT, bool GATE, int TT>
 __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs a) {
   constexpr int kStages = tiled_stages(TT), kTokens = 64 * TT;
   constexpr bool kCodes = DT == EEP_FP8_E4M3;
-  constexpr int kStage = tiled_stage_bytes(kCodes, TT);
+  constexpr int kStage = tiled_stage_bytes(TT), kScaleBytes = tiled_scale_bytes(TT);
   constexpr int kLoads = (kTiledRows + kTokens) / 8 / kTiledWaves;  // of 8 rows each, a wavefront and step
-  constexpr int kScales = (kTiledRows + kTokens) * kStepBytes;      // where a stage has them: tokens', weights'
-  constexpr int kScaleLanes = kTokens / kTiledWaves;                 // tokens whose scales a wavefront loads
   constexpr int kWeightLoads = kTiledRows / 8 / kTiledWaves;
+  constexpr int kScaleLoads = 4 * TT >= kTiledWaves ? 4 * TT / kTiledWaves : 1;  // of 16 tokens each, a wavefront
   extern __shared__ __align__(1024) uint8_t lds[];
-  uint32_t* s_top = (uint32_t*)(lds + kStages * kStage);  // [2][kTokens]
+  uint8_t* const scale_lds = lds + kStages * kStage;
+  uint32_t* s_top = (uint32_t*)(scale_lds + (kCodes ? kScaleBuffers * kScaleBytes : 0));  // [2][kTokens]
 
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -493,8 +497,8 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
   Tile t = {}, next = {};
   const uint8_t *w_base, *x_base;      // of the tile whose rows are loaded
   uint32_t row_at[kLoads];             // first byte of the lane's rows from there
-  const float* scale_base = nullptr;   // and the scale that it loads, if any, of a step
-  const bool loads_scale = kCodes && lane < kScaleLanes + (wave == kTiledWaves - 1 ? 2 : 0);
+  const float *x_scale = nullptr, *w_scale = nullptr;
+  uint32_t scale_at[kScaleLoads];      // and of its tokens' scales
   auto aim = [&](const Tile& tile) {
     const int half = GATE ? 128 : 256;  // weight rows in one piece
     const int n0 = tile.feature_tile * half;
@@ -515,23 +519,32 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
       row_at[i] = (uint32_t)r * (uint32_t)a.row_bytes;
     }
     if constexpr (kCodes) {
-      // a token's; behind the last wavefront's those of the two blocks of 128 weight rows
-      if (lane < kScaleLanes) {
-        int r = wave * kScaleLanes + lane;
+      x_scale = a.x_scale + (int64_t)tile.first * steps;
+#pragma unroll
+      for (int i = 0; i < kScaleLoads; ++i) {
+        int r = (wave * kScaleLoads + i) % (4 * TT) * 16 + (lane >> 2);
         r = tile.first + r < tile.end ? r : tile.end - 1 - tile.first;
-        scale_base = a.x_scale + (tile.first + (int64_t)(r > 0 ? r : 0)) * steps;
-      } else {
-        const int second = lane == kScaleLanes ? 0 : 1;
-        int block = GATE ? tile.feature_tile + second * (a.features / kScaleBlock) : 2 * tile.feature_tile + second;
-        const int last = (weight_rows - 1) / kScaleBlock;
-        block = block < last ? block : last;
-        scale_base = (const float*)((const uint8_t*)a.w_scale + tile.slot * a.scale_stride) + (int64_t)block * steps;
+        scale_at[i] = (uint32_t)(r > 0 ? r : 0) * (uint32_t)steps;
       }
+      // blocks of 128 weight rows: one of each factor with the gate, else the two of the tile, if it has two
+      const int block = GATE ? tile.feature_tile : 2 * tile.feature_tile;
+      w_scale = (const float*)((const uint8_t*)a.w_scale + tile.slot * a.scale_stride) + (int64_t)block * steps;
     }
   };
-  auto fetch = [&](int step, int stage) {
+  const int last_block = (weight_rows - 1) / kScaleBlock;
+  auto fetch_scales = [&](const Tile& tile, int chunk, uint8_t* to_lds) {
+    int q = chunk * kScaleSteps + (lane & 3);
+    q = q < steps ? q : steps - 1;
+#pragma unroll
+    for (int i = 0; i < kScaleLoads; ++i)
+      __builtin_amdgcn_global_load_lds((global_void*)(x_scale + (scale_at[i] + (uint32_t)q)),
+                                       (lds_void*)(to_lds + (wave * kScaleLoads + i) % (4 * TT) * 256), 4, 0, 0);
+    const int second = GATE ? a.features / kScaleBlock : 2 * tile.feature_tile < last_block ? 1 : 0;
+    __builtin_amdgcn_global_load_lds((global_void*)(w_scale + (uint32_t)((lane & 4 ? second * steps : 0) + q)),
+                                     (lds_void*)(to_lds + kTokens * 16), 4, 0, 0);
+  };
+  auto fetch = [&](int step, uint8_t* to_lds) {
     const uint32_t at = (uint32_t)(step * kStepBytes + (step < full_steps ? load_chunk : tail_chunk) * 16);
-    uint8_t* to_lds = lds + stage * kStage;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int group = i < kWeightLoads ? wave * kWeightLoads + i
@@ -540,25 +553,72 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
       __builtin_amdgcn_global_load_lds((global_void*)(base + (row_at[i] + at)), (lds_void*)(to_lds + group * 8 * kStepBytes),
                                        16, 0, 0);
     }
-    if constexpr (kCodes) {
-      if (loads_scale)
-        __builtin_amdgcn_global_load_lds((global_void*)(scale_base + step),
-                                         (lds_void*)(to_lds + kScales + wave * kScaleLanes * 4), 4, 0, 0);
-    }
   };
 
   int64_t item = from + seat;
   if (item >= to) return;
   map.find(a, item, &t.slot, &t.feature_tile, &t.first, &t.end);
   aim(t);
+  // The steps of all tiles are one stream, fetched kStages ahead (no row is shorter than that).  Behind its end the last step
+  // is fetched again, to no purpose, so that the number of loads under way is always the same.
+  int64_t fetch_item = item;
+  int fetch_step = 0;
+  uint8_t* chunk = scale_lds;  // where the scales of the step are
+  auto behind = [&](uint8_t* p, int n) {
+    p += n * kScaleBytes;
+    return p < scale_lds + kScaleBuffers * kScaleBytes ? p : p - kScaleBuffers * kScaleBytes;
+  };
+  // At the top of step s: the scales of the next four steps, and the next tile, once the fetches have come to them.
+  auto look_ahead = [&](int s) {
+    if constexpr (kCodes) {
+      if ((s & 3) == 0 && s + kScaleSteps < steps) fetch_scales(t, s / kScaleSteps + 1, behind(chunk, 1));
+    }
+    if (fetch_step < steps) return;
+    if (fetch_item + seats < to) {
+      fetch_item += seats;
+      map.find(a, fetch_item, &next.slot, &next.feature_tile, &next.first, &next.end);
+      aim(next);
+      if constexpr (kCodes) fetch_scales(next, 0, behind(chunk, (steps - 1) / kScaleSteps - s / kScaleSteps + 1));
+      fetch_step = 0;
+    } else {
+      fetch_step = steps - 1;
+    }
+  };
+  if constexpr (kCodes) fetch_scales(t, 0, chunk);
 #pragma unroll
-  for (int s = 0; s < kStages - 1; ++s)
-    if (s < steps) fetch(s, s);
+  for (int s = 0; s < kStages; ++s) fetch(fetch_step++, lds + s * kStage);
+
+  // What a step begins with: the tokens' rows, the first weight rows, the scales; read while the step before ends.
+  Frag b_raw[TT], a_raw;
+  [[maybe_unused]] float token_scale[TT], row_scale[2];
+  uint8_t* stage = lds;  // of the step
+  auto read = [&](const uint8_t* from_lds, int tile_row) {
+    Frag f;
+    f.c[0] = *(const u32x4*)(from_lds + tile_row * kStepBytes + read_at);
+    f.c[1] = *(const u32x4*)(from_lds + tile_row * kStepBytes + (read_at ^ 64));
+    return f;
+  };
+  auto row_of_tile = [&](int f) {
+    return GATE ? (f < 4 ? wm * 64 + f * 16 : 128 + wm * 64 + (f - 4) * 16) : wm * 128 + f * 16;
+  };
+  auto read_scales = [&](int s) {
+    if constexpr (kCodes) {
+      const float* scales = (const float*)chunk + (s & 3);
+#pragma unroll
+      for (int j = 0; j < TT; ++j) token_scale[j] = scales[((wn * TT + j) * 16 + col) * 4];
+      row_scale[0] = scales[kTokens * 4 + (GATE ? 0 : wm * 4)];
+      if constexpr (GATE) row_scale[1] = scales[kTokens * 4 + 4];
+    }
+  };
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kStages - 1) * kLoads) : "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  read_scales(0);
+#pragma unroll
+  for (int j = 0; j < TT; ++j) b_raw[j] = read(stage, kTiledRows + (wn * TT + j) * 16);
+  a_raw = read(stage, row_of_tile(0));
 
   for (;;) {
-    const bool more = item + seats < to;
-    if (more) map.find(a, item + seats, &next.slot, &next.feature_tile, &next.first, &next.end);
-
     f32x4 acc[8][TT];
 #pragma unroll
     for (int f = 0; f < 8; ++f)
@@ -567,92 +627,95 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
 
     auto step = [&](int s, auto is_cut) {
       constexpr bool kCut = decltype(is_cut)::value;  // the last step of rows that end within it
-      // this step's rows are there once no more than the steps behind it are under way; and all wavefronts have read the
-      // stage that is filled next
-      if (kStages > 2 && s + 1 < steps)
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kStages - 2) * (kLoads + (kCodes ? 1 : 0))) : "memory");
-      else
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-      __builtin_amdgcn_s_barrier();
-      asm volatile("" ::: "memory");
-      if (s + kStages - 1 < steps) fetch(s + kStages - 1, (s + kStages - 1) % kStages);
-
-      const uint8_t* stage = lds + (s % kStages) * kStage;
-      auto read = [&](int tile_row) {
-        Frag f;
-        const uint8_t* at = stage + tile_row * kStepBytes + read_at;
-        f.c[0] = *(const u32x4*)at;
-        f.c[1] = *(const u32x4*)(stage + tile_row * kStepBytes + (read_at ^ 64));
+      auto ready = [&](Frag f) {
         if constexpr (kCut) {
 #pragma unroll
           for (int j = 0; j < 2; ++j)
             if (j * 64 + part * 16 >= tail) f.c[j] = u32x4{0, 0, 0, 0};
         }
-        return f;
+        Operand<DT, WIDE> o;
+        o.set(f);
+        return o;
       };
       Operand<DT, WIDE> b[TT];
 #pragma unroll
-      for (int j = 0; j < TT; ++j) b[j].set(read(kTiledRows + (wn * TT + j) * 16));
-      auto row_of_tile = [&](int f) {
-        return GATE ? (f < 4 ? wm * 64 + f * 16 : 128 + wm * 64 + (f - 4) * 16) : wm * 128 + f * 16;
-      };
+      for (int j = 0; j < TT; ++j) b[j] = ready(b_raw[j]);
       [[maybe_unused]] float scale[GATE ? 2 : 1][TT];
       if constexpr (kCodes) {
-        const float* scales = (const float*)(stage + kScales);
 #pragma unroll
         for (int j = 0; j < TT; ++j) {
-          const float token = scales[(wn * TT + j) * 16 + col];
-          scale[0][j] = token * scales[kTokens + (GATE ? 0 : wm)];
-          if constexpr (GATE) scale[1][j] = token * scales[kTokens + 1];
+          scale[0][j] = token_scale[j] * row_scale[0];
+          if constexpr (GATE) scale[1][j] = token_scale[j] * row_scale[1];
         }
       }
       // codes: the block's sums of a tile are multiplied by the scales and added while the next ones are multiplied
-      constexpr int kBehind = 3;
+      constexpr int kBehind = 2;
       [[maybe_unused]] f32x4 block[kBehind + 1];
+      // the i-th tile: 6 times the tokens, then the last two side by side
+      auto tile_f = [](int i) { return i < 6 * TT ? i / TT : 6 + (i & 1); };
+      auto tile_j = [](int i) { return i < 6 * TT ? i % TT : (i - 6 * TT) / 2; };
       auto add_block = [&](int i) {
         if constexpr (kCodes) {
-          const int f = i / TT, j = i % TT;
+          const int f = tile_f(i), j = tile_j(i);
 #pragma unroll
           for (int n = 0; n < 4; ++n)
             acc[f][j][n] = fmaf(block[i % (kBehind + 1)][n], scale[GATE ? f / 4 : 0][j], acc[f][j][n]);
         }
       };
-      Frag ahead = read(row_of_tile(0));
-#pragma unroll
-      for (int f = 0; f < 8; ++f) {
-        Operand<DT, WIDE> av;
-        av.set(ahead);
-        if (f < 7) ahead = read(row_of_tile(f + 1));
-#pragma unroll
-        for (int j = 0; j < TT; ++j) {
-          if constexpr (kCodes) {
-            const int i = f * TT + j;
-            block[i % (kBehind + 1)] = av.times(b[j], f32x4{0, 0, 0, 0});
-            if (i >= kBehind) add_block(i - kBehind);
-            __builtin_amdgcn_sched_barrier(0);
-          } else {
-            acc[f][j] = av.times(b[j], acc[f][j]);
-          }
+      auto multiply = [&](int i, const Operand<DT, WIDE>& av) {
+        const int f = tile_f(i), j = tile_j(i);
+        if constexpr (kCodes) {
+          block[i % (kBehind + 1)] = av.times(b[j], f32x4{0, 0, 0, 0});
+          if (i >= kBehind) add_block(i - kBehind);
+          __builtin_amdgcn_sched_barrier(0);
+        } else {
+          acc[f][j] = av.times(b[j], acc[f][j]);
         }
+      };
+      Operand<DT, WIDE> last[2];
+#pragma unroll
+      for (int f = 0; f < 6; ++f) {
+        const Operand<DT, WIDE> av = ready(a_raw);
+        a_raw = read(stage, row_of_tile(f + 1));
+#pragma unroll
+        for (int j = 0; j < TT; ++j) multiply(f * TT + j, av);
         if constexpr (!kCodes) __builtin_amdgcn_sched_barrier(0);
       }
+      last[0] = ready(a_raw);
+      last[1] = ready(read(stage, row_of_tile(7)));
+      // This wavefront has read all it needs of the stage.  Once all have, and the next step's rows are there (no more than
+      // the fetches behind them are under way), the stage is filled again and the next step's first operands are read.
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kStages - 2) * kLoads) : "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      uint8_t* following = stage + kStage < lds + kStages * kStage ? stage + kStage : lds;
+      fetch(fetch_step++, stage);
+      a_raw = read(following, row_of_tile(0));
+#pragma unroll
+      for (int j = 0; j < TT; ++j) {
+        multiply(6 * TT + 2 * j, last[0]);
+        multiply(6 * TT + 2 * j + 1, last[1]);
+        b_raw[j] = read(following, kTiledRows + (wn * TT + j) * 16);
+        if constexpr (!kCodes) __builtin_amdgcn_sched_barrier(0);
+      }
+      const int upcoming = s + 1 < steps ? s + 1 : 0;
+      if ((upcoming & 3) == 0) chunk = behind(chunk, 1);
+      read_scales(upcoming);
       if constexpr (kCodes) {
 #pragma unroll
         for (int i = 8 * TT - kBehind; i < 8 * TT; ++i) add_block(i);
       }
+      stage = following;
     };
-    for (int s = 0; s < full_steps; ++s) step(s, std::false_type());
-    if constexpr (DT != EEP_FP8_E4M3)
-      if (tail != 0) step(full_steps, std::true_type());
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    // the next tile's first rows are on their way while this one's results are stored
-    if (more) {
-      aim(next);
-#pragma unroll
-      for (int s = 0; s < kStages - 1; ++s)
-        if (s < steps) fetch(s, s);
+    for (int s = 0; s < full_steps; ++s) {
+      look_ahead(s);
+      step(s, std::false_type());
+    }
+    if constexpr (!kCodes) {
+      if (tail != 0) {
+        look_ahead(full_steps);
+        step(full_steps, std::true_type());
+      }
     }
 
     if constexpr (GATE) {
@@ -717,10 +780,11 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
         }
       }
     }
-    if (!more) return;
     item += seats;
+    if (item >= to) break;
     t = next;
   }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // nothing may still write to LDS when the workgroup is gone
 }
 
 // Tiles of `tokens` rows that the slots may have at most.
@@ -743,7 +807,7 @@ hipError_t launch_thin(ProductArgs a, hipStream_t st) {
 template <int DT, int YT, bool GATE, int TT>
 hipError_t launch_tiled(ProductArgs a, int cus, hipStream_t st) {
   constexpr bool kWide = DT == EEP_FP8_E4M3 && YT == EEP_F32;
-  constexpr int kLds = tiled_stages(TT) * tiled_stage_bytes(DT == EEP_FP8_E4M3, TT) + 2 * 64 * TT * (int)sizeof(uint32_t);
+  constexpr int kLds = tiled_lds_bytes(DT == EEP_FP8_E4M3, TT);
   const auto kernel = k_product_tiled<DT, kWide, YT, GATE, TT>;
   static const hipError_t allowed =
       hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
@@ -758,8 +822,10 @@ hipError_t launch_tiled(ProductArgs a, int cus, hipStream_t st) {
 template <int DT, int YT, bool GATE>
 hipError_t launch_product(const ProductArgs& a, int cus, hipStream_t st) {
   const int mean = (a.rows + a.slots - 1) / a.slots;  // rows a slot
-  if (mean <= 16) return launch_thin<DT, YT, GATE>(a, st);
+  if (mean <= 16 || a.row_bytes <= 2 * kStepBytes) return launch_thin<DT, YT, GATE>(a, st);
   if (mean <= 64) return launch_tiled<DT, YT, GATE, 1>(a, cus, st);
+  // (widened codes take twice the registers)
+  if constexpr (DT == EEP_FP8_E4M3 && YT == EEP_F32) return launch_tiled<DT, YT, GATE, 2>(a, cus, st);
   if (mean <= 160) return launch_tiled<DT, YT, GATE, 2>(a, cus, st);
   return launch_tiled<DT, YT, GATE, 4>(a, cus, st);
 }
