@@ -360,13 +360,13 @@ __global__ __launch_bounds__(64 * kThinWaves) void k_product_thin(ProductArgs a,
 constexpr int kTiledWaves = 8, kTiledRows = 256;
 constexpr int kTiledThreads = 64 * kTiledWaves;
 __host__ __device__ constexpr int tiled_stages(int tt) { return tt == 4 ? 2 : 3; }
-// A stage: the weight rows and the tokens' rows of a step.  Codes' scales come four steps at a time: a token's side by side, behind
-// them those of two blocks of weight rows.
+// Codes' scales come four steps at a time: a token's side by side, behind them those of two blocks of weight rows.
 constexpr int kScaleSteps = 4, kScaleBuffers = 3;
-__host__ __device__ constexpr int tiled_stage_bytes(int tt) { return (kTiledRows + 64 * tt) * kStepBytes; }
+constexpr int kWeightStage = kTiledRows * kStepBytes;
 __host__ __device__ constexpr int tiled_scale_bytes(int tt) { return 64 * tt * kScaleSteps * 4 + 256; }
 __host__ __device__ constexpr int tiled_lds_bytes(bool codes, int tt) {
-  return tiled_stages(tt) * tiled_stage_bytes(tt) + (codes ? kScaleBuffers * tiled_scale_bytes(tt) : 0) + 2 * 64 * tt * 4;
+  return tiled_stages(tt) * (kWeightStage + 64 * tt * kStepBytes) +
+         (codes ? kScaleBuffers * tiled_scale_bytes(tt) : 0) + 2 * 64 * tt * 4;
 }
 
 typedef __attribute__((address_space(3))) void lds_void;
@@ -459,12 +459,13 @@ template <int DT, bool WIDE, int YT, bool GATE, int TT>
 __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs a) {
   constexpr int kStages = tiled_stages(TT), kTokens = 64 * TT;
   constexpr bool kCodes = DT == EEP_FP8_E4M3;
-  constexpr int kStage = tiled_stage_bytes(TT), kScaleBytes = tiled_scale_bytes(TT);
-  constexpr int kLoads = (kTiledRows + kTokens) / 8 / kTiledWaves;  // of 8 rows each, a wavefront and step
-  constexpr int kWeightLoads = kTiledRows / 8 / kTiledWaves;
+  constexpr int kXStage = kTokens * kStepBytes, kScaleBytes = tiled_scale_bytes(TT);
+  constexpr int kWeightLoads = kTiledRows / 8 / kTiledWaves, kXLoads = kTokens / 8 / kTiledWaves;  // of 8 rows each, a wavefront and step
+  constexpr bool kEarly = TT == 4;  // the tokens' rows are fetched as soon as all wavefronts have read theirs
   constexpr int kScaleLoads = 4 * TT >= kTiledWaves ? 4 * TT / kTiledWaves : 1;  // of 16 tokens each, a wavefront
   extern __shared__ __align__(1024) uint8_t lds[];
-  uint8_t* const scale_lds = lds + kStages * kStage;
+  uint8_t* const x_lds = lds + kStages * kWeightStage;
+  uint8_t* const scale_lds = x_lds + kStages * kXStage;
   uint32_t* s_top = (uint32_t*)(scale_lds + (kCodes ? kScaleBuffers * kScaleBytes : 0));  // [2][kTokens]
 
   const int lane = threadIdx.x & 63;
@@ -495,28 +496,19 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
     int slot, feature_tile, first, end;
   };
   Tile t = {}, next = {};
-  const uint8_t *w_base, *x_base;      // of the tile whose rows are loaded
-  uint32_t row_at[kLoads];             // first byte of the lane's rows from there
+  const uint8_t *w_base, *x_base;                   // of the tiles whose rows are loaded
+  uint32_t w_row_at[kWeightLoads], x_row_at[kXLoads];  // first byte of the lane's rows from there
   const float *x_scale = nullptr, *w_scale = nullptr;
-  uint32_t scale_at[kScaleLoads];      // and of its tokens' scales
-  auto aim = [&](const Tile& tile) {
+  uint32_t scale_at[kScaleLoads];                   // and of its tokens' scales
+  auto aim_weights = [&](const Tile& tile) {
     const int half = GATE ? 128 : 256;  // weight rows in one piece
     const int n0 = tile.feature_tile * half;
     const int piece = GATE && wave >= kTiledWaves / 2 ? 1 : 0;
     w_base = a.w + tile.slot * a.slot_stride + (int64_t)(n0 + piece * a.features) * a.row_bytes;
-    x_base = a.x + (int64_t)tile.first * a.row_bytes;
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      int r;
-      if (i < kWeightLoads) {
-        r = (wave * kWeightLoads + i) * 8 + load_row - piece * half;
-        r = n0 + r < a.features ? r : a.features - 1 - n0;
-      } else {
-        r = (wave * (kLoads - kWeightLoads) + i - kWeightLoads) * 8 + load_row;
-        r = tile.first + r < tile.end ? r : tile.end - 1 - tile.first;
-        r = r > 0 ? r : 0;
-      }
-      row_at[i] = (uint32_t)r * (uint32_t)a.row_bytes;
+    for (int i = 0; i < kWeightLoads; ++i) {
+      const int r = (wave * kWeightLoads + i) * 8 + load_row - piece * half;
+      w_row_at[i] = (uint32_t)(n0 + r < a.features ? r : a.features - 1 - n0) * (uint32_t)a.row_bytes;
     }
     if constexpr (kCodes) {
       x_scale = a.x_scale + (int64_t)tile.first * steps;
@@ -531,6 +523,15 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
       w_scale = (const float*)((const uint8_t*)a.w_scale + tile.slot * a.scale_stride) + (int64_t)block * steps;
     }
   };
+  auto aim_tokens = [&](const Tile& tile) {
+    x_base = a.x + (int64_t)tile.first * a.row_bytes;
+#pragma unroll
+    for (int i = 0; i < kXLoads; ++i) {
+      int r = (wave * kXLoads + i) * 8 + load_row;
+      r = tile.first + r < tile.end ? r : tile.end - 1 - tile.first;
+      x_row_at[i] = (uint32_t)(r > 0 ? r : 0) * (uint32_t)a.row_bytes;
+    }
+  };
   const int last_block = (weight_rows - 1) / kScaleBlock;
   auto fetch_scales = [&](const Tile& tile, int chunk, uint8_t* to_lds) {
     int q = chunk * kScaleSteps + (lane & 3);
@@ -543,26 +544,34 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
     __builtin_amdgcn_global_load_lds((global_void*)(w_scale + (uint32_t)((lane & 4 ? second * steps : 0) + q)),
                                      (lds_void*)(to_lds + kTokens * 16), 4, 0, 0);
   };
-  auto fetch = [&](int step, uint8_t* to_lds) {
-    const uint32_t at = (uint32_t)(step * kStepBytes + (step < full_steps ? load_chunk : tail_chunk) * 16);
+  auto bytes_in = [&](int step) {
+    return (uint32_t)(step * kStepBytes + (step < full_steps ? load_chunk : tail_chunk) * 16);
+  };
+  auto fetch_weights = [&](int step, uint8_t* to_lds) {
+    const uint32_t at = bytes_in(step);
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int group = i < kWeightLoads ? wave * kWeightLoads + i
-                                         : kTiledRows / 8 + wave * (kLoads - kWeightLoads) + i - kWeightLoads;
-      const uint8_t* base = i < kWeightLoads ? w_base : x_base;
-      __builtin_amdgcn_global_load_lds((global_void*)(base + (row_at[i] + at)), (lds_void*)(to_lds + group * 8 * kStepBytes),
-                                       16, 0, 0);
-    }
+    for (int i = 0; i < kWeightLoads; ++i)
+      __builtin_amdgcn_global_load_lds((global_void*)(w_base + (w_row_at[i] + at)),
+                                       (lds_void*)(to_lds + (wave * kWeightLoads + i) * 8 * kStepBytes), 16, 0, 0);
+  };
+  auto fetch_tokens = [&](int step, uint8_t* to_lds) {
+    const uint32_t at = bytes_in(step);
+#pragma unroll
+    for (int i = 0; i < kXLoads; ++i)
+      __builtin_amdgcn_global_load_lds((global_void*)(x_base + (x_row_at[i] + at)),
+                                       (lds_void*)(to_lds + (wave * kXLoads + i) * 8 * kStepBytes), 16, 0, 0);
   };
 
   int64_t item = from + seat;
   if (item >= to) return;
   map.find(a, item, &t.slot, &t.feature_tile, &t.first, &t.end);
-  aim(t);
-  // The steps of all tiles are one stream, fetched kStages ahead (no row is shorter than that).  Behind its end the last step
+  aim_weights(t);
+  aim_tokens(t);
+  // The steps of all tiles are one stream, fetched ahead (no row is shorter than that).  Behind its end the last step
   // is fetched again, to no purpose, so that the number of loads under way is always the same.
   int64_t fetch_item = item;
-  int fetch_step = 0;
+  int w_step = 0, x_step = 0;  // to be fetched next
+  bool more = true;
   uint8_t* chunk = scale_lds;  // where the scales of the step are
   auto behind = [&](uint8_t* p, int n) {
     p += n * kScaleBytes;
@@ -573,25 +582,32 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
     if constexpr (kCodes) {
       if ((s & 3) == 0 && s + kScaleSteps < steps) fetch_scales(t, s / kScaleSteps + 1, behind(chunk, 1));
     }
-    if (fetch_step < steps) return;
-    if (fetch_item + seats < to) {
-      fetch_item += seats;
-      map.find(a, fetch_item, &next.slot, &next.feature_tile, &next.first, &next.end);
-      aim(next);
-      if constexpr (kCodes) fetch_scales(next, 0, behind(chunk, (steps - 1) / kScaleSteps - s / kScaleSteps + 1));
-      fetch_step = 0;
-    } else {
-      fetch_step = steps - 1;
+    if (w_step == steps) {
+      more = fetch_item + seats < to;
+      if (more) {
+        fetch_item += seats;
+        map.find(a, fetch_item, &next.slot, &next.feature_tile, &next.first, &next.end);
+        aim_weights(next);
+        if constexpr (kCodes) fetch_scales(next, 0, behind(chunk, (steps - 1) / kScaleSteps - s / kScaleSteps + 1));
+      }
+      w_step = more ? 0 : steps - 1;
+    }
+    if (x_step == steps) {
+      if (more) aim_tokens(next);
+      x_step = more ? 0 : steps - 1;
     }
   };
   if constexpr (kCodes) fetch_scales(t, 0, chunk);
 #pragma unroll
-  for (int s = 0; s < kStages; ++s) fetch(fetch_step++, lds + s * kStage);
+  for (int s = 0; s < kStages; ++s) {
+    fetch_tokens(x_step++, x_lds + s * kXStage);
+    fetch_weights(w_step++, lds + s * kWeightStage);
+  }
 
   // What a step begins with: the tokens' rows, the first weight rows, the scales; read while the step before ends.
   Frag b_raw[TT], a_raw;
   [[maybe_unused]] float token_scale[TT], row_scale[2];
-  uint8_t* stage = lds;  // of the step
+  uint8_t *stage = lds, *x_stage = x_lds;  // of the step
   auto read = [&](const uint8_t* from_lds, int tile_row) {
     Frag f;
     f.c[0] = *(const u32x4*)(from_lds + tile_row * kStepBytes + read_at);
@@ -610,12 +626,12 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
       if constexpr (GATE) row_scale[1] = scales[kTokens * 4 + 4];
     }
   };
-  asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kStages - 1) * kLoads) : "memory");
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kStages - 1) * (kWeightLoads + kXLoads)) : "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
   read_scales(0);
 #pragma unroll
-  for (int j = 0; j < TT; ++j) b_raw[j] = read(stage, kTiledRows + (wn * TT + j) * 16);
+  for (int j = 0; j < TT; ++j) b_raw[j] = read(x_stage, (wn * TT + j) * 16);
   a_raw = read(stage, row_of_tile(0));
 
   for (;;) {
@@ -680,22 +696,32 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
 #pragma unroll
         for (int j = 0; j < TT; ++j) multiply(f * TT + j, av);
         if constexpr (!kCodes) __builtin_amdgcn_sched_barrier(0);
+        if (kEarly && f == 2) {
+          // All wavefronts have their tokens' rows in registers (only the two reads of the next weight rows may be under
+          // way): the stage of these is filled again.
+          asm volatile("s_waitcnt lgkmcnt(2)" ::: "memory");
+          __builtin_amdgcn_s_barrier();
+          asm volatile("" ::: "memory");
+          fetch_tokens(x_step++, x_stage);
+        }
       }
       last[0] = ready(a_raw);
       last[1] = ready(read(stage, row_of_tile(7)));
       // This wavefront has read all it needs of the stage.  Once all have, and the next step's rows are there (no more than
-      // the fetches behind them are under way), the stage is filled again and the next step's first operands are read.
-      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kStages - 2) * kLoads) : "memory");
+      // the fetches behind them are under way), the stage may be filled again and the next step's first operands are read.
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kEarly ? kXLoads : (kStages - 2) * (kWeightLoads + kXLoads)) : "memory");
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
-      uint8_t* following = stage + kStage < lds + kStages * kStage ? stage + kStage : lds;
-      fetch(fetch_step++, stage);
+      if (!kEarly) fetch_tokens(x_step++, x_stage);
+      fetch_weights(w_step++, stage);
+      uint8_t* following = stage + kWeightStage < lds + kStages * kWeightStage ? stage + kWeightStage : lds;
+      uint8_t* x_following = x_stage + kXStage < x_lds + kStages * kXStage ? x_stage + kXStage : x_lds;
       a_raw = read(following, row_of_tile(0));
 #pragma unroll
       for (int j = 0; j < TT; ++j) {
         multiply(6 * TT + 2 * j, last[0]);
         multiply(6 * TT + 2 * j + 1, last[1]);
-        b_raw[j] = read(following, kTiledRows + (wn * TT + j) * 16);
+        b_raw[j] = read(x_following, (wn * TT + j) * 16);
         if constexpr (!kCodes) __builtin_amdgcn_sched_barrier(0);
       }
       const int upcoming = s + 1 < steps ? s + 1 : 0;
@@ -706,6 +732,7 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
         for (int i = 8 * TT - kBehind; i < 8 * TT; ++i) add_block(i);
       }
       stage = following;
+      x_stage = x_following;
     };
     for (int s = 0; s < full_steps; ++s) {
       look_ahead(s);
@@ -825,9 +852,9 @@ hipError_t launch_product(const ProductArgs& a, int cus, hipStream_t st) {
   if (mean <= 16 || a.row_bytes <= 2 * kStepBytes) return launch_thin<DT, YT, GATE>(a, st);
   if (mean <= 64) return launch_tiled<DT, YT, GATE, 1>(a, cus, st);
   // (widened codes take twice the registers)
-  if constexpr (DT == EEP_FP8_E4M3 && YT == EEP_F32) return launch_tiled<DT, YT, GATE, 2>(a, cus, st);
-  if (mean <= 160) return launch_tiled<DT, YT, GATE, 2>(a, cus, st);
-  return launch_tiled<DT, YT, GATE, 4>(a, cus, st);
+  if constexpr (DT != EEP_FP8_E4M3 || YT != EEP_F32)
+    if (mean > 160) return launch_tiled<DT, YT, GATE, 4>(a, cus, st);
+  return launch_tiled<DT, YT, GATE, 2>(a, cus, st);
 }
 
 template <int DT>
