@@ -17,6 +17,8 @@ struct eep_product {
   eep_product_config cfg;
   int64_t slot_stride, scale_stride;  // bytes
   int cus;                            // of the device
+  float* partial;                     // sums of a part of in_features, kSplitWork workgroups' of k_product_thin
+  uint32_t* arrived;                  // how many workgroups of a tile have theirs; zero between calls
 };
 
 namespace eep {
@@ -205,16 +207,25 @@ __device__ __forceinline__ void store4(uint8_t* y, int64_t element, const float 
 // A workgroup of 8 wavefronts has 16 rows of one slot and 128 features of y with the gate, 256 without: each wavefront two
 // matrix-core tiles of 16 weight rows, with the gate the two factors of 16 features.  No weight is used by two
 // wavefronts, so nothing of them goes through LDS; the rows of x come from the caches.
+//
+// Where that makes fewer workgroups than the card holds, in_features are divided between `splits` workgroups (SPLIT): each
+// leaves its sums in memory, past the L2s, which do not see one another's writes; the last to arrive adds them up, in the order of
+// the parts whoever that is, and goes on as if they were its own.
 // ---------------------------------------------------------------------------
 constexpr int kThinTokens = 16, kThinWaves = 8;
+constexpr int kSplitWork = 512;                                // workgroups of a divided product at most
+constexpr int kSplitFloats = kThinTokens * 32 * kThinWaves;    // sums of one
 
-template <int DT, int YT, bool GATE>
-__global__ __launch_bounds__(64 * kThinWaves) void k_product_thin(ProductArgs a, int64_t first_tile) {
+template <int DT, int YT, bool GATE, bool SPLIT>
+__global__ __launch_bounds__(64 * kThinWaves) void k_product_thin(ProductArgs a, int64_t first_tile, int splits,
+                                                                  float* partial, uint32_t* arrived) {
   constexpr int U = 2;  // steps of loads in flight ahead of the ones that are multiplied
   __shared__ uint32_t s_top[kThinWaves][16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int col = lane & 15, part = lane >> 4;
-  const int64_t work = first_tile + blockIdx.x;
+  [[maybe_unused]] __shared__ uint32_t s_arrived;
+  const int64_t work = SPLIT ? blockIdx.x / splits : first_tile + blockIdx.x;
+  const int split = SPLIT ? blockIdx.x - (int)work * splits : 0;
   const int64_t row_tile = work / a.feature_tiles;
   const int feature_tile = (int)(work - row_tile * a.feature_tiles);
   int slot, row0, end;
@@ -239,17 +250,20 @@ __global__ __launch_bounds__(64 * kThinWaves) void k_product_thin(ProductArgs a,
   }
   const int token = row0 + col < end ? row0 + col : end - 1;
   from[2] = a.x + (int64_t)token * a.row_bytes + part * 16;
-  const int steps = a.row_bytes / kStepBytes;
-  const int tail = a.row_bytes - steps * kStepBytes;  // bytes, a multiple of 16; 0 for fp8
+  const int row_steps = a.row_bytes / kStepBytes;
+  const int begin = SPLIT ? row_steps * split / splits : 0;
+  const int steps = SPLIT ? row_steps * (split + 1) / splits : row_steps;  // (the one behind the last)
+  // bytes, a multiple of 16; 0 for fp8
+  const int tail = !SPLIT || split == splits - 1 ? a.row_bytes - row_steps * kStepBytes : 0;
   const float* sx = nullptr;
   const float* sw[2] = {nullptr, nullptr};
   if constexpr (DT == EEP_FP8_E4M3) {
-    sx = a.x_scale + (int64_t)token * steps;
+    sx = a.x_scale + (int64_t)token * row_steps;
     const float* slot_scale = (const float*)((const uint8_t*)a.w_scale + slot * a.scale_stride);
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
       const int n = n0[m] < weight_rows ? n0[m] : weight_rows - 1;
-      sw[m] = slot_scale + (int64_t)(n / kScaleBlock) * steps;
+      sw[m] = slot_scale + (int64_t)(n / kScaleBlock) * row_steps;
     }
   }
 
@@ -289,14 +303,12 @@ __global__ __launch_bounds__(64 * kThinWaves) void k_product_thin(ProductArgs a,
       }
     }
   };
-  if (steps > 0) {
-    load(0, 0);
-    for (int s = 0; s < steps; s += 2 * U) {
-      load(1, s + U);
-      multiply(0, s);
-      load(0, s + 2 * U);
-      multiply(1, s + U);
-    }
+  if (begin < steps) load(0, begin);
+  for (int s = begin; s < steps; s += 2 * U) {
+    if (s + U < steps) load(1, s + U);
+    multiply(0, s);
+    if (s + 2 * U < steps) load(0, s + 2 * U);
+    multiply(1, s + U);
   }
   if (tail != 0) {
     Frag t[3];
@@ -311,8 +323,40 @@ __global__ __launch_bounds__(64 * kThinWaves) void k_product_thin(ProductArgs a,
     for (int m = 0; m < 2; ++m) acc[m] = mma<DT>(t[m], t[2], acc[m]);
   }
 
-  const int64_t out_row = (int64_t)(row0 + col) * a.features;
   const bool in_rows = row0 + col < end;
+  if constexpr (SPLIT) {
+    float* own = partial + (work * splits + split) * kSplitFloats;
+    const int at = ((wave * 2 * 16 + col) * 4 + part) * 4;
+    if (in_rows) {
+#pragma unroll
+      for (int m = 0; m < 2; ++m) store_row((u32x4*)(own + at + m * 256), __builtin_bit_cast(u32x4, acc[m]));
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the stores are where all workgroups see them
+    __syncthreads();
+    if (threadIdx.x == 0) s_arrived = __hip_atomic_fetch_add(&arrived[work], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    if (s_arrived != (uint32_t)splits - 1) return;
+    if (threadIdx.x == 0) __hip_atomic_store(&arrived[work], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    acc[0] = acc[1] = f32x4{0, 0, 0, 0};
+    if (in_rows) {
+      const float* all = partial + work * splits * kSplitFloats + at;
+#pragma unroll 4
+      for (int p = 0; p < splits; ++p) {
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+          const uint64_t* v = (const uint64_t*)(all + (int64_t)p * kSplitFloats + m * 256);
+          const uint64_t lo = __hip_atomic_load(v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          const uint64_t hi = __hip_atomic_load(v + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          acc[m][0] += __uint_as_float((uint32_t)lo);
+          acc[m][1] += __uint_as_float((uint32_t)(lo >> 32));
+          acc[m][2] += __uint_as_float((uint32_t)hi);
+          acc[m][3] += __uint_as_float((uint32_t)(hi >> 32));
+        }
+      }
+    }
+  }
+
+  const int64_t out_row = (int64_t)(row0 + col) * a.features;
   if constexpr (GATE) {
     const int n = n0[0] + part * 4;
     float v[4];
@@ -821,12 +865,22 @@ int64_t most_tiles(int rows, int slots, int tokens) {
 }
 
 template <int DT, int YT, bool GATE>
-hipError_t launch_thin(ProductArgs a, hipStream_t st) {
+hipError_t launch_thin(const eep_product& p, ProductArgs a, hipStream_t st) {
+  constexpr int kThreads = 64 * kThinWaves, kMinSteps = 4;  // steps of a part: those that are in flight at a time
   const int features = GATE ? 16 * kThinWaves : 32 * kThinWaves;
   a.feature_tiles = (a.features + features - 1) / features;
   const int64_t work = most_tiles(a.rows, a.slots, kThinTokens) * a.feature_tiles;
-  return in_launches(work, max_blocks(64 * kThinWaves), [&](int64_t first, int64_t n) {
-    hipLaunchKernelGGL((k_product_thin<DT, YT, GATE>), dim3((unsigned)n), dim3(64 * kThinWaves), 0, st, a, first);
+  const int steps = a.row_bytes / kStepBytes;
+  int64_t splits = kSplitWork / work;
+  if (splits > steps / kMinSteps) splits = steps / kMinSteps;
+  if (splits > 1) {
+    hipLaunchKernelGGL((k_product_thin<DT, YT, GATE, true>), dim3((unsigned)(work * splits)), dim3(kThreads), 0, st, a,
+                       (int64_t)0, (int)splits, p.partial, p.arrived);
+    return hipGetLastError();
+  }
+  return in_launches(work, max_blocks(kThreads), [&](int64_t first, int64_t n) {
+    hipLaunchKernelGGL((k_product_thin<DT, YT, GATE, false>), dim3((unsigned)n), dim3(kThreads), 0, st, a, first, 1, nullptr,
+                       nullptr);
     return hipGetLastError();
   });
 }
@@ -847,25 +901,25 @@ hipError_t launch_tiled(ProductArgs a, int cus, hipStream_t st) {
 }
 
 template <int DT, int YT, bool GATE>
-hipError_t launch_product(const ProductArgs& a, int cus, hipStream_t st) {
+hipError_t launch_product(const eep_product& p, const ProductArgs& a, hipStream_t st) {
   const int mean = (a.rows + a.slots - 1) / a.slots;  // rows a slot
-  if (mean <= 16 || a.row_bytes <= 2 * kStepBytes) return launch_thin<DT, YT, GATE>(a, st);
-  if (mean <= 64) return launch_tiled<DT, YT, GATE, 1>(a, cus, st);
+  if (mean <= 16 || a.row_bytes <= 2 * kStepBytes) return launch_thin<DT, YT, GATE>(p, a, st);
+  if (mean <= 64) return launch_tiled<DT, YT, GATE, 1>(a, p.cus, st);
   // (widened codes take twice the registers)
   if constexpr (DT != EEP_FP8_E4M3 || YT != EEP_F32)
-    if (mean > 160) return launch_tiled<DT, YT, GATE, 4>(a, cus, st);
-  return launch_tiled<DT, YT, GATE, 2>(a, cus, st);
+    if (mean > 160) return launch_tiled<DT, YT, GATE, 4>(a, p.cus, st);
+  return launch_tiled<DT, YT, GATE, 2>(a, p.cus, st);
 }
 
 template <int DT>
-hipError_t launch_product(const ProductArgs& a, int y_dtype, bool gate, int cus, hipStream_t st) {
+hipError_t launch_product(const eep_product& p, const ProductArgs& a, int y_dtype, bool gate, hipStream_t st) {
   if (gate) {
-    if (y_dtype == EEP_FP8_E4M3) return launch_product<DT, EEP_FP8_E4M3, true>(a, cus, st);
-    if (y_dtype == EEP_BF16) return launch_product<DT, EEP_BF16, true>(a, cus, st);
-    return launch_product<DT, EEP_F32, true>(a, cus, st);
+    if (y_dtype == EEP_FP8_E4M3) return launch_product<DT, EEP_FP8_E4M3, true>(p, a, st);
+    if (y_dtype == EEP_BF16) return launch_product<DT, EEP_BF16, true>(p, a, st);
+    return launch_product<DT, EEP_F32, true>(p, a, st);
   }
-  if (y_dtype == EEP_BF16) return launch_product<DT, EEP_BF16, false>(a, cus, st);
-  return launch_product<DT, EEP_F32, false>(a, cus, st);
+  if (y_dtype == EEP_BF16) return launch_product<DT, EEP_BF16, false>(p, a, st);
+  return launch_product<DT, EEP_F32, false>(p, a, st);
 }
 
 }  // namespace eep
@@ -910,6 +964,21 @@ int eep_product_create(const eep_product_config* cfg, eep_product** out) {
     delete p;
     return EEP_ERR_HIP;
   }
+  const int64_t partial_bytes = (int64_t)kSplitWork * kSplitFloats * sizeof(float);
+  void* workspace = nullptr;
+  hipError_t e = hipMalloc(&workspace, partial_bytes + kSplitWork * sizeof(uint32_t));
+  if (e == hipSuccess) {
+    p->partial = (float*)workspace;
+    p->arrived = (uint32_t*)((uint8_t*)workspace + partial_bytes);
+    e = launch_fill((int32_t*)p->arrived, 0, kSplitWork, nullptr);
+    if (e == hipSuccess) e = hipStreamSynchronize(nullptr);
+    if (e != hipSuccess) (void)hipFree(workspace);
+  }
+  if (e != hipSuccess) {
+    (void)hipGetLastError();
+    delete p;
+    return EEP_ERR_HIP;
+  }
   p->slot_stride = f.slot_stride ? f.slot_stride : packed;
   p->scale_stride = f.scale_stride ? f.scale_stride : packed_scale;
   *out = p;
@@ -918,9 +987,9 @@ int eep_product_create(const eep_product_config* cfg, eep_product** out) {
 
 int eep_product_destroy(eep_product* product) {
   if (!product) return EEP_OK;
-  const hipError_t e = hipDeviceSynchronize();
+  const hipError_t e = hipDeviceSynchronize(), e2 = hipFree(product->partial);
   delete product;
-  return e == hipSuccess ? EEP_OK : EEP_ERR_HIP;
+  return e == hipSuccess && e2 == hipSuccess ? EEP_OK : EEP_ERR_HIP;
 }
 
 int eep_expert_product(eep_product* product, const void* x, const float* x_scale, const void* w, const float* w_scale,
@@ -952,9 +1021,9 @@ int eep_expert_product(eep_product* product, const void* x, const float* x_scale
   const bool gate = f.gate == EEP_GATE_SILU;
   hipError_t e;
   switch (f.x_dtype) {
-    case EEP_FP8_E4M3: e = launch_product<EEP_FP8_E4M3>(a, f.y_dtype, gate, product->cus, (hipStream_t)stream); break;
-    case EEP_BF16: e = launch_product<EEP_BF16>(a, f.y_dtype, gate, product->cus, (hipStream_t)stream); break;
-    default: e = launch_product<EEP_F32>(a, f.y_dtype, gate, product->cus, (hipStream_t)stream);
+    case EEP_FP8_E4M3: e = launch_product<EEP_FP8_E4M3>(*product, a, f.y_dtype, gate, (hipStream_t)stream); break;
+    case EEP_BF16: e = launch_product<EEP_BF16>(*product, a, f.y_dtype, gate, (hipStream_t)stream); break;
+    default: e = launch_product<EEP_F32>(*product, a, f.y_dtype, gate, (hipStream_t)stream);
   }
   return e == hipSuccess ? EEP_OK : EEP_ERR_HIP;
 }

@@ -167,6 +167,27 @@ def test_captured_with_offsets_that_change():
     p.destroy()
 
 
+@pytest.mark.parametrize("K", [512, 1024, 1080, 2168, 7168])
+@pytest.mark.parametrize("x,y,gate", [("fp8", "fp8", True), ("fp8", "f32", False), ("bf16", "bf16", True), ("f32", "f32", False)])
+@pytest.mark.parametrize("counts", [(1,), (0, 3, 0, 16), (2, 1, 17, 0, 1)])
+def test_few_rows_divide_in_features(K, x, y, gate, counts):
+    """Few workgroups' worth of rows: parts of in_features by several workgroups, steps that do not divide evenly, a tail."""
+    if x == "fp8":
+        K = K // 128 * 128
+    case_and_check(21, counts, K, 256, x, y, gate, spare=1)
+
+
+def test_divided_product_twice_with_one_handle():
+    """The words that count the parts are as they were after every call, also where a call has fewer tiles than the one before."""
+    from paper_2605_10670_amd import layer
+    p = layer.ExpertProduct(num_slots=4, in_features=1024, out_features=256, x_dtype="fp8", y_dtype="fp8", gate=True, max_rows=40)
+    for i, counts in enumerate([(1, 0, 0, 0), (3, 1, 1, 3), (0, 0, 0, 0), (0, 16, 0, 17), (0, 0, 0, 2)] * 3):
+        c = lu.product_case(22 + i, counts, 1024, 256, "fp8", True, spare=1)
+        out, y_scale = lu.run_product(c, "fp8", product=p)
+        lu.check_product(c, "fp8", out, y_scale)
+    p.destroy()
+
+
 def test_results_do_not_depend_on_the_run():
     c = lu.product_case(20, (1, 40, 300), 1024, 256, "fp8", True)
     first = lu.run_product(c, "fp8")
