@@ -17,8 +17,8 @@ struct eep_product {
   eep_product_config cfg;
   int64_t slot_stride, scale_stride;  // bytes
   int cus;                            // of the device
-  float* partial;                     // sums of a part of in_features, kSplitWork workgroups' of k_product_thin
-  uint32_t* arrived;                  // how many workgroups of a tile have theirs; zero between calls
+  float* values;                      // of y before its scales are known, kFewGroups of k_product_few
+  uint32_t* arrived;                  // how many workgroups of a group have theirs there; zero between calls
 };
 
 namespace eep {
@@ -61,37 +61,81 @@ __device__ __forceinline__ void widen(const u32x4& c, bf16x8 (&out)[2]) {
 }
 
 // acc + a * b over the 128 bytes of a step.
-//
-// Codes are multiplied as bf16, of which the matrix cores keep every product: their 8-bit forms line the products of
-// 8 neighbouring k up with the largest of them and keep 13 bits below its first (measured with single products
-// beside a large one; across the eights nothing is lost).  On normally distributed rows a sum of 128 then is
-// 1.3e-5 off (2-norm), and 5.4e-5 with wider ones; as bf16 1e-8 and 7e-8.
 template <int DT>
 __device__ __forceinline__ f32x4 mma(const Frag& a, const Frag& b, f32x4 acc) {
-  if constexpr (DT == EEP_FP8_E4M3) {
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      bf16x8 av[2], bv[2];
-      widen(a.c[j], av);
-      widen(b.c[j], bv);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[i], bv[i], acc, 0, 0, 0);
-    }
-    return acc;
-  } else if constexpr (DT == EEP_BF16) {
+  if constexpr (DT == EEP_BF16) {
 #pragma unroll
     for (int j = 0; j < 2; ++j)
       acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a.c[j]),
                                                     __builtin_bit_cast(bf16x8, b.c[j]), acc, 0, 0, 0);
-    return acc;
   } else {
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.c[j][i]), __uint_as_float(b.c[j][i]), acc, 0, 0, 0);
-    return acc;
   }
+  return acc;
+}
+
+// Codes are multiplied as bf16, of which the matrix cores keep every product: their 8-bit forms line the products of
+// 8 neighbouring k up with the largest of them and keep 13 bits below its first (measured with single products
+// beside a large one; across the eights nothing is lost).  On normally distributed rows a sum of 128 then is
+// 1.3e-5 off (2-norm), and 5.4e-5 with wider ones; as bf16 1e-8 and 7e-8.  Only where the matrix cores are the bound and
+// the result is rounded to 16 or 8 bits are the 8-bit forms used (Operand).
+//
+// One block of 128: p[m] + w[m] * x.
+template <int M>
+__device__ __forceinline__ void multiply_codes(const Frag (&w)[M], const Frag& x, f32x4 (&p)[M]) {
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    bf16x8 xv[2];
+    widen(x.c[j], xv);
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+      bf16x8 wv[2];
+      widen(w[m].c[j], wv);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) p[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[i], xv[i], p[m], 0, 0, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);  // (what is widened ahead of time takes registers)
+  }
+}
+
+// The chunks of a row's last bytes; `left` of them from the first chunk on, the rest zeros.
+__device__ __forceinline__ Frag load_tail(const uint8_t* from, int left) {
+  Frag f;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    f.c[j] = u32x4{0, 0, 0, 0};
+    if (j * 64 < left) f.c[j] = *(const u32x4*)(from + j * 64);
+  }
+  return f;
+}
+
+// load(buffer, step) and multiply(buffer) over the steps [begin, end), AHEAD of them under way.
+template <int AHEAD, class Load, class Multiply>
+__device__ __forceinline__ void stream(int begin, int end, Load load, Multiply multiply) {
+  if (begin >= end) return;
+#pragma unroll
+  for (int u = 0; u < AHEAD; ++u) load(u, begin + u < end ? begin + u : end - 1);
+  int s = begin;
+  for (; s + 2 * AHEAD <= end; s += AHEAD) {
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      multiply(u);
+      load(u, s + u + AHEAD);
+    }
+  }
+  // fewer than twice AHEAD steps are left, up to AHEAD of them loaded
+#pragma unroll
+  for (int u = 0; u < AHEAD; ++u) {
+    if (s + u < end) multiply(u);
+    if (s + u + AHEAD < end) load(u, s + u + AHEAD);
+  }
+#pragma unroll
+  for (int u = 0; u < AHEAD; ++u)
+    if (s + u + AHEAD < end) multiply(u);
 }
 
 // An operand of mma, ready to be used several times.  WIDE: e4m3 codes are widened to bf16 (once), see above; else they are
@@ -207,25 +251,17 @@ __device__ __forceinline__ void store4(uint8_t* y, int64_t element, const float 
 // A workgroup of 8 wavefronts has 16 rows of one slot and 128 features of y with the gate, 256 without: each wavefront two
 // matrix-core tiles of 16 weight rows, with the gate the two factors of 16 features.  No weight is used by two
 // wavefronts, so nothing of them goes through LDS; the rows of x come from the caches.
-//
-// Where that makes fewer workgroups than the card holds, in_features are divided between `splits` workgroups (SPLIT): each
-// leaves its sums in memory, past the L2s, which do not see one another's writes; the last to arrive adds them up, in the order of
-// the parts whoever that is, and goes on as if they were its own.
 // ---------------------------------------------------------------------------
 constexpr int kThinTokens = 16, kThinWaves = 8;
-constexpr int kSplitWork = 512;                                // workgroups of a divided product at most
-constexpr int kSplitFloats = kThinTokens * 32 * kThinWaves;    // sums of one
-
-template <int DT, int YT, bool GATE, bool SPLIT>
-__global__ __launch_bounds__(64 * kThinWaves) void k_product_thin(ProductArgs a, int64_t first_tile, int splits,
-                                                                  float* partial, uint32_t* arrived) {
-  constexpr int U = 2;  // steps of loads in flight ahead of the ones that are multiplied
+template <int DT, int YT, bool GATE>
+__global__ __launch_bounds__(64 * kThinWaves, 4) void k_product_thin(ProductArgs a, int64_t first_tile) {
+  // steps under way; with the registers that widening takes, as many as leave two workgroups to a CU
+  constexpr int kAhead = DT == EEP_FP8_E4M3 ? 3 : 4;
   __shared__ uint32_t s_top[kThinWaves][16];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, part = lane >> 4;
-  [[maybe_unused]] __shared__ uint32_t s_arrived;
-  const int64_t work = SPLIT ? blockIdx.x / splits : first_tile + blockIdx.x;
-  const int split = SPLIT ? blockIdx.x - (int)work * splits : 0;
+  const int64_t work = first_tile + blockIdx.x;
   const int64_t row_tile = work / a.feature_tiles;
   const int feature_tile = (int)(work - row_tile * a.feature_tiles);
   int slot, row0, end;
@@ -241,121 +277,74 @@ __global__ __launch_bounds__(64 * kThinWaves) void k_product_thin(ProductArgs a,
     n0[1] = n0[0] + 16;
   }
   // rows past the end are read as the last one; their results are not stored
-  const uint8_t* slot_w = a.w + slot * a.slot_stride;
-  const uint8_t* from[3];
+  const uint8_t* from[3];  // the tiles' first rows, and where the lane reads from there
+  uint32_t at[3];
 #pragma unroll
   for (int m = 0; m < 2; ++m) {
+    const int first = n0[m] < weight_rows ? n0[m] : weight_rows - 1;
     const int n = n0[m] + col < weight_rows ? n0[m] + col : weight_rows - 1;
-    from[m] = slot_w + (int64_t)n * a.row_bytes + part * 16;
+    from[m] = a.w + slot * a.slot_stride + (int64_t)first * a.row_bytes;
+    at[m] = (uint32_t)(n - first) * (uint32_t)a.row_bytes + part * 16;
   }
   const int token = row0 + col < end ? row0 + col : end - 1;
-  from[2] = a.x + (int64_t)token * a.row_bytes + part * 16;
-  const int row_steps = a.row_bytes / kStepBytes;
-  const int begin = SPLIT ? row_steps * split / splits : 0;
-  const int steps = SPLIT ? row_steps * (split + 1) / splits : row_steps;  // (the one behind the last)
-  // bytes, a multiple of 16; 0 for fp8
-  const int tail = !SPLIT || split == splits - 1 ? a.row_bytes - row_steps * kStepBytes : 0;
+  from[2] = a.x + (int64_t)row0 * a.row_bytes;
+  at[2] = (uint32_t)(token - row0) * (uint32_t)a.row_bytes + part * 16;
+  const int steps = a.row_bytes / kStepBytes;
+  [[maybe_unused]] const int tail = a.row_bytes - steps * kStepBytes;  // bytes, a multiple of 16; 0 for fp8
   const float* sx = nullptr;
   const float* sw[2] = {nullptr, nullptr};
   if constexpr (DT == EEP_FP8_E4M3) {
-    sx = a.x_scale + (int64_t)token * row_steps;
+    sx = a.x_scale + (int64_t)token * steps;
     const float* slot_scale = (const float*)((const uint8_t*)a.w_scale + slot * a.scale_stride);
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
       const int n = n0[m] < weight_rows ? n0[m] : weight_rows - 1;
-      sw[m] = slot_scale + (int64_t)(n / kScaleBlock) * row_steps;
+      sw[m] = slot_scale + (int64_t)(n / kScaleBlock) * steps;
     }
   }
 
   f32x4 acc[2] = {};
-  Frag f[2][U][3];
-  float xs[2][U], ws[2][U][2];
-  auto load = [&](int buffer, int step) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int s = step + u < steps ? step + u : steps - 1;
-#pragma unroll
-      for (int m = 0; m < 3; ++m)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-          f[buffer][u][m].c[j] = *(const u32x4*)(from[m] + (int64_t)s * kStepBytes + j * 64);
-      if constexpr (DT == EEP_FP8_E4M3) {
-        xs[buffer][u] = sx[s];
-#pragma unroll
-        for (int m = 0; m < 2; ++m) ws[buffer][u][m] = sw[m][s];
-      }
-    }
-  };
-  auto multiply = [&](int buffer, int step) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (step + u >= steps) break;
-#pragma unroll
-      for (int m = 0; m < 2; ++m) {
-        if constexpr (DT == EEP_FP8_E4M3) {
-          const f32x4 p = mma<DT>(f[buffer][u][m], f[buffer][u][2], f32x4{0, 0, 0, 0});
-          const float scale = xs[buffer][u] * ws[buffer][u][m];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) acc[m][i] = fmaf(p[i], scale, acc[m][i]);
-        } else {
-          acc[m] = mma<DT>(f[buffer][u][m], f[buffer][u][2], acc[m]);
-        }
-      }
-    }
-  };
-  if (begin < steps) load(0, begin);
-  for (int s = begin; s < steps; s += 2 * U) {
-    if (s + U < steps) load(1, s + U);
-    multiply(0, s);
-    if (s + 2 * U < steps) load(0, s + 2 * U);
-    multiply(1, s + U);
-  }
-  if (tail != 0) {
-    Frag t[3];
+  Frag f[kAhead][3];
+  float xs[kAhead], ws[kAhead][2];
+  auto load = [&](int buffer, int s) {
 #pragma unroll
     for (int m = 0; m < 3; ++m)
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        t[m].c[j] = u32x4{0, 0, 0, 0};
-        if (j * 64 + part * 16 < tail) t[m].c[j] = *(const u32x4*)(from[m] + (int64_t)steps * kStepBytes + j * 64);
-      }
+      for (int j = 0; j < 2; ++j) f[buffer][m].c[j] = *(const u32x4*)(from[m] + (at[m] + (uint32_t)(s * kStepBytes + j * 64)));
+    if constexpr (DT == EEP_FP8_E4M3) {
+      xs[buffer] = sx[s];
 #pragma unroll
-    for (int m = 0; m < 2; ++m) acc[m] = mma<DT>(t[m], t[2], acc[m]);
+      for (int m = 0; m < 2; ++m) ws[buffer][m] = sw[m][s];
+    }
+  };
+  auto multiply = [&](int buffer) {
+    if constexpr (DT == EEP_FP8_E4M3) {
+      f32x4 p[2] = {};
+      multiply_codes<2>({f[buffer][0], f[buffer][1]}, f[buffer][2], p);
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        const float scale = xs[buffer] * ws[buffer][m];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[m][i] = fmaf(p[m][i], scale, acc[m][i]);
+      }
+    } else {
+#pragma unroll
+      for (int m = 0; m < 2; ++m) acc[m] = mma<DT>(f[buffer][m], f[buffer][2], acc[m]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  stream<kAhead>(0, steps, load, multiply);
+  if constexpr (DT != EEP_FP8_E4M3) {
+    if (tail != 0) {
+      Frag t[3];
+#pragma unroll
+      for (int m = 0; m < 3; ++m) t[m] = load_tail(from[m] + (at[m] + (uint32_t)(steps * kStepBytes)), tail - part * 16);
+#pragma unroll
+      for (int m = 0; m < 2; ++m) acc[m] = mma<DT>(t[m], t[2], acc[m]);
+    }
   }
 
   const bool in_rows = row0 + col < end;
-  if constexpr (SPLIT) {
-    float* own = partial + (work * splits + split) * kSplitFloats;
-    const int at = ((wave * 2 * 16 + col) * 4 + part) * 4;
-    if (in_rows) {
-#pragma unroll
-      for (int m = 0; m < 2; ++m) store_row((u32x4*)(own + at + m * 256), __builtin_bit_cast(u32x4, acc[m]));
-    }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the stores are where all workgroups see them
-    __syncthreads();
-    if (threadIdx.x == 0) s_arrived = __hip_atomic_fetch_add(&arrived[work], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __syncthreads();
-    if (s_arrived != (uint32_t)splits - 1) return;
-    if (threadIdx.x == 0) __hip_atomic_store(&arrived[work], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    acc[0] = acc[1] = f32x4{0, 0, 0, 0};
-    if (in_rows) {
-      const float* all = partial + work * splits * kSplitFloats + at;
-#pragma unroll 4
-      for (int p = 0; p < splits; ++p) {
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-          const uint64_t* v = (const uint64_t*)(all + (int64_t)p * kSplitFloats + m * 256);
-          const uint64_t lo = __hip_atomic_load(v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-          const uint64_t hi = __hip_atomic_load(v + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-          acc[m][0] += __uint_as_float((uint32_t)lo);
-          acc[m][1] += __uint_as_float((uint32_t)(lo >> 32));
-          acc[m][2] += __uint_as_float((uint32_t)hi);
-          acc[m][3] += __uint_as_float((uint32_t)(hi >> 32));
-        }
-      }
-    }
-  }
-
   const int64_t out_row = (int64_t)(row0 + col) * a.features;
   if constexpr (GATE) {
     const int n = n0[0] + part * 4;
@@ -385,6 +374,173 @@ __global__ __launch_bounds__(64 * kThinWaves) void k_product_thin(ProductArgs a,
       const float v[4] = {acc[m][0], acc[m][1], acc[m][2], acc[m][3]};
       if (in_rows && n < a.features) store4<YT>(a.y, out_row + n, v);
     }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// so few rows that the others would leave CUs idle: 16 * M weight rows by 16 * TN tokens a workgroup.
+//
+// The workgroup's 8 wavefronts divide in_features and add their sums up in LDS, in the order of the parts; with the gate a
+// tile's 16 rows are 8 of either factor.  Codes need the largest of 128 features, which are 16 tiles' here: each leaves
+// its values in memory, past the L2s, which do not see one another's writes, and the last to arrive makes the codes of
+// all.  (Its loads look past the caches one by one; a fence would empty them for everybody.)
+// ---------------------------------------------------------------------------
+constexpr int kFewGroups = 256;  // groups of 16 tokens by 128 features that the workspace holds
+
+// Two workgroups to a CU, or one with twice the registers.
+constexpr bool few_alone(int m, int tn) { return m * tn > 2; }
+
+template <int DT, int YT, bool GATE, int M, int TN>
+__global__ __launch_bounds__(64 * kThinWaves, few_alone(M, TN) ? 2 : 4) void k_product_few(ProductArgs a, float* values, uint32_t* arrived) {
+  constexpr bool kCodes = DT == EEP_FP8_E4M3;
+  constexpr int kAhead = few_alone(M, TN) ? (M + TN > 8 ? 1 : 16 / (M + TN)) : M + TN == 2 ? 4 : 3;  // steps under way, as many as there are registers for
+  constexpr int kFeatures = GATE ? 8 : 16;
+  __shared__ f32x4 s_sum[kThinWaves][M * TN][64];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 15, part = lane >> 4;
+  const int row_tile = blockIdx.x / a.feature_tiles, feature_tile = blockIdx.x - row_tile * a.feature_tiles;
+  int slot, row0, end;
+  if (!find_tile<kThinTokens * TN>(a, row_tile, &slot, &row0, &end)) return;
+
+  const int row_steps = a.row_bytes / kStepBytes;
+  const int begin = row_steps * wave / kThinWaves, steps = row_steps * (wave + 1) / kThinWaves;
+  const uint8_t* w_base = a.w + slot * a.slot_stride;
+  const uint8_t* x_base = a.x + (int64_t)row0 * a.row_bytes;
+  const float *w_scale = nullptr, *x_scale = nullptr;
+  uint32_t w_at[M], x_at[TN], w_scale_at[M], x_scale_at[TN];
+  if constexpr (kCodes) {
+    w_scale = (const float*)((const uint8_t*)a.w_scale + slot * a.scale_stride);
+    x_scale = a.x_scale + (int64_t)row0 * row_steps;
+  }
+#pragma unroll
+  for (int m = 0; m < M; ++m) {
+    const int n0 = (feature_tile * M + m) * kFeatures;
+    const int second = GATE && col >= kFeatures ? 1 : 0;  // of the factors
+    int n = n0 + col - second * kFeatures;
+    n = n < a.features ? n : a.features - 1;
+    w_at[m] = (uint32_t)(n + second * a.features) * (uint32_t)a.row_bytes + part * 16;
+    // the scale is that of the lane's sums: with the gate those of parts 2 and 3 belong to the other factor
+    const int row = (n0 < a.features ? n0 : 0) + (GATE && part >= 2 ? a.features : 0);
+    w_scale_at[m] = (uint32_t)(row / kScaleBlock * row_steps);
+  }
+#pragma unroll
+  for (int t = 0; t < TN; ++t) {
+    const int token = row0 + t * 16 + col < end ? t * 16 + col : end - 1 - row0;
+    x_at[t] = (uint32_t)token * (uint32_t)a.row_bytes + part * 16;
+    x_scale_at[t] = (uint32_t)(token * row_steps);
+  }
+
+  f32x4 acc[M][TN] = {};
+  Frag w[kAhead][M], x[kAhead][TN];
+  float xs[kAhead][TN], ws[kAhead][M];
+  auto load = [&](int buffer, int s) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const uint32_t at = (uint32_t)(s * kStepBytes + j * 64);
+#pragma unroll
+      for (int m = 0; m < M; ++m) w[buffer][m].c[j] = *(const u32x4*)(w_base + (w_at[m] + at));
+#pragma unroll
+      for (int t = 0; t < TN; ++t) x[buffer][t].c[j] = *(const u32x4*)(x_base + (x_at[t] + at));
+    }
+    if constexpr (kCodes) {
+#pragma unroll
+      for (int m = 0; m < M; ++m) ws[buffer][m] = w_scale[w_scale_at[m] + (uint32_t)s];
+#pragma unroll
+      for (int t = 0; t < TN; ++t) xs[buffer][t] = x_scale[x_scale_at[t] + (uint32_t)s];
+    }
+  };
+  auto multiply = [&](int buffer) {
+#pragma unroll
+    for (int t = 0; t < TN; ++t) {
+      if constexpr (kCodes) {
+        f32x4 p[M] = {};
+        multiply_codes<M>(w[buffer], x[buffer][t], p);
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+          const float scale = xs[buffer][t] * ws[buffer][m];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[m][t][i] = fmaf(p[m][i], scale, acc[m][t][i]);
+        }
+      } else {
+#pragma unroll
+        for (int m = 0; m < M; ++m) acc[m][t] = mma<DT>(w[buffer][m], x[buffer][t], acc[m][t]);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  stream<kAhead>(begin, steps, load, multiply);
+  if constexpr (!kCodes) {
+    const int tail = a.row_bytes - row_steps * kStepBytes;
+    if (tail != 0 && wave == kThinWaves - 1) {
+      const uint32_t at = (uint32_t)(row_steps * kStepBytes);
+#pragma unroll
+      for (int m = 0; m < M; ++m) {
+        const Frag wt = load_tail(w_base + (w_at[m] + at), tail - part * 16);
+#pragma unroll
+        for (int t = 0; t < TN; ++t) acc[m][t] = mma<DT>(wt, load_tail(x_base + (x_at[t] + at), tail - part * 16), acc[m][t]);
+      }
+    }
+  }
+#pragma unroll
+  for (int m = 0; m < M; ++m)
+#pragma unroll
+    for (int t = 0; t < TN; ++t) s_sum[wave][m * TN + t][lane] = acc[m][t];
+  __syncthreads();
+  // a wavefront finishes a tile
+  if (wave >= M * TN) return;
+  const int m = wave / TN, t = wave % TN;
+  const int n0 = (feature_tile * M + m) * kFeatures;
+  if (n0 >= a.features) return;
+  f32x4 sum = s_sum[0][wave][lane];
+#pragma unroll
+  for (int other = 1; other < kThinWaves; ++other) sum += s_sum[other][wave][lane];
+
+  const int64_t row = row0 + t * 16 + col;
+  const bool in_rows = row < end;
+  float v[4] = {sum[0], sum[1], sum[2], sum[3]};
+  if constexpr (GATE) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = silu_times(v[i], __shfl_xor(v[i], 32, 64));
+  }
+  const bool has = in_rows && (!GATE || part < 2);  // (with the gate the other parts have nothing of their own now)
+  const int n = n0 + part * 4;
+  if constexpr (YT != EEP_FP8_E4M3) {
+    if (has && n < a.features) store4<YT>(a.y, row * a.features + n, v);
+  } else {
+    constexpr int kMembers = kScaleBlock / kFeatures;  // (whole groups: features are a multiple of 128)
+    const int blocks = a.features / kScaleBlock, block = n0 / kScaleBlock;
+    const int group = (row_tile * TN + t) * blocks + block;
+    float* all = values + ((int64_t)group * kThinTokens + col) * kScaleBlock;
+    if (has) store_row((u32x4*)(all + n % kScaleBlock), __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]}));
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // they are where all workgroups see them
+    uint32_t before = 0;
+    if (lane == 0) before = __hip_atomic_fetch_add(&arrived[group], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (__builtin_amdgcn_readfirstlane(before) != kMembers - 1) return;
+    if (lane == 0) __hip_atomic_store(&arrived[group], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (!in_rows) return;  // (lanes of one token go together)
+    // a lane has every fourth 8 features of a token
+    float q[4][8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint64_t d = __hip_atomic_load((const uint64_t*)(all + (i * 4 + part) * 8) + j, __ATOMIC_RELAXED,
+                                             __HIP_MEMORY_SCOPE_AGENT);
+        q[i][2 * j] = __uint_as_float((uint32_t)d);
+        q[i][2 * j + 1] = __uint_as_float((uint32_t)(d >> 32));
+      }
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = max(top, top_magnitude<8>(q[i]));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
+    const float scale = scale_of(top);
+    if (part == 0) a.y_scale[row * blocks + block] = scale;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *(u32x2*)(a.y + row * a.features + block * kScaleBlock + (i * 4 + part) * 8) =
+          u32x2{codes4(q[i][0], q[i][1], q[i][2], q[i][3], scale), codes4(q[i][4], q[i][5], q[i][6], q[i][7], scale)};
   }
 }
 
@@ -865,24 +1021,30 @@ int64_t most_tiles(int rows, int slots, int tokens) {
 }
 
 template <int DT, int YT, bool GATE>
-hipError_t launch_thin(const eep_product& p, ProductArgs a, hipStream_t st) {
-  constexpr int kThreads = 64 * kThinWaves, kMinSteps = 4;  // steps of a part: those that are in flight at a time
-  const int features = GATE ? 16 * kThinWaves : 32 * kThinWaves;
-  a.feature_tiles = (a.features + features - 1) / features;
+hipError_t launch_thin(ProductArgs a, hipStream_t st) {
+  constexpr int kThreads = 64 * kThinWaves, kFeatures = GATE ? 16 * kThinWaves : 32 * kThinWaves;
+  a.feature_tiles = (a.features + kFeatures - 1) / kFeatures;
   const int64_t work = most_tiles(a.rows, a.slots, kThinTokens) * a.feature_tiles;
-  const int steps = a.row_bytes / kStepBytes;
-  int64_t splits = kSplitWork / work;
-  if (splits > steps / kMinSteps) splits = steps / kMinSteps;
-  if (splits > 1) {
-    hipLaunchKernelGGL((k_product_thin<DT, YT, GATE, true>), dim3((unsigned)(work * splits)), dim3(kThreads), 0, st, a,
-                       (int64_t)0, (int)splits, p.partial, p.arrived);
-    return hipGetLastError();
-  }
   return in_launches(work, max_blocks(kThreads), [&](int64_t first, int64_t n) {
-    hipLaunchKernelGGL((k_product_thin<DT, YT, GATE, false>), dim3((unsigned)n), dim3(kThreads), 0, st, a, first, 1, nullptr,
-                       nullptr);
+    hipLaunchKernelGGL((k_product_thin<DT, YT, GATE>), dim3((unsigned)n), dim3(kThreads), 0, st, a, first);
     return hipGetLastError();
   });
+}
+
+// false: that would be more workgroups than the CUs take at a time, or more groups than the workspace holds, or weights of a
+// slot that 32 bits do not span
+template <int DT, int YT, bool GATE, int M, int TN>
+bool launch_few(const eep_product& p, ProductArgs a, hipStream_t st, hipError_t* e) {
+  constexpr int kFeatures = (GATE ? 8 : 16) * M;
+  a.feature_tiles = (a.features + kFeatures - 1) / kFeatures;
+  const int64_t row_tiles = most_tiles(a.rows, a.slots, kThinTokens * TN), work = row_tiles * a.feature_tiles;
+  if (work > (few_alone(M, TN) ? 1 : 2) * p.cus || (int64_t)a.features * (GATE ? 2 : 1) * a.row_bytes >= (int64_t)1 << 32)
+    return false;
+  if (YT == EEP_FP8_E4M3 && row_tiles * TN * (a.features / kScaleBlock) > kFewGroups) return false;
+  hipLaunchKernelGGL((k_product_few<DT, YT, GATE, M, TN>), dim3((unsigned)work), dim3(64 * kThinWaves), 0, st, a, p.values,
+                     p.arrived);
+  *e = hipGetLastError();
+  return true;
 }
 
 template <int DT, int YT, bool GATE, int TT>
@@ -903,7 +1065,17 @@ hipError_t launch_tiled(ProductArgs a, int cus, hipStream_t st) {
 template <int DT, int YT, bool GATE>
 hipError_t launch_product(const eep_product& p, const ProductArgs& a, hipStream_t st) {
   const int mean = (a.rows + a.slots - 1) / a.slots;  // rows a slot
-  if (mean <= 16 || a.row_bytes <= 2 * kStepBytes) return launch_thin<DT, YT, GATE>(p, a, st);
+  hipError_t e = hipSuccess;
+  if (mean <= 16) {
+    if (launch_few<DT, YT, GATE, 1, 1>(p, a, st, &e) || launch_few<DT, YT, GATE, 2, 1>(p, a, st, &e) ||
+        launch_few<DT, YT, GATE, 8, 1>(p, a, st, &e))
+      return e;
+  } else if (mean <= 32) {
+    if (launch_few<DT, YT, GATE, 1, 2>(p, a, st, &e) || launch_few<DT, YT, GATE, 4, 2>(p, a, st, &e)) return e;
+  } else if (mean <= 64) {
+    if (launch_few<DT, YT, GATE, 1, 4>(p, a, st, &e) || launch_few<DT, YT, GATE, 2, 4>(p, a, st, &e)) return e;
+  }
+  if (mean <= 16 || a.row_bytes <= 2 * kStepBytes) return launch_thin<DT, YT, GATE>(a, st);
   if (mean <= 64) return launch_tiled<DT, YT, GATE, 1>(a, p.cus, st);
   // (widened codes take twice the registers)
   if constexpr (DT != EEP_FP8_E4M3 || YT != EEP_F32)
@@ -964,13 +1136,13 @@ int eep_product_create(const eep_product_config* cfg, eep_product** out) {
     delete p;
     return EEP_ERR_HIP;
   }
-  const int64_t partial_bytes = (int64_t)kSplitWork * kSplitFloats * sizeof(float);
+  const int64_t value_bytes = (int64_t)kFewGroups * kThinTokens * kScaleBlock * sizeof(float);
   void* workspace = nullptr;
-  hipError_t e = hipMalloc(&workspace, partial_bytes + kSplitWork * sizeof(uint32_t));
+  hipError_t e = hipMalloc(&workspace, value_bytes + kFewGroups * sizeof(uint32_t));
   if (e == hipSuccess) {
-    p->partial = (float*)workspace;
-    p->arrived = (uint32_t*)((uint8_t*)workspace + partial_bytes);
-    e = launch_fill((int32_t*)p->arrived, 0, kSplitWork, nullptr);
+    p->values = (float*)workspace;
+    p->arrived = (uint32_t*)((uint8_t*)workspace + value_bytes);
+    e = launch_fill((int32_t*)p->arrived, 0, kFewGroups, nullptr);
     if (e == hipSuccess) e = hipStreamSynchronize(nullptr);
     if (e != hipSuccess) (void)hipFree(workspace);
   }
@@ -987,7 +1159,7 @@ int eep_product_create(const eep_product_config* cfg, eep_product** out) {
 
 int eep_product_destroy(eep_product* product) {
   if (!product) return EEP_OK;
-  const hipError_t e = hipDeviceSynchronize(), e2 = hipFree(product->partial);
+  const hipError_t e = hipDeviceSynchronize(), e2 = hipFree(product->values);
   delete product;
   return e == hipSuccess && e2 == hipSuccess ? EEP_OK : EEP_ERR_HIP;
 }
