@@ -6,6 +6,8 @@
 // per block, and stores 8 or 16 bytes of a row of y.  Whatever the type, a step is 128 bytes along in_features, of which lane
 // l takes 16 bytes of row l % 16 at 16 * (l / 16) and 16 more 64 bytes on, of both operands alike: a product of sums
 // does not ask in which order its terms come, so the matrix cores' own order of k plays no part.
+#include <math.h>
+
 #include <new>
 #include <type_traits>
 
@@ -246,7 +248,7 @@ __device__ __forceinline__ void store4(uint8_t* y, int64_t element, const float 
 }
 
 // ---------------------------------------------------------------------------
-// few rows a slot: the weights go straight to registers.
+// a row or so a slot: the weights go straight to registers.
 //
 // A workgroup of 8 wavefronts has 16 rows of one slot and 128 features of y with the gate, 256 without: each wavefront two
 // matrix-core tiles of 16 weight rows, with the gate the two factors of 16 features.  No weight is used by two
@@ -1062,6 +1064,22 @@ hipError_t launch_tiled(ProductArgs a, int cus, hipStream_t st) {
   return hipGetLastError();
 }
 
+// What the tiles of 64 * tt tokens cost, in time: what a step of one takes (measured, us), as often as a CU has one.  A slot's last
+// tile is half empty on average.
+float tiled_cost(int tt, int rows, int slots, int64_t feature_tiles, int cus) {
+  const float step = tt == 1 ? 0.95f : tt == 2 ? 1.35f : 2.2f;
+  const int touched = rows < slots ? rows : slots;
+  float tiles = (float)rows / touched / (64 * tt) + 0.5f;
+  if (touched == 1) tiles = (float)((rows + 64 * tt - 1) / (64 * tt));
+  const float rounds = (tiles < 1.0f ? 1.0f : tiles) * touched * feature_tiles / cus;
+  return step * (rounds < 4.0f ? ceilf(rounds) : rounds);
+}
+
+// Rows a slot up to which the thin kernel is chosen.  Thin / tiles of 64 tokens, us: 32 tokens of 288 slots 2048 -> 7168 fp8
+// to fp32 (0.9 rows a slot) 405 / 510, 7168 -> 2 x 2048 822 / 802; 64 tokens (1.8) 1178 / 1146, 144 slots bf16 4096 ->
+// 2 x 1024 (3.6) 464 / 410; 256 tokens (7.1) 1480 / 1353; 512 (14.2: many slots have more than 16) 1986 / 1362.
+constexpr int kThinMean = 1;
+
 template <int DT, int YT, bool GATE>
 hipError_t launch_product(const eep_product& p, const ProductArgs& a, hipStream_t st) {
   const int mean = (a.rows + a.slots - 1) / a.slots;  // rows a slot
@@ -1075,12 +1093,15 @@ hipError_t launch_product(const eep_product& p, const ProductArgs& a, hipStream_
   } else if (mean <= 64) {
     if (launch_few<DT, YT, GATE, 1, 4>(p, a, st, &e) || launch_few<DT, YT, GATE, 2, 4>(p, a, st, &e)) return e;
   }
-  if (mean <= 16 || a.row_bytes <= 2 * kStepBytes) return launch_thin<DT, YT, GATE>(a, st);
-  if (mean <= 64) return launch_tiled<DT, YT, GATE, 1>(a, p.cus, st);
-  // (widened codes take twice the registers)
-  if constexpr (DT != EEP_FP8_E4M3 || YT != EEP_F32)
-    if (mean > 160) return launch_tiled<DT, YT, GATE, 4>(a, p.cus, st);
-  return launch_tiled<DT, YT, GATE, 2>(a, p.cus, st);
+  // (the tiles' stream is as long as three steps at least)
+  if (mean <= kThinMean || a.row_bytes <= 2 * kStepBytes) return launch_thin<DT, YT, GATE>(a, st);
+  constexpr bool kLarge = DT != EEP_FP8_E4M3 || YT != EEP_F32;  // (widened codes take twice the registers)
+  const int64_t feature_tiles = (a.features + kTiledRows / (GATE ? 2 : 1) - 1) / (kTiledRows / (GATE ? 2 : 1));
+  auto cost = [&](int tt) { return tiled_cost(tt, a.rows, a.slots, feature_tiles, p.cus); };
+  const float one = cost(1), two = cost(2), four = cost(4);
+  if constexpr (kLarge)
+    if (four <= one && four <= two) return launch_tiled<DT, YT, GATE, 4>(a, p.cus, st);
+  return one <= two ? launch_tiled<DT, YT, GATE, 1>(a, p.cus, st) : launch_tiled<DT, YT, GATE, 2>(a, p.cus, st);
 }
 
 template <int DT>
