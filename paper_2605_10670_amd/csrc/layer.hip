@@ -12,7 +12,9 @@ namespace eep {
 // One workgroup has a row, all of it in registers (NV vectors of 8 channels a thread, neighbouring threads on
 // neighbouring vectors): the row is read once, and only the sum of squares crosses wavefronts.  The lanes of
 // a scale group are neighbours of one wavefront.  Bound by memory at many rows, by one trip to memory and
-// the exchange at few.
+// the exchange at few.  Measured: 16384 rows of 7168 bf16 with residual, sum, y and codes 177 us (6.0 TB/s; with plain instead of
+// non-temporal stores 196, with up to 128 / 256 / 1024 threads a row 196 / 187 / 185); 5976 rows of 2880 fp32 38.9 us (6.2 TB/s);
+// one row of 7168 3.4 us on the device.
 // ---------------------------------------------------------------------------
 constexpr int kNormMaxHidden = 65536;  // 1024 threads of 8 vectors
 
@@ -51,17 +53,17 @@ __device__ __forceinline__ void store8(void* base, int64_t vec, const float (&v)
     u32x4 d;
 #pragma unroll
     for (int i = 0; i < 4; ++i) d[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
-    ((u32x4*)base)[vec] = d;
+    __builtin_nontemporal_store(d, &((u32x4*)base)[vec]);
   } else {
-    ((f32x4*)base)[2 * vec] = f32x4{v[0], v[1], v[2], v[3]};
-    ((f32x4*)base)[2 * vec + 1] = f32x4{v[4], v[5], v[6], v[7]};
+    __builtin_nontemporal_store(f32x4{v[0], v[1], v[2], v[3]}, &((f32x4*)base)[2 * vec]);
+    __builtin_nontemporal_store(f32x4{v[4], v[5], v[6], v[7]}, &((f32x4*)base)[2 * vec + 1]);
   }
 }
 
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) v += __shfl_xor(v, m, 64);
-  return v;
+// The sum over groups of 16 or all 64 lanes, in every lane.
+template <int LANES>
+__device__ __forceinline__ float lane_sum(float v) {
+  return fold<LANES>(v, [](float a, float b) { return a + b; });
 }
 
 template <bool IN_BF16, bool GAIN_BF16, bool OUT_BF16, int NV>
@@ -97,7 +99,7 @@ __global__ __launch_bounds__(1024) void k_norm(NormArgs a, int64_t first) {
         squares = fmaf(v, v, squares);
       }
     }
-    squares = wave_sum(squares);
+    squares = lane_sum<64>(squares);
     if (threads > 64) {
       if ((tid & 63) == 0) s_part[tid >> 6] = squares;
       __syncthreads();
@@ -130,7 +132,7 @@ __global__ __launch_bounds__(1024) void k_norm(NormArgs a, int64_t first) {
       u32x2 c;
       c[0] = codes4(h[j][0], h[j][1], h[j][2], h[j][3], scale);
       c[1] = codes4(h[j][4], h[j][5], h[j][6], h[j][7], scale);
-      ((u32x2*)a.code)[row_vec + v] = c;
+      __builtin_nontemporal_store(c, &((u32x2*)a.code)[row_vec + v]);
     }
   }
 }
@@ -138,9 +140,9 @@ __global__ __launch_bounds__(1024) void k_norm(NormArgs a, int64_t first) {
 template <bool IN_BF16, bool GAIN_BF16, bool OUT_BF16>
 hipError_t launch_norm(const NormArgs& a, int T, hipStream_t st) {
   const int vecs = a.H / 8;
-  // vectors a thread: the fewest that fit a workgroup at few rows; at many rows as many as leave two wavefronts
+  // vectors a thread: one at few rows, up to 1024 threads; at many rows up to 512 threads, of which a CU takes more workgroups
   int nv = 1;
-  while (nv < 8 && (vecs > nv * 1024 || (T >= 1024 && vecs > nv * 128))) nv *= 2;
+  while (nv < 8 && (vecs > nv * 1024 || (T >= 1024 && vecs > nv * 512))) nv *= 2;
   const int threads = ((vecs + nv - 1) / nv + 63) / 64 * 64;
   return in_launches(T, max_blocks(threads), [&](int64_t first, int64_t n) {
     const dim3 grid((unsigned)n), block((unsigned)threads);
@@ -157,12 +159,18 @@ hipError_t launch_norm(const NormArgs& a, int T, hipStream_t st) {
 // ---------------------------------------------------------------------------
 // route: the k largest of E logits, ties to the lower index, and their softmax weights.
 //
-// One wavefront has a token, lane l the logits [l * NV, (l + 1) * NV), so that the order of the indices is the order of
-// lanes and of registers.  A round finds the largest of the lanes' best, takes the first lane that has it and the
-// first register there, and strikes it out.  The values are compared as integers of the same order (order_of);
-// 0 is what may not be chosen.
+// A group of LANES lanes has a token, lane l of it the logits [l * NV, (l + 1) * NV), so that the order of the indices is the
+// order of lanes and of registers.  A round finds the largest of the lanes' best; the first lane that has it writes its index,
+// strikes out the first register there and looks for its next best.  The values are compared as integers of the same
+// order (order_of); 0 is what may not be chosen.
+//
+// The rounds are the bound, not memory.  At many tokens four share a wavefront (16 lanes, up to 16 logits each) and the
+// instructions of a round, whose exchanges stay within a row of lanes; at few, where a round's latency counts, and beyond
+// 256 logits a token has one for itself.  Measured, 256 logits, top-8, a token a wavefront / four, us: 32 tokens 4.1 / 6.0,
+// 4096 4.6 / 5.4, 8192 6.5 / 6.0, 16384 (bf16) 11.0 / 8.8; 128 logits, 16384 tokens 10.7 / 5.7.
 // ---------------------------------------------------------------------------
 constexpr int kRouteMaxExperts = 4096;
+constexpr int kRouteShared = 8192;  // tokens from which four share a wavefront
 
 // An integer that grows with the value; 0 for -infinity and NaN.  -0 and +0 are one value.
 __device__ __forceinline__ uint32_t order_of(float v) {
@@ -176,87 +184,115 @@ __device__ __forceinline__ float value_of(uint32_t order) {
 // exp(v - top) where top >= v, also where both are +infinity
 __device__ __forceinline__ float exp_below(float v, float top) { return v == top ? 1.0f : expf(v - top); }
 
-template <bool BF16, int NV>
+// FOURS: four logits at a time, of rows that are whole fours and aligned to them.
+template <bool BF16, int LANES, int NV, bool FOURS>
 __global__ __launch_bounds__(256) void k_route(const void* __restrict__ logits, int32_t* __restrict__ topk_idx,
                                                float* __restrict__ topk_w, int E, int k, int over_all, int64_t first,
                                                int64_t end) {
-  const int lane = threadIdx.x & 63;
-  const int64_t t = first + (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (t >= end) return;
+  constexpr int kTokens = 256 / LANES;
+  const int lane = threadIdx.x & (LANES - 1);
+  const int64_t t = first + (int64_t)blockIdx.x * kTokens + threadIdx.x / LANES;
+  if (t >= end) return;  // (a group's lanes go together)
   uint32_t o[NV];
+  if constexpr (FOURS) {
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int e = lane * NV + i;
-    o[i] = 0;
-    if (e < E)
-      o[i] = order_of(BF16 ? __uint_as_float((uint32_t)((const uint16_t*)logits)[t * E + e] << 16)
-                           : ((const float*)logits)[t * E + e]);
+    for (int i = 0; i < NV; i += 4) {
+      const int e = lane * NV + i;
+      float v[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      if (e < E) {
+        if constexpr (BF16) {
+          const u32x2 d = *(const u32x2*)((const uint16_t*)logits + t * E + e);
+          v[0] = bf16_lo(d[0]), v[1] = bf16_hi(d[0]), v[2] = bf16_lo(d[1]), v[3] = bf16_hi(d[1]);
+        } else {
+          const f32x4 d = *(const f32x4*)((const float*)logits + t * E + e);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[j] = d[j];
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[i + j] = order_of(v[j]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int e = lane * NV + i;
+      o[i] = 0;
+      if (e < E)
+        o[i] = order_of(BF16 ? __uint_as_float((uint32_t)((const uint16_t*)logits)[t * E + e] << 16)
+                             : ((const float*)logits)[t * E + e]);
+    }
   }
   uint32_t best = 0;
 #pragma unroll
   for (int i = 0; i < NV; ++i) best = o[i] > best ? o[i] : best;
-  uint32_t mine = 0;  // lane j: the order and the index of the j-th choice
-  int32_t choice = -1;
-  int32_t index = 0;  // what this lane won last
-  uint32_t top = 0;
+  const auto larger = [](uint32_t a, uint32_t b) { return a > b ? a : b; };
+  uint32_t mine = 0;  // lane j: the order of the j-th choice
+  const uint32_t top = fold<LANES>(best, larger);
   float all = 0.0f;
-  for (int j = 0; j < k; ++j) {
-    const uint32_t largest = group_max(best, 64);
-    if (j == 0) {
-      top = largest;
-      if (over_all != 0 && top != 0) {
+  if (over_all != 0 && top != 0) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) all += o[i] != 0 ? exp_below(value_of(o[i]), value_of(top)) : 0.0f;
-      }
+    for (int i = 0; i < NV; ++i) all += o[i] != 0 ? exp_below(value_of(o[i]), value_of(top)) : 0.0f;
+  }
+  uint32_t largest = top;
+  for (int j = 0; j < k; ++j) {
+    if (j > 0) largest = fold<LANES>(best, larger);
+    if (lane == j) mine = largest;
+    if (largest == 0) {
+      if (lane == 0) topk_idx[t * k + j] = -1;
+      continue;
     }
-    if (largest == 0) break;
-    const int winner = __builtin_ctzll(__ballot(best == largest));
-    if (lane == winner) {
-      // strike out the first register that has it; the next best of what is left
+    uint64_t have = __ballot(best == largest);
+    if constexpr (LANES < 64) have = (have >> (threadIdx.x & 63 & ~(LANES - 1))) & ((1ull << LANES) - 1);
+    if (lane == __builtin_ctzll(have)) {
       uint32_t next = 0;
-      bool found = false;
-      int at = 0;
+      int at = -1;
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        if (!found && o[i] == largest) {
-          found = true;
-          at = i;
-          o[i] = 0;
-        }
-        next = o[i] > next ? o[i] : next;
+        const bool struck = at < 0 && o[i] == largest;
+        at = struck ? i : at;
+        o[i] = struck ? 0 : o[i];
+        next = larger(next, o[i]);
       }
       best = next;
-      index = lane * NV + at;
-    }
-    const int32_t chosen = __builtin_amdgcn_readlane(index, winner);
-    if (lane == j) {
-      mine = largest;
-      choice = chosen;
+      topk_idx[t * k + j] = lane * NV + at;
     }
   }
   const float e = mine != 0 ? exp_below(value_of(mine), value_of(top)) : 0.0f;
-  const float sum = wave_sum(over_all != 0 ? all : e);
-  if (lane < k) {
-    topk_idx[t * k + lane] = choice;
-    topk_w[t * k + lane] = mine != 0 ? e / sum : 0.0f;
-  }
+  const float sum = lane_sum<LANES>(over_all != 0 ? all : e);
+  if (lane < k) topk_w[t * k + lane] = mine != 0 ? e / sum : 0.0f;
+}
+
+template <bool BF16, int LANES, int NV>
+hipError_t launch_route(const eep_router_shape& s, const void* logits, int32_t* topk_idx, float* topk_w, int T,
+                        hipStream_t st) {
+  constexpr int kTokens = 256 / LANES;
+  const bool fours = NV >= 4 && s.num_logical % 4 == 0 && (uintptr_t)logits % (4 * dtype_bytes(s.in_dtype)) == 0;
+  return in_launches(T, max_blocks(256) * kTokens, [&](int64_t first, int64_t n) {
+    const dim3 grid((unsigned)((n + kTokens - 1) / kTokens)), block(256);
+    if constexpr (NV >= 4) {
+      if (fours) {
+        hipLaunchKernelGGL((k_route<BF16, LANES, NV, true>), grid, block, 0, st, logits, topk_idx, topk_w, s.num_logical,
+                           s.topk, s.over_all, first, first + n);
+        return hipGetLastError();
+      }
+    }
+    hipLaunchKernelGGL((k_route<BF16, LANES, NV, false>), grid, block, 0, st, logits, topk_idx, topk_w, s.num_logical, s.topk,
+                       s.over_all, first, first + n);
+    return hipGetLastError();
+  });
 }
 
 template <bool BF16>
 hipError_t launch_route(const eep_router_shape& s, const void* logits, int32_t* topk_idx, float* topk_w, int T,
                         hipStream_t st) {
-  return in_launches(T, max_blocks(256) * 4, [&](int64_t first, int64_t n) {
-    const dim3 grid((unsigned)((n + 3) / 4)), block(256);
-#define EEP_ROUTE(NV)                                                                                            \
-  if (s.num_logical <= 64 * NV) {                                                                                \
-    hipLaunchKernelGGL((k_route<BF16, NV>), grid, block, 0, st, logits, topk_idx, topk_w, s.num_logical, s.topk, \
-                       s.over_all, first, first + n);                                                            \
-    return hipGetLastError();                                                                                    \
+#define EEP_ROUTE(LANES, NV) \
+  if (s.num_logical <= LANES * NV && s.topk <= LANES) return launch_route<BF16, LANES, NV>(s, logits, topk_idx, topk_w, T, st);
+  if (T >= kRouteShared) {
+    EEP_ROUTE(16, 4) EEP_ROUTE(16, 8) EEP_ROUTE(16, 16)
   }
-    EEP_ROUTE(1) EEP_ROUTE(2) EEP_ROUTE(4) EEP_ROUTE(8) EEP_ROUTE(16) EEP_ROUTE(64)
+  EEP_ROUTE(64, 1) EEP_ROUTE(64, 2) EEP_ROUTE(64, 4) EEP_ROUTE(64, 8) EEP_ROUTE(64, 16) EEP_ROUTE(64, 64)
 #undef EEP_ROUTE
-    return hipErrorInvalidValue;
-  });
+  return hipErrorInvalidValue;
 }
 
 bool f32_or_bf16(int dtype) { return dtype == EEP_F32 || dtype == EEP_BF16; }

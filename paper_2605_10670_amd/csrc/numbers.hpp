@@ -33,6 +33,27 @@ __device__ __forceinline__ uint32_t group_max(uint32_t v, int n) {
   return v;
 }
 
+// One of 16 (a row of lanes) or all 64 lanes' values, in every lane: op joins two, in any order.
+template <int LANES, class T, class Op>
+__device__ __forceinline__ T fold(T v, Op op) {
+  static_assert(sizeof(T) == 4 && (LANES == 16 || LANES == 64), "");
+  const auto bits = [&]() { return __builtin_bit_cast(uint32_t, v); };
+  const auto join = [&](uint32_t other) { v = op(v, __builtin_bit_cast(T, other)); };
+  join(__builtin_amdgcn_update_dpp(0u, bits(), 0xB1, 0xf, 0xf, false));   // lane ^ 1
+  join(__builtin_amdgcn_update_dpp(0u, bits(), 0x4E, 0xf, 0xf, false));   // lane ^ 2
+  join(__builtin_amdgcn_update_dpp(0u, bits(), 0x141, 0xf, 0xf, false));  // half row mirrored
+  join(__builtin_amdgcn_update_dpp(0u, bits(), 0x140, 0xf, 0xf, false));  // row mirrored
+  if constexpr (LANES == 64) {
+    const auto rows = __builtin_amdgcn_permlane16_swap(bits(), bits(), false, false);  // both of a pair of rows
+    const uint32_t even = rows[0], odd = rows[1];
+    v = op(__builtin_bit_cast(T, even), __builtin_bit_cast(T, odd));
+    const auto halves = __builtin_amdgcn_permlane32_swap(bits(), bits(), false, false);
+    const uint32_t low = halves[0], high = halves[1];
+    v = op(__builtin_bit_cast(T, low), __builtin_bit_cast(T, high));
+  }
+  return v;
+}
+
 // The largest magnitude of N fp32 values as its bits, which are ordered as the values are, NaN above everything.
 template <int N>
 __device__ __forceinline__ uint32_t top_magnitude(const float (&v)[N]) {

@@ -60,25 +60,26 @@ def load():
 
 
 def _call(*args):
-    """native/marshal.cpp's call_ten, which binding's first call loads (and builds if it is not there)."""
+    """native/marshal.cpp's call_sized, which binding's first call loads (and builds if it is not there)."""
     global _call
     try:
         binding._call(None)  # loads the module; no entry point's call
     except TypeError:
         pass
     from . import _marshal
-    _call = _marshal.call_ten
+    _call = _marshal.call_sized
     return _call(*args)
+
+
+def _refuse(rc, name, arguments):
+    """What a return code other than OK means; arguments: the entry point's, by name."""
+    if rc <= -1000:
+        raise ValueError(f"{name}: {arguments[-1000 - rc]} is smaller than what the call reads or writes")
+    raise binding.EepError(rc, name)
 
 
 def _dtype(name):
     return DTYPES[name] if isinstance(name, str) else name
-
-
-def _holds(name, t, nbytes):
-    """Refuses a tensor that is too small for what the call reads or writes."""
-    if t is not None and not isinstance(t, int) and t.nbytes < nbytes:
-        raise ValueError(f"{name} has {t.nbytes} bytes, the call needs {nbytes}")
 
 
 class Norm:
@@ -89,22 +90,16 @@ class Norm:
         self._shape = _NormShape(hidden, _dtype(in_dtype), _dtype(gain_dtype), _dtype(out_dtype), scale_group, epsilon)
         self._at = ctypes.addressof(self._shape)
         s = self._shape
-        self._in, self._out = hidden * _BYTES.get(s.in_dtype, 1), hidden * _BYTES.get(s.out_dtype, 1)
-        self._gain, self._hidden = hidden * _BYTES.get(s.gain_dtype, 1), hidden
-        self._scales = 4 * (hidden // scale_group) if scale_group else 0
+        size = lambda dtype: hidden * _BYTES.get(dtype, 1)
+        # bytes a row, of gain in all
+        self._needs = (size(s.in_dtype), size(s.in_dtype), -size(s.gain_dtype), size(s.in_dtype), size(s.out_dtype), hidden,
+                       4 * (hidden // scale_group) if scale_group else 0)
 
     def run(self, x, gain, T, *, residual=None, sum=None, y=None, code=None, code_scale=None, stream=None):
-        _holds("x", x, T * self._in)
-        _holds("gain", gain, self._gain)
-        _holds("residual", residual, T * self._in)
-        _holds("sum", sum, T * self._in)
-        _holds("y", y, T * self._out)
-        _holds("code", code, T * self._hidden)
-        _holds("code_scale", code_scale, T * self._scales)
-        rc = _call(_address["eep_residual_norm"], "hpppppppis", self._at, x, residual, gain, sum, y, code, code_scale, T,
-                   stream)
-        if rc != binding.OK:
-            raise binding.EepError(rc, "eep_residual_norm")
+        rc = _call(_address["eep_residual_norm"], "hpppppppis", self._needs, T, self._at, x, residual, gain, sum, y, code,
+                   code_scale, T, stream)
+        if rc:
+            _refuse(rc, "eep_residual_norm", ("shape", "x", "residual", "gain", "sum", "y", "code", "code_scale"))
 
 
 class Router:
@@ -114,15 +109,12 @@ class Router:
         load()
         self._shape = _RouterShape(num_logical, topk, _dtype(in_dtype), 1 if over_all else 0)
         self._at = ctypes.addressof(self._shape)
-        self._in, self._k = num_logical * _BYTES.get(self._shape.in_dtype, 1), topk
+        self._needs = (num_logical * _BYTES.get(self._shape.in_dtype, 1), 4 * topk, 4 * topk)
 
     def run(self, logits, topk_idx, topk_w, T, stream=None):
-        _holds("logits", logits, T * self._in)
-        _holds("topk_idx", topk_idx, 4 * T * self._k)
-        _holds("topk_w", topk_w, 4 * T * self._k)
-        rc = _call(_address["eep_route"], "hpppis", self._at, logits, topk_idx, topk_w, T, stream)
-        if rc != binding.OK:
-            raise binding.EepError(rc, "eep_route")
+        rc = _call(_address["eep_route"], "hpppis", self._needs, T, self._at, logits, topk_idx, topk_w, T, stream)
+        if rc:
+            _refuse(rc, "eep_route", ("shape", "logits", "topk_idx", "topk_w"))
 
 
 class ExpertProduct:
@@ -139,26 +131,19 @@ class ExpertProduct:
         if rc != binding.OK:
             raise binding.EepError(rc, "eep_product_create")
         n = out_features * (2 if gate else 1)
-        self._x, self._y = in_features * _BYTES[c.x_dtype], out_features * _BYTES[c.y_dtype]
-        weights = n * self._x
-        self._w = (num_slots - 1) * (slot_stride or weights) + weights
-        blocks = 4 * -(-n // SCALE_BLOCK) * (in_features // SCALE_BLOCK)
-        self._w_scale = (num_slots - 1) * (scale_stride or blocks) + blocks
-        self._x_scale, self._y_scale = 4 * (in_features // SCALE_BLOCK), 4 * (out_features // SCALE_BLOCK)
-        self._offset = 4 * (num_slots + 1)
+        weights = n * in_features * _BYTES[c.x_dtype]
+        scales = 4 * -(-n // SCALE_BLOCK) * (in_features // SCALE_BLOCK)
+        whole = lambda stride, last: -((num_slots - 1) * (stride or last) + last)
+        # bytes a row, of the slots' arrays in all
+        self._needs = (in_features * _BYTES[c.x_dtype], 4 * (in_features // SCALE_BLOCK), whole(slot_stride, weights),
+                       whole(scale_stride, scales), -4 * (num_slots + 1), out_features * _BYTES[c.y_dtype],
+                       4 * (out_features // SCALE_BLOCK))
 
     def run(self, x, w, y, rows, *, offset=None, x_scale=None, w_scale=None, y_scale=None, stream=None):
-        _holds("x", x, rows * self._x)
-        _holds("w", w, self._w)
-        _holds("y", y, rows * self._y)
-        _holds("offset", offset, self._offset)
-        _holds("x_scale", x_scale, rows * self._x_scale)
-        _holds("w_scale", w_scale, self._w_scale)
-        _holds("y_scale", y_scale, rows * self._y_scale)
-        rc = _call(_address["eep_expert_product"], "hpppppppis", self._h.value or 0, x, x_scale, w, w_scale, offset, y,
-                   y_scale, rows, stream)
-        if rc != binding.OK:
-            raise binding.EepError(rc, "eep_expert_product")
+        rc = _call(_address["eep_expert_product"], "hpppppppis", self._needs, rows, self._h.value or 0, x, x_scale, w,
+                   w_scale, offset, y, y_scale, rows, stream)
+        if rc:
+            _refuse(rc, "eep_expert_product", ("product", "x", "x_scale", "w", "w_scale", "offset", "y", "y_scale"))
 
     def destroy(self):
         if self._h:

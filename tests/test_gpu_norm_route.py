@@ -128,22 +128,19 @@ def test_outputs_that_are_not_asked_for():
 
 # ---- router ------------------------------------------------------------------------------------
 def exact_route(logits, k, over_all):
-    v = logits.double()
-    v = torch.where(v.isnan(), -math.inf, v)
-    T, E = v.shape
-    idx, w = torch.full((T, k), -1), torch.zeros((T, k), dtype=torch.float64)
-    for t in range(T):
-        row = v[t].tolist()
-        order = sorted((e for e in range(E) if row[e] != -math.inf), key=lambda e: (-row[e], e))
-        chosen = order[:k]
-        if not chosen:
-            continue
-        top = row[chosen[0]]
-        ex = lambda e: 1.0 if row[e] == top else math.exp(row[e] - top)
-        total = sum(ex(e) for e in (order if over_all else chosen))
-        for j, e in enumerate(chosen):
-            idx[t, j], w[t, j] = e, ex(e) / total
-    return idx.to(torch.int32), w
+    v = logits.double().numpy()
+    v = np.where(np.isnan(v), -np.inf, v)
+    order = np.argsort(-v, axis=1, kind="stable")[:, :k]          # equal ones stay in ascending order of their index
+    value = np.take_along_axis(v, order, axis=1)
+    top = value[:, :1]
+
+    def ex(a):
+        with np.errstate(invalid="ignore"):
+            return np.where(a == -np.inf, 0.0, np.where(a == top, 1.0, np.exp(a - top)))
+    total = ex(v if over_all else value).sum(axis=1, keepdims=True)
+    chosen = value > -np.inf
+    w = np.divide(ex(value), total, out=np.zeros_like(value), where=chosen)
+    return torch.from_numpy(np.where(chosen, order, -1).astype(np.int32)), torch.from_numpy(w)
 
 
 def run_route(logits, k, over_all=False, dtype="f32"):
@@ -172,6 +169,18 @@ def check_route(logits, k, over_all=False, dtype="f32"):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_route(T, E, k, over_all, dtype):
     check_route(lu.randn(lu.gen(E + k), T, E) * 2, k, over_all, dtype)
+
+
+@pytest.mark.parametrize("E,k", [(16, 4), (60, 6), (96, 16), (97, 8), (128, 32), (256, 8)])
+@pytest.mark.parametrize("dtype,over_all", [("f32", False), ("bf16", True)])
+def test_many_tokens(E, k, dtype, over_all):
+    """Enough of them that several share a wavefront, the last one not full; ties among them, blocked logits and empty rows."""
+    T = 8195
+    logits = lu.randn(lu.gen(E), T, E)
+    logits[::7] = torch.randint(-1, 2, (len(logits[::7]), E), generator=lu.gen(1)).float()
+    logits[::11, E // 2:] = -math.inf
+    logits[::13] = math.nan
+    check_route(logits, k, over_all, dtype)
 
 
 def test_ties_go_to_the_lower_index():
