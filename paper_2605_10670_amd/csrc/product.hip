@@ -83,8 +83,8 @@ __device__ __forceinline__ f32x4 mma(const Frag& a, const Frag& b, f32x4 acc) {
 // Codes are multiplied as bf16, of which the matrix cores keep every product: their 8-bit forms line the products of
 // 8 neighbouring k up with the largest of them and keep 13 bits below its first (measured with single products
 // beside a large one; across the eights nothing is lost).  On normally distributed rows a sum of 128 then is
-// 1.3e-5 off (2-norm), and 5.4e-5 with wider ones; as bf16 1e-8 and 7e-8.  Only where the matrix cores are the bound and
-// the result is rounded to 16 or 8 bits are the 8-bit forms used (Operand).
+// 1.3e-5 off (2-norm), and 5.4e-5 with wider ones; as bf16 1e-8 and 7e-8.  Only the tiles' kernel, whose bound the matrix
+// cores are, uses the 8-bit forms, and only for results that are rounded to bf16 (Operand, widens).
 //
 // One block of 128: p[m] + w[m] * x.
 template <int M>
@@ -140,8 +140,8 @@ __device__ __forceinline__ void stream(int begin, int end, Load load, Multiply m
     if (s + u + AHEAD < end) multiply(u);
 }
 
-// An operand of mma, ready to be used several times.  WIDE: e4m3 codes are widened to bf16 (once), see above; else they are
-// multiplied as they are, where the sums are rounded to 16 or 8 bits anyway.
+// An operand, ready to be used several times.  WIDE: e4m3 codes are widened to bf16 (once), see above; else they are
+// multiplied as they are.
 template <int DT, bool WIDE>
 struct Operand {
   Frag f;
@@ -549,9 +549,8 @@ __global__ __launch_bounds__(64 * kThinWaves, few_alone(M, TN) ? 2 : 4) void k_p
 // ---------------------------------------------------------------------------
 // many rows a slot: tiles through LDS.
 //
-// A workgroup of 8 wavefronts has 256 weight rows (with the gate 128 of each factor) by 64 * TT tokens; two wavefronts share
-// the weight rows, four the tokens, so that one holds 128 by 16 * TT sums and reads 128 + 16 * TT rows of a step for
-// them.  A step's rows go from memory to LDS without passing through registers, STAGES - 1 steps ahead; a row's eight
+// A workgroup of 8 wavefronts has 256 weight rows (with the gate 128 of each factor) by 64 * TT tokens; of these a wavefront
+// holds the sums of 128 by 64, 64 by 64 or 64 by 32, near a square, so that it reads few rows of a step for them.  A step's rows go from memory to LDS without passing through registers, STAGES - 1 steps ahead; a row's eight
 // 16-byte chunks lie in LDS at their number XOR the row's, so that the 16 rows of a tile are read without bank
 // conflicts although each begins at the same bank.
 //
@@ -561,6 +560,7 @@ __global__ __launch_bounds__(64 * kThinWaves, few_alone(M, TN) ? 2 : 4) void k_p
 // ---------------------------------------------------------------------------
 constexpr int kTiledWaves = 8, kTiledRows = 256;
 constexpr int kTiledThreads = 64 * kTiledWaves;
+__host__ __device__ constexpr int tiled_across(int tt) { return tt == 4 ? 2 : 4; }  // wavefronts side by side on the weight rows
 __host__ __device__ constexpr int tiled_stages(int tt) { return tt == 4 ? 2 : 3; }
 // Codes' scales come four steps at a time: a token's side by side, behind them those of two blocks of weight rows.
 constexpr int kScaleSteps = 4, kScaleBuffers = 3;
@@ -568,7 +568,7 @@ constexpr int kWeightStage = kTiledRows * kStepBytes;
 __host__ __device__ constexpr int tiled_scale_bytes(int tt) { return 64 * tt * kScaleSteps * 4 + 256; }
 __host__ __device__ constexpr int tiled_lds_bytes(bool codes, int tt) {
   return tiled_stages(tt) * (kWeightStage + 64 * tt * kStepBytes) +
-         (codes ? kScaleBuffers * tiled_scale_bytes(tt) : 0) + 2 * 64 * tt * 4;
+         (codes ? kScaleBuffers * tiled_scale_bytes(tt) : 0) + tiled_across(tt) * 64 * tt * 4;
 }
 
 typedef __attribute__((address_space(3))) void lds_void;
@@ -659,6 +659,8 @@ struct TileMap {
 
 template <int DT, bool WIDE, int YT, bool GATE, int TT>
 __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs a) {
+  constexpr int kWM = tiled_across(TT), kWN = kTiledWaves / kWM;
+  constexpr int kA = kTiledRows / 16 / kWM, kB = 4 * TT / kWN;  // tiles of 16 weight rows and of 16 tokens a wavefront
   constexpr int kStages = tiled_stages(TT), kTokens = 64 * TT;
   constexpr bool kCodes = DT == EEP_FP8_E4M3;
   constexpr int kXStage = kTokens * kStepBytes, kScaleBytes = tiled_scale_bytes(TT);
@@ -668,11 +670,11 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
   extern __shared__ __align__(1024) uint8_t lds[];
   uint8_t* const x_lds = lds + kStages * kWeightStage;
   uint8_t* const scale_lds = x_lds + kStages * kXStage;
-  uint32_t* s_top = (uint32_t*)(scale_lds + (kCodes ? kScaleBuffers * kScaleBytes : 0));  // [2][kTokens]
+  uint32_t* s_top = (uint32_t*)(scale_lds + (kCodes ? kScaleBuffers * kScaleBytes : 0));  // [kWM][kTokens]
 
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wm = wave & 1, wn = wave >> 1;
+  const int wm = wave % kWM, wn = wave / kWM;
   const int col = lane & 15, part = lane >> 4;
 
   TileMap<kTokens> map;
@@ -807,8 +809,8 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
   }
 
   // What a step begins with: the tokens' rows, the first weight rows, the scales; read while the step before ends.
-  Frag b_raw[TT], a_raw;
-  [[maybe_unused]] float token_scale[TT], row_scale[2];
+  Frag b_raw[kB], a_raw;
+  [[maybe_unused]] float token_scale[kB], row_scale[2];
   uint8_t *stage = lds, *x_stage = x_lds;  // of the step
   auto read = [&](const uint8_t* from_lds, int tile_row) {
     Frag f;
@@ -817,14 +819,14 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
     return f;
   };
   auto row_of_tile = [&](int f) {
-    return GATE ? (f < 4 ? wm * 64 + f * 16 : 128 + wm * 64 + (f - 4) * 16) : wm * 128 + f * 16;
+    return GATE ? f / (kA / 2) * 128 + wm * (128 / kWM) + f % (kA / 2) * 16 : wm * (256 / kWM) + f * 16;
   };
   auto read_scales = [&](int s) {
     if constexpr (kCodes) {
       const float* scales = (const float*)chunk + (s & 3);
 #pragma unroll
-      for (int j = 0; j < TT; ++j) token_scale[j] = scales[((wn * TT + j) * 16 + col) * 4];
-      row_scale[0] = scales[kTokens * 4 + (GATE ? 0 : wm * 4)];
+      for (int j = 0; j < kB; ++j) token_scale[j] = scales[((wn * kB + j) * 16 + col) * 4];
+      row_scale[0] = scales[kTokens * 4 + (GATE ? 0 : wm / (kWM / 2) * 4)];
       if constexpr (GATE) row_scale[1] = scales[kTokens * 4 + 4];
     }
   };
@@ -833,15 +835,15 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
   asm volatile("" ::: "memory");
   read_scales(0);
 #pragma unroll
-  for (int j = 0; j < TT; ++j) b_raw[j] = read(x_stage, (wn * TT + j) * 16);
+  for (int j = 0; j < kB; ++j) b_raw[j] = read(x_stage, (wn * kB + j) * 16);
   a_raw = read(stage, row_of_tile(0));
 
   for (;;) {
-    f32x4 acc[8][TT];
+    f32x4 acc[kA][kB];
 #pragma unroll
-    for (int f = 0; f < 8; ++f)
+    for (int f = 0; f < kA; ++f)
 #pragma unroll
-      for (int j = 0; j < TT; ++j) acc[f][j] = f32x4{0, 0, 0, 0};
+      for (int j = 0; j < kB; ++j) acc[f][j] = f32x4{0, 0, 0, 0};
 
     auto step = [&](int s, auto is_cut) {
       constexpr bool kCut = decltype(is_cut)::value;  // the last step of rows that end within it
@@ -855,13 +857,13 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
         o.set(f);
         return o;
       };
-      Operand<DT, WIDE> b[TT];
+      Operand<DT, WIDE> b[kB];
 #pragma unroll
-      for (int j = 0; j < TT; ++j) b[j] = ready(b_raw[j]);
-      [[maybe_unused]] float scale[GATE ? 2 : 1][TT];
+      for (int j = 0; j < kB; ++j) b[j] = ready(b_raw[j]);
+      [[maybe_unused]] float scale[GATE ? 2 : 1][kB];
       if constexpr (kCodes) {
 #pragma unroll
-        for (int j = 0; j < TT; ++j) {
+        for (int j = 0; j < kB; ++j) {
           scale[0][j] = token_scale[j] * row_scale[0];
           if constexpr (GATE) scale[1][j] = token_scale[j] * row_scale[1];
         }
@@ -869,15 +871,16 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
       // codes: the block's sums of a tile are multiplied by the scales and added while the next ones are multiplied
       constexpr int kBehind = 2;
       [[maybe_unused]] f32x4 block[kBehind + 1];
-      // the i-th tile: 6 times the tokens, then the last two side by side
-      auto tile_f = [](int i) { return i < 6 * TT ? i / TT : 6 + (i & 1); };
-      auto tile_j = [](int i) { return i < 6 * TT ? i % TT : (i - 6 * TT) / 2; };
+      // the i-th tile: weight rows by weight rows, then the last two of them side by side
+      constexpr int kPairs = (kA - 2) * kB;
+      auto tile_f = [](int i) { return i < kPairs ? i / kB : kA - 2 + (i & 1); };
+      auto tile_j = [](int i) { return i < kPairs ? i % kB : (i - kPairs) / 2; };
       auto add_block = [&](int i) {
         if constexpr (kCodes) {
           const int f = tile_f(i), j = tile_j(i);
 #pragma unroll
           for (int n = 0; n < 4; ++n)
-            acc[f][j][n] = fmaf(block[i % (kBehind + 1)][n], scale[GATE ? f / 4 : 0][j], acc[f][j][n]);
+            acc[f][j][n] = fmaf(block[i % (kBehind + 1)][n], scale[GATE ? f / (kA / 2) : 0][j], acc[f][j][n]);
         }
       };
       auto multiply = [&](int i, const Operand<DT, WIDE>& av) {
@@ -892,11 +895,11 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
       };
       Operand<DT, WIDE> last[2];
 #pragma unroll
-      for (int f = 0; f < 6; ++f) {
+      for (int f = 0; f < kA - 2; ++f) {
         const Operand<DT, WIDE> av = ready(a_raw);
         a_raw = read(stage, row_of_tile(f + 1));
 #pragma unroll
-        for (int j = 0; j < TT; ++j) multiply(f * TT + j, av);
+        for (int j = 0; j < kB; ++j) multiply(f * kB + j, av);
         if constexpr (!kCodes) __builtin_amdgcn_sched_barrier(0);
         if (kEarly && f == 2) {
           // All wavefronts have their tokens' rows in registers (only the two reads of the next weight rows may be under
@@ -908,7 +911,7 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
         }
       }
       last[0] = ready(a_raw);
-      last[1] = ready(read(stage, row_of_tile(7)));
+      last[1] = ready(read(stage, row_of_tile(kA - 1)));
       // This wavefront has read all it needs of the stage.  Once all have, and the next step's rows are there (no more than
       // the fetches behind them are under way), the stage may be filled again and the next step's first operands are read.
       asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kEarly ? kXLoads : (kStages - 2) * (kWeightLoads + kXLoads)) : "memory");
@@ -920,10 +923,10 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
       uint8_t* x_following = x_stage + kXStage < x_lds + kStages * kXStage ? x_stage + kXStage : x_lds;
       a_raw = read(following, row_of_tile(0));
 #pragma unroll
-      for (int j = 0; j < TT; ++j) {
-        multiply(6 * TT + 2 * j, last[0]);
-        multiply(6 * TT + 2 * j + 1, last[1]);
-        b_raw[j] = read(x_following, (wn * TT + j) * 16);
+      for (int j = 0; j < kB; ++j) {
+        multiply(kPairs + 2 * j, last[0]);
+        multiply(kPairs + 2 * j + 1, last[1]);
+        b_raw[j] = read(x_following, (wn * kB + j) * 16);
         if constexpr (!kCodes) __builtin_amdgcn_sched_barrier(0);
       }
       const int upcoming = s + 1 < steps ? s + 1 : 0;
@@ -931,7 +934,7 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
       read_scales(upcoming);
       if constexpr (kCodes) {
 #pragma unroll
-        for (int i = 8 * TT - kBehind; i < 8 * TT; ++i) add_block(i);
+        for (int i = kA * kB - kBehind; i < kA * kB; ++i) add_block(i);
       }
       stage = following;
       x_stage = x_following;
@@ -948,39 +951,40 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
     }
 
     if constexpr (GATE) {
-      const int n0 = t.feature_tile * 128 + wm * 64 + part * 4;
-      uint32_t top[TT];
+      const int n0 = t.feature_tile * 128 + wm * (128 / kWM) + part * 4;
+      uint32_t top[kB];
 #pragma unroll
-      for (int j = 0; j < TT; ++j) {
+      for (int j = 0; j < kB; ++j) {
         top[j] = 0;
 #pragma unroll
-        for (int f = 0; f < 4; ++f) {
+        for (int f = 0; f < kA / 2; ++f) {
           float v[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) acc[f][j][i] = v[i] = silu_times(acc[f][j][i], acc[f + 4][j][i]);
+          for (int i = 0; i < 4; ++i) acc[f][j][i] = v[i] = silu_times(acc[f][j][i], acc[f + kA / 2][j][i]);
           const uint32_t m = top_magnitude<4>(v);
           top[j] = m > top[j] ? m : top[j];
         }
       }
       if constexpr (YT == EEP_FP8_E4M3) {
 #pragma unroll
-        for (int j = 0; j < TT; ++j) {
+        for (int j = 0; j < kB; ++j) {
           top[j] = max(top[j], (uint32_t)__shfl_xor((int)top[j], 16, 64));
           top[j] = max(top[j], (uint32_t)__shfl_xor((int)top[j], 32, 64));
-          if (part == 0) s_top[wm * kTokens + (wn * TT + j) * 16 + col] = top[j];
+          if (part == 0) s_top[wm * kTokens + (wn * kB + j) * 16 + col] = top[j];
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
 #pragma unroll
-        for (int j = 0; j < TT; ++j) {
-          const int at = (wn * TT + j) * 16 + col;
-          const uint32_t other = s_top[(wm ^ 1) * kTokens + at];
-          const float scale = scale_of(max(top[j], other));
+        for (int j = 0; j < kB; ++j) {
+          const int at = (wn * kB + j) * 16 + col;
+#pragma unroll
+          for (int w = 0; w < kWM; ++w) top[j] = max(top[j], s_top[w * kTokens + at]);
+          const float scale = scale_of(top[j]);
           const int64_t row = t.first + at;
           if (row < t.end) {
 #pragma unroll
-            for (int f = 0; f < 4; ++f)
+            for (int f = 0; f < kA / 2; ++f)
               *(uint32_t*)(a.y + row * a.features + n0 + f * 16) =
                   codes4(acc[f][j][0], acc[f][j][1], acc[f][j][2], acc[f][j][3], scale);
             if (wm == 0 && part == 0) a.y_scale[row * a.feature_tiles + t.feature_tile] = scale;
@@ -988,22 +992,22 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
         }
       } else {
 #pragma unroll
-        for (int j = 0; j < TT; ++j) {
-          const int64_t row = t.first + (wn * TT + j) * 16 + col;
+        for (int j = 0; j < kB; ++j) {
+          const int64_t row = t.first + (wn * kB + j) * 16 + col;
 #pragma unroll
-          for (int f = 0; f < 4; ++f) {
+          for (int f = 0; f < kA / 2; ++f) {
             const float v[4] = {acc[f][j][0], acc[f][j][1], acc[f][j][2], acc[f][j][3]};
             if (row < t.end && n0 + f * 16 < a.features) store4<YT>(a.y, row * a.features + n0 + f * 16, v);
           }
         }
       }
     } else {
-      const int n0 = t.feature_tile * 256 + wm * 128 + part * 4;
+      const int n0 = t.feature_tile * 256 + wm * (256 / kWM) + part * 4;
 #pragma unroll
-      for (int j = 0; j < TT; ++j) {
-        const int64_t row = t.first + (wn * TT + j) * 16 + col;
+      for (int j = 0; j < kB; ++j) {
+        const int64_t row = t.first + (wn * kB + j) * 16 + col;
 #pragma unroll
-        for (int f = 0; f < 8; ++f) {
+        for (int f = 0; f < kA; ++f) {
           const float v[4] = {acc[f][j][0], acc[f][j][1], acc[f][j][2], acc[f][j][3]};
           if (row < t.end && n0 + f * 16 < a.features) store4<YT>(a.y, row * a.features + n0 + f * 16, v);
         }
@@ -1049,9 +1053,12 @@ bool launch_few(const eep_product& p, ProductArgs a, hipStream_t st, hipError_t*
   return true;
 }
 
+// Are codes widened (see widen)?  Where the result keeps more than 8 bits of significand: fp32, and the fp32 scales of codes.
+constexpr bool widens(int dt, int yt) { return dt == EEP_FP8_E4M3 && yt != EEP_BF16; }
+
 template <int DT, int YT, bool GATE, int TT>
 hipError_t launch_tiled(ProductArgs a, int cus, hipStream_t st) {
-  constexpr bool kWide = DT == EEP_FP8_E4M3 && YT == EEP_F32;
+  constexpr bool kWide = widens(DT, YT);
   constexpr int kLds = tiled_lds_bytes(DT == EEP_FP8_E4M3, TT);
   const auto kernel = k_product_tiled<DT, kWide, YT, GATE, TT>;
   static const hipError_t allowed =
@@ -1075,10 +1082,11 @@ float tiled_cost(int tt, int rows, int slots, int64_t feature_tiles, int cus) {
   return step * (rounds < 4.0f ? ceilf(rounds) : rounds);
 }
 
-// Rows a slot up to which the thin kernel is chosen.  Thin / tiles of 64 tokens, us: 32 tokens of 288 slots 2048 -> 7168 fp8
-// to fp32 (0.9 rows a slot) 405 / 510, 7168 -> 2 x 2048 822 / 802; 64 tokens (1.8) 1178 / 1146, 144 slots bf16 4096 ->
-// 2 x 1024 (3.6) 464 / 410; 256 tokens (7.1) 1480 / 1353; 512 (14.2: many slots have more than 16) 1986 / 1362.
-constexpr int kThinMean = 1;
+// Rows a slot up to which the thin kernel is chosen: about one; more where the tiles' kernel has codes to widen, which there takes
+// the time of the products themselves.  Thin / tiles of 64 tokens, us: 144 slots bf16 4096 -> 2 x 1024, 64 tokens (3.6 rows
+// a slot) 464 / 410, 200 tokens (11) 477 / 417; 288 slots 7168 -> 2 x 2048 fp8 to codes, 256 tokens (7.1) 1455 / 1529, 512 tokens
+// (14.2, where many slots have more than 16 and are read twice) 1986 / 1539; 2048 -> 7168 to fp32, 32 tokens (0.9) 405 / 510.
+constexpr int thin_mean(bool wide) { return wide ? 8 : 1; }
 
 template <int DT, int YT, bool GATE>
 hipError_t launch_product(const eep_product& p, const ProductArgs& a, hipStream_t st) {
@@ -1094,8 +1102,8 @@ hipError_t launch_product(const eep_product& p, const ProductArgs& a, hipStream_
     if (launch_few<DT, YT, GATE, 1, 4>(p, a, st, &e) || launch_few<DT, YT, GATE, 2, 4>(p, a, st, &e)) return e;
   }
   // (the tiles' stream is as long as three steps at least)
-  if (mean <= kThinMean || a.row_bytes <= 2 * kStepBytes) return launch_thin<DT, YT, GATE>(a, st);
-  constexpr bool kLarge = DT != EEP_FP8_E4M3 || YT != EEP_F32;  // (widened codes take twice the registers)
+  if (mean <= thin_mean(widens(DT, YT)) || a.row_bytes <= 2 * kStepBytes) return launch_thin<DT, YT, GATE>(a, st);
+  constexpr bool kLarge = !widens(DT, YT);  // (widened codes take twice the registers)
   const int64_t feature_tiles = (a.features + kTiledRows / (GATE ? 2 : 1) - 1) / (kTiledRows / (GATE ? 2 : 1));
   auto cost = [&](int tt) { return tiled_cost(tt, a.rows, a.slots, feature_tiles, p.cus); };
   const float one = cost(1), two = cost(2), four = cost(4);

@@ -118,7 +118,7 @@ def lost_by_alignment(c):
 def result(c, y):
     """(the product in 64 bits, what it may be off before it is rounded to y)."""
     N, s, e = c["N"], c["sums"], c["sum_err"]
-    if c["xt"] == "fp8" and y != "f32":
+    if c["xt"] == "fp8" and y == "bf16":
         e = e + lost_by_alignment(c)
     if not c["gate"]:
         return s, e
