@@ -167,7 +167,8 @@ hipError_t launch_norm(const NormArgs& a, int T, hipStream_t st) {
 // The rounds are the bound, not memory.  At many tokens four share a wavefront (16 lanes, up to 16 logits each) and the
 // instructions of a round, whose exchanges stay within a row of lanes; at few, where a round's latency counts, and beyond
 // 256 logits a token has one for itself.  Measured, 256 logits, top-8, a token a wavefront / four, us: 32 tokens 4.1 / 6.0,
-// 4096 4.6 / 5.4, 8192 6.5 / 6.0, 16384 (bf16) 11.0 / 8.8; 128 logits, 16384 tokens 10.7 / 5.7.
+// 4096 4.6 / 5.4, 8192 6.5 / 6.0, 128 logits, 16384 tokens 10.7 / 5.7; 16384 tokens of 256 bf16 logits 11.0 / 8.7, with the index in the
+// value's free bits 6.9.
 // ---------------------------------------------------------------------------
 constexpr int kRouteMaxExperts = 4096;
 constexpr int kRouteShared = 8192;  // tokens from which four share a wavefront
@@ -183,6 +184,20 @@ __device__ __forceinline__ float value_of(uint32_t order) {
 }
 // exp(v - top) where top >= v, also where both are +infinity
 __device__ __forceinline__ float exp_below(float v, float top) { return v == top ? 1.0f : expf(v - top); }
+
+// What a round compares.  bf16 logits leave 16 bits for the index, the lower one above: no two are equal, and a round needs no
+// search for the first of them.  0: not to be chosen.
+template <bool BF16>
+__device__ __forceinline__ uint32_t key_of(float v, int index) {
+  const uint32_t o = order_of(v);
+  if constexpr (!BF16) return o;
+  return o != 0 ? (o & 0xffff0000u) | (0xffffu - (uint32_t)index) : 0;
+}
+template <bool BF16>
+__device__ __forceinline__ float value_of_key(uint32_t key) {
+  // (the bits that a negative value's order has below the bf16 are ones)
+  return value_of(BF16 ? (key & 0x80000000u ? key & 0xffff0000u : key | 0xffffu) : key);
+}
 
 // FOURS: four logits at a time, of rows that are whole fours and aligned to them.
 template <bool BF16, int LANES, int NV, bool FOURS>
@@ -210,7 +225,7 @@ __global__ __launch_bounds__(256) void k_route(const void* __restrict__ logits, 
         }
       }
 #pragma unroll
-      for (int j = 0; j < 4; ++j) o[i + j] = order_of(v[j]);
+      for (int j = 0; j < 4; ++j) o[i + j] = key_of<BF16>(v[j], e + j);
     }
   } else {
 #pragma unroll
@@ -218,8 +233,8 @@ __global__ __launch_bounds__(256) void k_route(const void* __restrict__ logits, 
       const int e = lane * NV + i;
       o[i] = 0;
       if (e < E)
-        o[i] = order_of(BF16 ? __uint_as_float((uint32_t)((const uint16_t*)logits)[t * E + e] << 16)
-                             : ((const float*)logits)[t * E + e]);
+        o[i] = key_of<BF16>(BF16 ? __uint_as_float((uint32_t)((const uint16_t*)logits)[t * E + e] << 16)
+                                 : ((const float*)logits)[t * E + e], e);
     }
   }
   uint32_t best = 0;
@@ -231,7 +246,7 @@ __global__ __launch_bounds__(256) void k_route(const void* __restrict__ logits, 
   float all = 0.0f;
   if (over_all != 0 && top != 0) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) all += o[i] != 0 ? exp_below(value_of(o[i]), value_of(top)) : 0.0f;
+    for (int i = 0; i < NV; ++i) all += o[i] != 0 ? exp_below(value_of_key<BF16>(o[i]), value_of_key<BF16>(top)) : 0.0f;
   }
   uint32_t largest = top;
   for (int j = 0; j < k; ++j) {
@@ -239,6 +254,17 @@ __global__ __launch_bounds__(256) void k_route(const void* __restrict__ logits, 
     if (lane == j) mine = largest;
     if (largest == 0) {
       if (lane == 0) topk_idx[t * k + j] = -1;
+      continue;
+    }
+    if constexpr (BF16) {
+      uint32_t next = 0;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        o[i] = o[i] == largest ? 0 : o[i];
+        next = larger(next, o[i]);
+      }
+      best = next;
+      if (lane == 0) topk_idx[t * k + j] = (int32_t)(0xffffu - (largest & 0xffffu));
       continue;
     }
     uint64_t have = __ballot(best == largest);
@@ -257,7 +283,7 @@ __global__ __launch_bounds__(256) void k_route(const void* __restrict__ logits, 
       topk_idx[t * k + j] = lane * NV + at;
     }
   }
-  const float e = mine != 0 ? exp_below(value_of(mine), value_of(top)) : 0.0f;
+  const float e = mine != 0 ? exp_below(value_of_key<BF16>(mine), value_of_key<BF16>(top)) : 0.0f;
   const float sum = lane_sum<LANES>(over_all != 0 ? all : e);
   if (lane < k) topk_w[t * k + lane] = mine != 0 ? e / sum : 0.0f;
 }
