@@ -219,3 +219,46 @@ def test_refusals_of_a_call():
         bf16.run(**{**one, "x": torch.zeros((15, 256), dtype=torch.bfloat16, device="cuda")})
     bf16.destroy()
     fp8.destroy()
+
+
+@pytest.mark.parametrize("rows,K,N,y", [(70000, 32768, 128, "f32"), (70000, 64, 16384, "f32")])
+def test_arrays_past_four_gigabytes(rows, K, N, y):
+    """x, then y, of 4.6 GB in 3 slots: the last rows of each slot against their definition."""
+    from paper_2605_10670_amd import layer
+    g = torch.Generator(device="cuda").manual_seed(30)
+    ends = [0, 33, 35000, rows]
+    x = torch.zeros((rows, K), dtype=torch.bfloat16, device="cuda")
+    out = torch.zeros((rows, N), device="cuda")
+    w = (torch.randn((3, N, K), generator=g, device="cuda") * K ** -0.5).bfloat16()
+    last = [list(range(e - 3, e)) for e in ends[1:]]
+    for picked in last:
+        x[picked] = torch.randn((3, K), generator=g, device="cuda").bfloat16()
+    p = layer.ExpertProduct(num_slots=3, in_features=K, out_features=N, y_dtype=y, max_rows=rows)
+    p.run(x, w, out, rows, offset=torch.tensor(ends, dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    for slot, picked in enumerate(last):
+        xd, wd = x[picked].cpu().double(), w[slot].cpu().double()
+        lu.check_rounded(out[picked].cpu(), xd @ wd.t(), (xd.abs() @ wd.abs().t()) * (K + 8) * 2.0 ** -23 + 2.0 ** -126)
+    p.destroy()
+
+
+@pytest.mark.parametrize("counts", [(2, 0, 3), (150, 1, 200)])
+def test_slots_far_apart(counts):
+    """A slot's weights begin past 4 GB of the store."""
+    from paper_2605_10670_amd import layer
+    c = lu.product_case(31, counts, 512, 128, "fp8", False)
+    stride = 2304 << 20
+    store = torch.empty(2 * stride + (1 << 20), dtype=torch.uint8, device="cuda")
+    size, scales = 512 * 128, 4 * 4
+    for s in range(3):
+        at = s * stride
+        store[at:at + size] = c["w"][s].view(torch.uint8).flatten().cuda()
+        store[at + size:at + size + scales] = c["w_scale"][s].contiguous().view(-1).view(torch.uint8).cuda()
+    y = torch.empty((c["rows"], 128), device="cuda")
+    p = layer.ExpertProduct(num_slots=3, in_features=512, out_features=128, x_dtype="fp8", y_dtype="f32", max_rows=c["rows"],
+                            slot_stride=stride, scale_stride=stride)
+    p.run(c["x"].cuda(), store.data_ptr(), y, c["rows"], offset=c["offset"].cuda(), x_scale=c["x_scale"].cuda(),
+          w_scale=store.data_ptr() + size)
+    torch.cuda.synchronize()
+    lu.check_product(c, "f32", y.cpu(), None)
+    p.destroy()
