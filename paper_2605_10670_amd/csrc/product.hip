@@ -247,6 +247,16 @@ __device__ __forceinline__ void store4(uint8_t* y, int64_t element, const float 
     *(u32x2*)(y + element * 2) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
 }
 
+// Two tiles of 16 features side by side, of which a lane has four neighbouring ones each, as bf16: rows of lanes exchange halves,
+// and each stores 16 bytes, so that a row of y gets 64 at once.  n: the first of the 32 features.
+__device__ __forceinline__ void store_tiles(uint8_t* y, int64_t row, int features, int n, int part, bool in_rows,
+                                            const f32x4& a, const f32x4& b) {
+  const auto low = __builtin_amdgcn_permlane16_swap(pack_bf16x2(a[0], a[1]), pack_bf16x2(b[0], b[1]), false, false);
+  const auto high = __builtin_amdgcn_permlane16_swap(pack_bf16x2(a[2], a[3]), pack_bf16x2(b[2], b[3]), false, false);
+  n += (part & 1) * 16 + (part >> 1) * 8;
+  if (in_rows && n < features) *(u32x4*)(y + (row * features + n) * 2) = u32x4{low[0], high[0], low[1], high[1]};
+}
+
 // ---------------------------------------------------------------------------
 // a row or so a slot: the weights go straight to registers.
 //
@@ -994,10 +1004,16 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
 #pragma unroll
         for (int j = 0; j < kB; ++j) {
           const int64_t row = t.first + (wn * kB + j) * 16 + col;
+          if constexpr (YT == EEP_BF16) {
 #pragma unroll
-          for (int f = 0; f < kA / 2; ++f) {
-            const float v[4] = {acc[f][j][0], acc[f][j][1], acc[f][j][2], acc[f][j][3]};
-            if (row < t.end && n0 + f * 16 < a.features) store4<YT>(a.y, row * a.features + n0 + f * 16, v);
+            for (int f = 0; f < kA / 2; f += 2)
+              store_tiles(a.y, row, a.features, n0 - part * 4 + f * 16, part, row < t.end, acc[f][j], acc[f + 1][j]);
+          } else {
+#pragma unroll
+            for (int f = 0; f < kA / 2; ++f) {
+              const float v[4] = {acc[f][j][0], acc[f][j][1], acc[f][j][2], acc[f][j][3]};
+              if (row < t.end && n0 + f * 16 < a.features) store4<YT>(a.y, row * a.features + n0 + f * 16, v);
+            }
           }
         }
       }
@@ -1006,10 +1022,16 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
 #pragma unroll
       for (int j = 0; j < kB; ++j) {
         const int64_t row = t.first + (wn * kB + j) * 16 + col;
+        if constexpr (YT == EEP_BF16) {
 #pragma unroll
-        for (int f = 0; f < kA; ++f) {
-          const float v[4] = {acc[f][j][0], acc[f][j][1], acc[f][j][2], acc[f][j][3]};
-          if (row < t.end && n0 + f * 16 < a.features) store4<YT>(a.y, row * a.features + n0 + f * 16, v);
+          for (int f = 0; f < kA; f += 2)
+            store_tiles(a.y, row, a.features, n0 - part * 4 + f * 16, part, row < t.end, acc[f][j], acc[f + 1][j]);
+        } else {
+#pragma unroll
+          for (int f = 0; f < kA; ++f) {
+            const float v[4] = {acc[f][j][0], acc[f][j][1], acc[f][j][2], acc[f][j][3]};
+            if (row < t.end && n0 + f * 16 < a.features) store4<YT>(a.y, row * a.features + n0 + f * 16, v);
+          }
         }
       }
     }
