@@ -262,7 +262,9 @@ __device__ __forceinline__ void store_tiles(uint8_t* y, int64_t row, int feature
 //
 // A workgroup of 8 wavefronts has 16 rows of one slot and 128 features of y with the gate, 256 without: each wavefront two
 // matrix-core tiles of 16 weight rows, with the gate the two factors of 16 features.  No weight is used by two
-// wavefronts, so nothing of them goes through LDS; the rows of x come from the caches.
+// wavefronts, so nothing of them goes through LDS; the rows of x come from the caches.  Bound by HBM: 16 tokens of 144 slots bf16
+// 4096 -> 2 x 1024 252 us (5.7 TB/s), 256 tokens of 288 slots fp8 7168 -> 2 x 2048 1.48 ms (5.7 TB/s); with loads two steps ahead and
+// one workgroup to a CU 255 us and 1.52 ms.
 // ---------------------------------------------------------------------------
 constexpr int kThinTokens = 16, kThinWaves = 8;
 template <int DT, int YT, bool GATE>
@@ -395,7 +397,9 @@ __global__ __launch_bounds__(64 * kThinWaves, 4) void k_product_thin(ProductArgs
 // The workgroup's 8 wavefronts divide in_features and add their sums up in LDS, in the order of the parts; with the gate a
 // tile's 16 rows are 8 of either factor.  Codes need the largest of 128 features, which are 16 tiles' here: each leaves
 // its values in memory, past the L2s, which do not see one another's writes, and the last to arrive makes the codes of
-// all.  (Its loads look past the caches one by one; a fence would empty them for everybody.)
+// all.  (Its loads look past the caches one by one; a fence would empty them for everybody.)  Bound by latency: one token through
+// 7168 -> 2 x 2048 fp8 to codes 12.2 us, of which the rows' trip and the sums are 7, the values' and the codes' 5; 2048 -> 7168
+// to bf16 6.7.  (In_features divided between workgroups instead, the last to arrive adding up: 15.0 and 9.9.)
 // ---------------------------------------------------------------------------
 constexpr int kFewGroups = 256;  // groups of 16 tokens by 128 features that the workspace holds
 
@@ -567,6 +571,14 @@ __global__ __launch_bounds__(64 * kThinWaves, few_alone(M, TN) ? 2 : 4) void k_p
 // The workgroups stay: each goes through its share of the work items, an item being a tile.  Workgroups of one XCD
 // (every eighth) have neighbouring items, those of one slot with the row tiles innermost: what runs at a time
 // shares weights and rows in that XCD's L2.
+//
+// Measured: 4096 tokens of 288 slots fp8 2048 -> 7168 to bf16 940 us (5.1 TB/s, 1.02 PFLOP/s: HBM and the stores of y), 4096 rows
+// through one such matrix 65 to 68 us (1.8 PFLOP/s), bf16 1408 -> 2880 to fp32, 35856 rows in 120 slots, 415 us (0.70 PFLOP/s, 3.5 TB/s),
+// 16384 tokens fp8 7168 -> 2 x 2048 to codes 8.1 ms (0.95 PFLOP/s).  The last is bound by instructions: a SIMD's matrix and vector
+// instructions take their times one after the other (two wavefronts of products with two vector instructions each ran
+// in the sum of both, not the larger), and a step of a wavefront has 64 products, 128 instructions that widen codes and
+// 64 that scale the sums.  With 8-bit products (and their error) it took 4.3 ms, there bound by the trip to LDS and a clock that
+// falls to 1.8 GHz.
 // ---------------------------------------------------------------------------
 constexpr int kTiledWaves = 8, kTiledRows = 256;
 constexpr int kTiledThreads = 64 * kTiledWaves;
@@ -1108,7 +1120,9 @@ float tiled_cost(int tt, int rows, int slots, int64_t feature_tiles, int cus) {
 // the time of the products themselves.  Thin / tiles of 64 tokens, us: 144 slots bf16 4096 -> 2 x 1024, 64 tokens (3.6 rows
 // a slot) 464 / 410, 200 tokens (11) 477 / 417; 288 slots 7168 -> 2 x 2048 fp8 to codes, 256 tokens (7.1) 1455 / 1529, 512 tokens
 // (14.2, where many slots have more than 16 and are read twice) 1986 / 1539; 2048 -> 7168 to fp32, 32 tokens (0.9) 405 / 510.
-constexpr int thin_mean(bool wide) { return wide ? 8 : 1; }
+// fp32 products take the matrix cores 16 times as long as bf16 ones, and tiles of 64 tokens are mostly empty there: 144 slots
+// 2048 -> 1024, 200 tokens (11 rows a slot) 291 / 389, 9 slots 4992 -> 4096, 76 rows 209 / 314.
+constexpr int thin_mean(int dt, bool wide) { return dt == EEP_F32 ? 16 : wide ? 8 : 1; }
 
 template <int DT, int YT, bool GATE>
 hipError_t launch_product(const eep_product& p, const ProductArgs& a, hipStream_t st) {
@@ -1124,7 +1138,7 @@ hipError_t launch_product(const eep_product& p, const ProductArgs& a, hipStream_
     if (launch_few<DT, YT, GATE, 1, 4>(p, a, st, &e) || launch_few<DT, YT, GATE, 2, 4>(p, a, st, &e)) return e;
   }
   // (the tiles' stream is as long as three steps at least)
-  if (mean <= thin_mean(widens(DT, YT)) || a.row_bytes <= 2 * kStepBytes) return launch_thin<DT, YT, GATE>(a, st);
+  if (mean <= thin_mean(DT, widens(DT, YT)) || a.row_bytes <= 2 * kStepBytes) return launch_thin<DT, YT, GATE>(a, st);
   constexpr bool kLarge = !widens(DT, YT);  // (widened codes take twice the registers)
   const int64_t feature_tiles = (a.features + kTiledRows / (GATE ? 2 : 1) - 1) / (kTiledRows / (GATE ? 2 : 1));
   auto cost = [&](int tt) { return tiled_cost(tt, a.rows, a.slots, feature_tiles, p.cus); };
