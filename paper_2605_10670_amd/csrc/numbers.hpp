@@ -72,10 +72,16 @@ __device__ __forceinline__ float scale_of(uint32_t top) {
   return scale == 0.0f ? 1.0f : scale;
 }
 
-// e4m3(v / scale) of four values, round to nearest even; |v| <= 448 * scale but for roundings.
+// v / scale, saturating at +-448 (NaN stays NaN), which the conversion by itself does not: it gives NaN above 464.  A normal scale
+// leaves no quotient above 448 but for its roundings, a subnormal one of up to 13 units of 2^-149 is rounded so far that there are some of 671.
+__device__ __forceinline__ float quotient(float v, float scale) {
+  return __builtin_elementwise_maximum(__builtin_elementwise_minimum(v / scale, 448.0f), -448.0f);
+}
+
+// e4m3(v / scale) of four values, round to nearest even, saturating.
 __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, float scale) {
-  const int low = __builtin_amdgcn_cvt_pk_fp8_f32(a / scale, b / scale, 0, false);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c / scale, d / scale, low, true);
+  const int low = __builtin_amdgcn_cvt_pk_fp8_f32(quotient(a, scale), quotient(b, scale), 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(quotient(c, scale), quotient(d, scale), low, true);
 }
 
 }  // namespace eep
