@@ -588,7 +588,8 @@ int eep_read_dedup(eep_ctx* ctx, int32_t field, int32_t* host_dst, int64_t n, vo
  * code: device bytes [T, H]; code_scale: device float [T, H/scale_group].  sum may be x or
  * residual itself, and so may y where the types agree.
  * hidden: 8 to 65536, a multiple of 8; scale_group: a power of two from 16 to 512 that divides
- * hidden, or 0 without codes.  A row with an infinity or a NaN gives what the formulas give. */
+ * hidden, or 0 without codes; epsilon: 0 or more.  Squares beyond fp32's range, on either side, do no harm.
+ * A row with an infinity or a NaN, or of zeros with epsilon 0, gives what the formulas give. */
 typedef struct {
   int32_t hidden;
   int32_t in_dtype, gain_dtype, out_dtype; /* EEP_F32 or EEP_BF16 */

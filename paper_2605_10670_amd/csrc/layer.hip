@@ -108,13 +108,18 @@ __global__ __launch_bounds__(1024) void k_norm(NormArgs a, int64_t first) {
     }
     return squares;
   };
-  const float squares = sum_squares(1.0f);
-  float inv = 1.0f / sqrtf(squares / (float)a.H + a.epsilon);
-  if (squares == INFINITY) {
-    // the squares of finite values may be too large for their type; then epsilon is nothing beside them
+  // Squares of finite values may be too large for fp32, or too small: each is cut off at 2^-149, which a mean beside epsilon
+  // of 2^-100 does not feel.  The sum of such a row is that of the row times a power of two, epsilon times its square; the row
+  // itself is multiplied by the larger of the two factors first, so that no small value of it is lost.
+  float by = 1.0f;
+  float mean = sum_squares(1.0f) / (float)a.H;
+  if (mean == INFINITY || mean + a.epsilon < 0x1p-100f) {
+    by = mean == INFINITY ? 0x1p-80f : 0x1p100f;
     __syncthreads();
-    inv = 0x1p-80f / sqrtf(sum_squares(0x1p-80f) / (float)a.H);
+    mean = sum_squares(by) / (float)a.H;
   }
+  const float inv = 1.0f / sqrtf(mean + a.epsilon * by * by);
+  const float factor = by > 1.0f ? by : inv, last_factor = by > 1.0f ? inv : by;
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     const int v = j * threads + tid;
@@ -123,7 +128,7 @@ __global__ __launch_bounds__(1024) void k_norm(NormArgs a, int64_t first) {
     float g[8];
     load8<GAIN_BF16>(a.gain, v, g);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) h[j][i] = h[j][i] * inv * g[i];
+    for (int i = 0; i < 8; ++i) h[j][i] = h[j][i] * factor * last_factor * g[i];
     if (a.y != nullptr) store8<OUT_BF16>(a.y, row_vec + v, h[j]);
     if (a.lanes_per_group != 0) {
       const float scale = scale_of(group_max(top_magnitude<8>(h[j]), a.lanes_per_group));
