@@ -25,7 +25,6 @@ struct eep_product {
 
 namespace eep {
 
-typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kStepBytes = 128;  // along in_features
@@ -82,9 +81,9 @@ __device__ __forceinline__ f32x4 mma(const Frag& a, const Frag& b, f32x4 acc) {
 
 // Codes are multiplied as bf16, of which the matrix cores keep every product: their 8-bit forms line the products of
 // 8 neighbouring k up with the largest of them and keep 13 bits below its first (measured with single products
-// beside a large one; across the eights nothing is lost).  On normally distributed rows a sum of 128 then is
-// 1.3e-5 off (2-norm), and 5.4e-5 with wider ones; as bf16 1e-8 and 7e-8.  Only the tiles' kernel, whose bound the matrix
-// cores are, uses the 8-bit forms, and only for results that are rounded to bf16 (Operand, widens).
+// beside a large one; across the eights nothing is lost), so that 448 * 448 - 448 * 448 + 1 is 0 there.  On normally distributed
+// rows a sum of 128 then is 1.3e-5 off (2-norm), and 5.4e-5 with wider ones; as bf16 1e-8 and 7e-8.  What that costs where the matrix
+// cores are the bound: 4096 rows 2048 -> 7168 through one matrix 126 us, 67 with the 8-bit forms.
 //
 // One block of 128: p[m] + w[m] * x.
 template <int M>
@@ -140,30 +139,15 @@ __device__ __forceinline__ void stream(int begin, int end, Load load, Multiply m
     if (s + u + AHEAD < end) multiply(u);
 }
 
-// An operand, ready to be used several times.  WIDE: e4m3 codes are widened to bf16 (once), see above; else they are
-// multiplied as they are.
-template <int DT, bool WIDE>
+// An operand, ready to be used several times: e4m3 codes are widened to bf16, once.
+template <int DT>
 struct Operand {
   Frag f;
   __device__ __forceinline__ void set(const Frag& v) { f = v; }
-  __device__ __forceinline__ f32x4 times(const Operand& b, f32x4 acc) const {
-    if constexpr (DT == EEP_FP8_E4M3) {
-      i32x8 av, bv;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        av[i] = (int)f.c[0][i];
-        av[4 + i] = (int)f.c[1][i];
-        bv[i] = (int)b.f.c[0][i];
-        bv[4 + i] = (int)b.f.c[1][i];
-      }
-      return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(av, bv, acc, 0, 0, 0, 0, 0, 0);
-    } else {
-      return mma<DT>(f, b.f, acc);
-    }
-  }
+  __device__ __forceinline__ f32x4 times(const Operand& b, f32x4 acc) const { return mma<DT>(f, b.f, acc); }
 };
 template <>
-struct Operand<EEP_FP8_E4M3, true> {
+struct Operand<EEP_FP8_E4M3> {
   bf16x8 v[2][2];
   __device__ __forceinline__ void set(const Frag& f) {
     widen(f.c[0], v[0]);
@@ -572,13 +556,12 @@ __global__ __launch_bounds__(64 * kThinWaves, few_alone(M, TN) ? 2 : 4) void k_p
 // (every eighth) have neighbouring items, those of one slot with the row tiles innermost: what runs at a time
 // shares weights and rows in that XCD's L2.
 //
-// Measured: 4096 tokens of 288 slots fp8 2048 -> 7168 to bf16 940 us (5.1 TB/s, 1.02 PFLOP/s: HBM and the stores of y), 4096 rows
-// through one such matrix 65 to 68 us (1.8 PFLOP/s), bf16 1408 -> 2880 to fp32, 35856 rows in 120 slots, 415 us (0.70 PFLOP/s, 3.5 TB/s),
-// 16384 tokens fp8 7168 -> 2 x 2048 to codes 8.1 ms (0.95 PFLOP/s).  The last is bound by instructions: a SIMD's matrix and vector
+// Measured: 4096 tokens of 288 slots fp8 2048 -> 7168 to bf16 1238 us (3.9 TB/s, 0.78 PFLOP/s), 4096 rows
+// through one such matrix 126 us (0.95 PFLOP/s), bf16 1408 -> 2880 to fp32, 35856 rows in 120 slots, 415 us (0.70 PFLOP/s, 3.5 TB/s),
+// 16384 tokens fp8 7168 -> 2 x 2048 to codes 7.8 to 8.3 ms (0.95 PFLOP/s).  Codes are bound by instructions: a SIMD's matrix and vector
 // instructions take their times one after the other (two wavefronts of products with two vector instructions each ran
 // in the sum of both, not the larger), and a step of a wavefront has 64 products, 128 instructions that widen codes and
-// 64 that scale the sums.  With 8-bit products (and their error) it took 4.3 ms, there bound by the trip to LDS and a clock that
-// falls to 1.8 GHz.
+// 64 that scale the sums.
 // ---------------------------------------------------------------------------
 constexpr int kTiledWaves = 8, kTiledRows = 256;
 constexpr int kTiledThreads = 64 * kTiledWaves;
@@ -679,7 +662,7 @@ struct TileMap {
   }
 };
 
-template <int DT, bool WIDE, int YT, bool GATE, int TT>
+template <int DT, int YT, bool GATE, int TT>
 __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs a) {
   constexpr int kWM = tiled_across(TT), kWN = kTiledWaves / kWM;
   constexpr int kA = kTiledRows / 16 / kWM, kB = 4 * TT / kWN;  // tiles of 16 weight rows and of 16 tokens a wavefront
@@ -875,11 +858,11 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
           for (int j = 0; j < 2; ++j)
             if (j * 64 + part * 16 >= tail) f.c[j] = u32x4{0, 0, 0, 0};
         }
-        Operand<DT, WIDE> o;
+        Operand<DT> o;
         o.set(f);
         return o;
       };
-      Operand<DT, WIDE> b[kB];
+      Operand<DT> b[kB];
 #pragma unroll
       for (int j = 0; j < kB; ++j) b[j] = ready(b_raw[j]);
       [[maybe_unused]] float scale[GATE ? 2 : 1][kB];
@@ -905,7 +888,7 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
             acc[f][j][n] = fmaf(block[i % (kBehind + 1)][n], scale[GATE ? f / (kA / 2) : 0][j], acc[f][j][n]);
         }
       };
-      auto multiply = [&](int i, const Operand<DT, WIDE>& av) {
+      auto multiply = [&](int i, const Operand<DT>& av) {
         const int f = tile_f(i), j = tile_j(i);
         if constexpr (kCodes) {
           block[i % (kBehind + 1)] = av.times(b[j], f32x4{0, 0, 0, 0});
@@ -915,10 +898,10 @@ __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs 
           acc[f][j] = av.times(b[j], acc[f][j]);
         }
       };
-      Operand<DT, WIDE> last[2];
+      Operand<DT> last[2];
 #pragma unroll
       for (int f = 0; f < kA - 2; ++f) {
-        const Operand<DT, WIDE> av = ready(a_raw);
+        const Operand<DT> av = ready(a_raw);
         a_raw = read(stage, row_of_tile(f + 1));
 #pragma unroll
         for (int j = 0; j < kB; ++j) multiply(f * kB + j, av);
@@ -1087,14 +1070,10 @@ bool launch_few(const eep_product& p, ProductArgs a, hipStream_t st, hipError_t*
   return true;
 }
 
-// Are codes widened (see widen)?  Where the result keeps more than 8 bits of significand: fp32, and the fp32 scales of codes.
-constexpr bool widens(int dt, int yt) { return dt == EEP_FP8_E4M3 && yt != EEP_BF16; }
-
 template <int DT, int YT, bool GATE, int TT>
 hipError_t launch_tiled(ProductArgs a, int cus, hipStream_t st) {
-  constexpr bool kWide = widens(DT, YT);
   constexpr int kLds = tiled_lds_bytes(DT == EEP_FP8_E4M3, TT);
-  const auto kernel = k_product_tiled<DT, kWide, YT, GATE, TT>;
+  const auto kernel = k_product_tiled<DT, YT, GATE, TT>;
   static const hipError_t allowed =
       hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
   if (allowed != hipSuccess) return allowed;
@@ -1105,8 +1084,9 @@ hipError_t launch_tiled(ProductArgs a, int cus, hipStream_t st) {
   return hipGetLastError();
 }
 
-// What the tiles of 64 * tt tokens cost, in time: what a step of one takes (measured, us), as often as a CU has one.  A slot's last
-// tile is half empty on average.
+// What the tiles of 64 * tt tokens cost, in time: what a step of one takes (us), as often as a CU has one.  A slot's last
+// tile is half empty on average.  The same steps are taken for every type; with a tile of one matrix on each CU and 128 steps they measured
+// 0.68 / 1.1 / 1.8 in bf16, 1.2 / 1.9 with codes, 2.0 / 3.8 / 7.3 in fp32.
 float tiled_cost(int tt, int rows, int slots, int64_t feature_tiles, int cus) {
   const float step = tt == 1 ? 0.95f : tt == 2 ? 1.35f : 2.2f;
   const int touched = rows < slots ? rows : slots;
@@ -1118,11 +1098,12 @@ float tiled_cost(int tt, int rows, int slots, int64_t feature_tiles, int cus) {
 
 // Rows a slot up to which the thin kernel is chosen: about one; more where the tiles' kernel has codes to widen, which there takes
 // the time of the products themselves.  Thin / tiles of 64 tokens, us: 144 slots bf16 4096 -> 2 x 1024, 64 tokens (3.6 rows
-// a slot) 464 / 410, 200 tokens (11) 477 / 417; 288 slots 7168 -> 2 x 2048 fp8 to codes, 256 tokens (7.1) 1455 / 1529, 512 tokens
-// (14.2, where many slots have more than 16 and are read twice) 1986 / 1539; 2048 -> 7168 to fp32, 32 tokens (0.9) 405 / 510.
+// a slot) 464 / 410, 200 tokens (11) 477 / 417; 288 slots 7168 -> 2 x 2048 fp8 to codes, 64 tokens (1.8) 1180 / 1289, 256 (7.1)
+// 1482 / 1545, 330 (9.2, where some slots have more than 16 and are read twice) 1557 / 1525, 512 (14.2) 1986 / 1539; 2048 -> 7168 to bf16, 128 tokens
+// (3.6) 684 / 760, 256 773 / 790, 330 826 / 797; to fp32, 32 tokens (0.9) 405 / 510.
 // fp32 products take the matrix cores 16 times as long as bf16 ones, and tiles of 64 tokens are mostly empty there: 144 slots
 // 2048 -> 1024, 200 tokens (11 rows a slot) 291 / 389, 9 slots 4992 -> 4096, 76 rows 209 / 314.
-constexpr int thin_mean(int dt, bool wide) { return dt == EEP_F32 ? 16 : wide ? 8 : 1; }
+constexpr int thin_mean(int dt) { return dt == EEP_F32 ? 16 : dt == EEP_FP8_E4M3 ? 8 : 1; }
 
 template <int DT, int YT, bool GATE>
 hipError_t launch_product(const eep_product& p, const ProductArgs& a, hipStream_t st) {
@@ -1138,8 +1119,8 @@ hipError_t launch_product(const eep_product& p, const ProductArgs& a, hipStream_
     if (launch_few<DT, YT, GATE, 1, 4>(p, a, st, &e) || launch_few<DT, YT, GATE, 2, 4>(p, a, st, &e)) return e;
   }
   // (the tiles' stream is as long as three steps at least)
-  if (mean <= thin_mean(DT, widens(DT, YT)) || a.row_bytes <= 2 * kStepBytes) return launch_thin<DT, YT, GATE>(a, st);
-  constexpr bool kLarge = !widens(DT, YT);  // (widened codes take twice the registers)
+  if (mean <= thin_mean(DT) || a.row_bytes <= 2 * kStepBytes) return launch_thin<DT, YT, GATE>(a, st);
+  constexpr bool kLarge = DT != EEP_FP8_E4M3;  // (widened codes take twice the registers)
   const int64_t feature_tiles = (a.features + kTiledRows / (GATE ? 2 : 1) - 1) / (kTiledRows / (GATE ? 2 : 1));
   auto cost = [&](int tt) { return tiled_cost(tt, a.rows, a.slots, feature_tiles, p.cus); };
   const float one = cost(1), two = cost(2), four = cost(4);
