@@ -640,7 +640,8 @@ int eep_route(const eep_router_shape* shape, const void* logits, int32_t* topk_i
  *   the unrounded fp32 values as eep_residual_norm makes them: the second product's x and x_scale.
  *
  * eep_product_create checks a shape and allocates what the product needs beside its operands (a
- * workspace for few rows; hipMalloc on the current device).  Calls with one handle share the
+ * workspace for few rows; hipMalloc on the current device, which is the handle's: calls with it are
+ * made there).  Calls with one handle share the
  * workspace: their kernels may not overlap (one stream, or events between); handles are
  * independent.  eep_product_destroy waits for the device.
  *   num_slots      1 to 65536;  max_rows  0 to 2^30: the most that a call may pass

@@ -1072,15 +1072,11 @@ bool launch_few(const eep_product& p, ProductArgs a, hipStream_t st, hipError_t*
 
 template <int DT, int YT, bool GATE, int TT>
 hipError_t launch_tiled(ProductArgs a, int cus, hipStream_t st) {
-  constexpr int kLds = tiled_lds_bytes(DT == EEP_FP8_E4M3, TT);
-  const auto kernel = k_product_tiled<DT, YT, GATE, TT>;
-  static const hipError_t allowed =
-      hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
-  if (allowed != hipSuccess) return allowed;
   const int features = GATE ? kTiledRows / 2 : kTiledRows;
   a.feature_tiles = (a.features + features - 1) / features;
   const int64_t work = most_tiles(a.rows, a.slots, 64 * TT) * a.feature_tiles;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)(work < cus ? work : cus)), dim3(kTiledThreads), kLds, st, a);
+  hipLaunchKernelGGL((k_product_tiled<DT, YT, GATE, TT>), dim3((unsigned)(work < cus ? work : cus)), dim3(kTiledThreads),
+                     tiled_lds_bytes(DT == EEP_FP8_E4M3, TT), st, a);
   return hipGetLastError();
 }
 
@@ -1105,6 +1101,23 @@ float tiled_cost(int tt, int rows, int slots, int64_t feature_tiles, int cus) {
 // 2048 -> 1024, 200 tokens (11 rows a slot) 291 / 389, 9 slots 4992 -> 4096, 76 rows 209 / 314.
 constexpr int thin_mean(int dt) { return dt == EEP_F32 ? 16 : dt == EEP_FP8_E4M3 ? 8 : 1; }
 
+// Are there tiles of 256 tokens?  (widened codes take twice the registers)
+constexpr bool tiled_large(int dt) { return dt != EEP_FP8_E4M3; }
+
+// More LDS than a kernel may have by default, for the tiles that a product may be launched with.  On the current device: a kernel has a
+// limit on each.
+template <int DT, int YT, bool GATE>
+hipError_t allow_lds() {
+  const auto allow = [](const void* kernel, int tt) {
+    return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, tiled_lds_bytes(DT == EEP_FP8_E4M3, tt));
+  };
+  hipError_t e = allow((const void*)k_product_tiled<DT, YT, GATE, 1>, 1);
+  if (e == hipSuccess) e = allow((const void*)k_product_tiled<DT, YT, GATE, 2>, 2);
+  if constexpr (tiled_large(DT))
+    if (e == hipSuccess) e = allow((const void*)k_product_tiled<DT, YT, GATE, 4>, 4);
+  return e;
+}
+
 template <int DT, int YT, bool GATE>
 hipError_t launch_product(const eep_product& p, const ProductArgs& a, hipStream_t st) {
   const int mean = (a.rows + a.slots - 1) / a.slots;  // rows a slot
@@ -1120,24 +1133,30 @@ hipError_t launch_product(const eep_product& p, const ProductArgs& a, hipStream_
   }
   // (the tiles' stream is as long as three steps at least)
   if (mean <= thin_mean(DT) || a.row_bytes <= 2 * kStepBytes) return launch_thin<DT, YT, GATE>(a, st);
-  constexpr bool kLarge = DT != EEP_FP8_E4M3;  // (widened codes take twice the registers)
   const int64_t feature_tiles = (a.features + kTiledRows / (GATE ? 2 : 1) - 1) / (kTiledRows / (GATE ? 2 : 1));
   auto cost = [&](int tt) { return tiled_cost(tt, a.rows, a.slots, feature_tiles, p.cus); };
   const float one = cost(1), two = cost(2), four = cost(4);
-  if constexpr (kLarge)
+  if constexpr (tiled_large(DT))
     if (four <= one && four <= two) return launch_tiled<DT, YT, GATE, 4>(a, p.cus, st);
   return one <= two ? launch_tiled<DT, YT, GATE, 1>(a, p.cus, st) : launch_tiled<DT, YT, GATE, 2>(a, p.cus, st);
 }
 
-template <int DT>
-hipError_t launch_product(const eep_product& p, const ProductArgs& a, int y_dtype, bool gate, hipStream_t st) {
-  if (gate) {
-    if (y_dtype == EEP_FP8_E4M3) return launch_product<DT, EEP_FP8_E4M3, true>(p, a, st);
-    if (y_dtype == EEP_BF16) return launch_product<DT, EEP_BF16, true>(p, a, st);
-    return launch_product<DT, EEP_F32, true>(p, a, st);
-  }
-  if (y_dtype == EEP_BF16) return launch_product<DT, EEP_BF16, false>(p, a, st);
-  return launch_product<DT, EEP_F32, false>(p, a, st);
+// call(x_dtype, y_dtype, gate), as constants, for a shape that eep_product_create accepts.
+template <int N>
+using Const = std::integral_constant<int, N>;
+template <class Call>
+hipError_t with_types(const eep_product_config& f, Call call) {
+  const auto with_x = [&](auto x) {
+    if (f.gate == EEP_GATE_SILU) {
+      const std::true_type gate;
+      if (f.y_dtype == EEP_FP8_E4M3) return call(x, Const<EEP_FP8_E4M3>(), gate);
+      return f.y_dtype == EEP_BF16 ? call(x, Const<EEP_BF16>(), gate) : call(x, Const<EEP_F32>(), gate);
+    }
+    const std::false_type gate;
+    return f.y_dtype == EEP_BF16 ? call(x, Const<EEP_BF16>(), gate) : call(x, Const<EEP_F32>(), gate);
+  };
+  if (f.x_dtype == EEP_FP8_E4M3) return with_x(Const<EEP_FP8_E4M3>());
+  return f.x_dtype == EEP_BF16 ? with_x(Const<EEP_BF16>()) : with_x(Const<EEP_F32>());
 }
 
 }  // namespace eep
@@ -1177,7 +1196,10 @@ int eep_product_create(const eep_product_config* cfg, eep_product** out) {
   p->cfg = f;
   int device = 0;
   if (hipGetDevice(&device) != hipSuccess ||
-      hipDeviceGetAttribute(&p->cus, hipDeviceAttributeMultiprocessorCount, device) != hipSuccess) {
+      hipDeviceGetAttribute(&p->cus, hipDeviceAttributeMultiprocessorCount, device) != hipSuccess ||
+      with_types(f, [](auto x_dtype, auto y_dtype, auto gate) {
+        return allow_lds<x_dtype.value, y_dtype.value, gate.value>();
+      }) != hipSuccess) {
     (void)hipGetLastError();
     delete p;
     return EEP_ERR_HIP;
@@ -1236,13 +1258,9 @@ int eep_expert_product(eep_product* product, const void* x, const float* x_scale
   a.features = f.out_features;
   a.slot_stride = product->slot_stride;
   a.scale_stride = product->scale_stride;
-  const bool gate = f.gate == EEP_GATE_SILU;
-  hipError_t e;
-  switch (f.x_dtype) {
-    case EEP_FP8_E4M3: e = launch_product<EEP_FP8_E4M3>(*product, a, f.y_dtype, gate, (hipStream_t)stream); break;
-    case EEP_BF16: e = launch_product<EEP_BF16>(*product, a, f.y_dtype, gate, (hipStream_t)stream); break;
-    default: e = launch_product<EEP_F32>(*product, a, f.y_dtype, gate, (hipStream_t)stream);
-  }
+  const hipError_t e = with_types(f, [&](auto x_dtype, auto y_dtype, auto gate) {
+    return launch_product<x_dtype.value, y_dtype.value, gate.value>(*product, a, (hipStream_t)stream);
+  });
   return e == hipSuccess ? EEP_OK : EEP_ERR_HIP;
 }
 
