@@ -639,11 +639,10 @@ int eep_route(const eep_router_shape* shape, const void* logits, int32_t* topk_i
  * y_dtype EEP_FP8_E4M3 (with the gate): codes, and y_scale device float [rows, out_features / 128], from
  *   the unrounded fp32 values as eep_residual_norm makes them: the second product's x and x_scale.
  *
- * eep_product_create checks a shape and allocates what the product needs beside its operands (a
- * workspace for few rows; hipMalloc on the current device, which is the handle's: calls with it are
- * made there).  Calls with one handle share the
- * workspace: their kernels may not overlap (one stream, or events between); handles are
- * independent.  eep_product_destroy waits for the device.
+ * eep_product_create checks a shape and prepares the current device, which is the handle's: calls with
+ * it are made there.  Where y is fp8 it allocates a workspace for few rows (2 MiB; hipMalloc).  Calls with
+ * such a handle share it: their kernels may not overlap (one stream, or events between; a handle for each
+ * of two micro-batches that run side by side), or their codes are wrong.  Handles are independent.  eep_product_destroy waits for the device.
  *   num_slots      1 to 65536;  max_rows  0 to 2^30: the most that a call may pass
  *   in_features, out_features   1 to 2^21
  *   in_features    rows of x and w must be multiples of 16 bytes (EEP_ERR_ALIGN), and whole scale

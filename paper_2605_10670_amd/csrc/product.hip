@@ -19,8 +19,9 @@ struct eep_product {
   eep_product_config cfg;
   int64_t slot_stride, scale_stride;  // bytes
   int cus;                            // of the device
-  float* values;                      // of y before its scales are known, kFewGroups of k_product_few
-  uint32_t* arrived;                  // how many workgroups of a group have theirs there; zero between calls
+  // where y is codes, else NULL:
+  float* values;      // of y before its scales are known, kFewGroups of k_product_few
+  uint32_t* arrived;  // how many workgroups of a group have theirs there; zero between calls
 };
 
 namespace eep {
@@ -1204,20 +1205,22 @@ int eep_product_create(const eep_product_config* cfg, eep_product** out) {
     delete p;
     return EEP_ERR_HIP;
   }
-  const int64_t value_bytes = (int64_t)kFewGroups * kThinTokens * kScaleBlock * sizeof(float);
-  void* workspace = nullptr;
-  hipError_t e = hipMalloc(&workspace, value_bytes + kFewGroups * sizeof(uint32_t));
-  if (e == hipSuccess) {
-    p->values = (float*)workspace;
-    p->arrived = (uint32_t*)((uint8_t*)workspace + value_bytes);
-    e = launch_fill((int32_t*)p->arrived, 0, kFewGroups, nullptr);
-    if (e == hipSuccess) e = hipStreamSynchronize(nullptr);
-    if (e != hipSuccess) (void)hipFree(workspace);
-  }
-  if (e != hipSuccess) {
-    (void)hipGetLastError();
-    delete p;
-    return EEP_ERR_HIP;
+  if (f.y_dtype == EEP_FP8_E4M3) {
+    const int64_t value_bytes = (int64_t)kFewGroups * kThinTokens * kScaleBlock * sizeof(float);
+    void* workspace = nullptr;
+    hipError_t e = hipMalloc(&workspace, value_bytes + kFewGroups * sizeof(uint32_t));
+    if (e == hipSuccess) {
+      p->values = (float*)workspace;
+      p->arrived = (uint32_t*)((uint8_t*)workspace + value_bytes);
+      e = launch_fill((int32_t*)p->arrived, 0, kFewGroups, nullptr);
+      if (e == hipSuccess) e = hipStreamSynchronize(nullptr);
+      if (e != hipSuccess) (void)hipFree(workspace);
+    }
+    if (e != hipSuccess) {
+      (void)hipGetLastError();
+      delete p;
+      return EEP_ERR_HIP;
+    }
   }
   p->slot_stride = f.slot_stride ? f.slot_stride : packed;
   p->scale_stride = f.scale_stride ? f.scale_stride : packed_scale;

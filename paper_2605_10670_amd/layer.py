@@ -119,7 +119,9 @@ class Router:
 
 class ExpertProduct:
     """eep_expert_product.  gate: w has the gate's out_features rows, then the other factor's.  slot_stride and
-    scale_stride: bytes from one slot's weights / scales to the next one's (None: packed)."""
+    scale_stride: bytes from one slot's weights / scales to the next one's (None: packed).  It belongs to the device that is
+    current here.  With y_dtype "fp8" its calls share a workspace: they may not overlap (one stream, or events
+    between); micro-batches that run side by side take a product each, as they take a staging set each."""
 
     def __init__(self, *, num_slots, in_features, out_features, max_rows, x_dtype="bf16", y_dtype="bf16", gate=False,
                  slot_stride=None, scale_stride=None):

@@ -65,3 +65,13 @@ def test_a_failure_is_not_kept(host):
     events = host("fail 1", f"create p 1 1024 1024 {BF16} {BF16} 0 4096", f"create q 1 1024 1024 {BF16} {BF16} 0 4096", "run q 4096 0")
     assert results(events) == [binding.ERR_HIP, binding.OK, binding.OK]
     assert large(events)
+
+
+@pytest.mark.parametrize("x,y,gate", ALL_TYPES)
+def test_a_workspace_for_codes_only(host, x, y, gate):
+    """What the kernel of few rows hands from one workgroup to another are the values behind codes."""
+    events = host("device 2", f"create p 1 1024 1024 {x} {y} {gate} 16", "run p 16 0", "destroy p")
+    assert results(events) == [binding.OK] * 3
+    kinds = [e[0] for e in events]
+    assert kinds.count("malloc") == kinds.count("free") == (1 if y == FP8 else 0)
+    assert all(e[1] == "2" for e in events if e[0] in ("malloc", "free"))
