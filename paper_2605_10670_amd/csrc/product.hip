@@ -162,8 +162,11 @@ struct Operand<EEP_FP8_E4M3> {
   }
 };
 
-// v / (1 + exp(-v)) * u
-__device__ __forceinline__ float silu_times(float v, float u) { return v / (1.0f + expf(-v)) * u; }
+// v / (1 + exp(-v)) * u, of an exponential that does not overflow (below -88 the quotient would be 0, however large u is)
+__device__ __forceinline__ float silu_times(float v, float u) {
+  const float e = expf(-fabsf(v));
+  return (v < 0.0f ? v * e : v) / (1.0f + e) * u;
+}
 
 // Where the `tile`-th tile of TOKENS rows lies: its slot, its first row and the end of the slot's rows.  false: there are
 // fewer.  A lane counts the tiles of a run of slots, a wavefront adds them up; all lanes get the answer.
