@@ -22,10 +22,11 @@ BLOCK = 128
 
 
 def quantise_blocks(w):
-    """fp32 [N, K] -> e4m3 codes and a scale for each 128 x 128 of them."""
+    """fp32 [N, K] -> e4m3 codes and a scale for each 128 x 128 of them (1 where all are zero)."""
     n, k = w.shape
     b = w.view(n // BLOCK, BLOCK, k // BLOCK, BLOCK)
     scale = b.abs().amax(dim=(1, 3)) / 448
+    scale = torch.where(scale == 0, 1.0, scale)
     code = (b / scale[:, None, :, None]).clamp(-448, 448).to(torch.float8_e4m3fn)
     return code.view(n, k), scale
 
