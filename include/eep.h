@@ -667,6 +667,96 @@ int eep_expert_product(eep_product* product, const void* x, const float* x_scale
                        const float* w_scale, const int32_t* offset, void* y, float* y_scale,
                        int32_t rows, void* stream);
 
+/* ---- the backward pass of the layer, and the layer norm (the paper serves; this is for fine-tuning a layer whose forward
+ * pass the calls above are).  As above: queued on `stream`, graph-capturable, grids depend only on T or rows; sums in fp32, each
+ * result rounded once.  A handle below prepares the device that is current when it is made, and belongs to it. */
+
+/* The gradient of eep_combine, by the layout of the last eep_dispatch_layout of the same T (whatever has become of membership
+ * and tables since):
+ *   grad_y[row_of[t, j], :] = round(topk_w[t, j] * grad_out[t, :])
+ *   grad_w[t, j] = sum over h of grad_out[t, h] * y[row_of[t, j], h]   (0 where the pair has no row)
+ * grad_out: device [T, H] out_dtype; y, grad_y: device [T*k, H] y_dtype (grad_y may be y itself; rows >= N are left untouched);
+ * topk_w, grad_w: device float [T, k].  grad_y or grad_w may be NULL; topk_w is only needed for grad_y, y for grad_w.
+ * A row whose pair failure detection dropped within the step took no part in the sum: it gets zeros.
+ * Same call order and errors as eep_combine; it waits for no signal. */
+int eep_combine_grad(eep_ctx* ctx, const void* y, const float* topk_w, const void* grad_out, void* grad_y, float* grad_w,
+                     int32_t T, void* stream);
+
+/* The gradient of eep_dispatch: grad_x[t, :] = round( sum over routed j, ascending, of grad_recv[row_of[t, j], :] ), zeros where
+ * no pair has a row.  Rows' gradients have y_dtype, tokens' out_dtype, whatever the payload's type (of fp8 payloads: the
+ * gradient with respect to the values that the codes stand for).  grad_recv: device [T*k, H]; grad_x: device [T, H]. */
+int eep_dispatch_grad(eep_ctx* ctx, const void* grad_recv, void* grad_x, int32_t T, void* stream);
+
+/* Residual addition and layer norm, row by row:
+ *   h = x + residual, sum = round(h) as eep_residual_norm;  d = h - mean(h)
+ *   y = round(d / sqrt(mean(d * d) + epsilon) * gain + bias)     (bias: device [H] gain_dtype, or NULL)
+ * Types, limits, NULLs and aliasing as there; scale_group must be 0, and y is always written. */
+int eep_layer_norm(const eep_norm_shape* shape, const void* x, const void* residual, const void* gain, const void* bias,
+                   void* sum, void* y, int32_t T, void* stream);
+
+/* The gradients of eep_residual_norm (centred 0) and eep_layer_norm (centred 1) at the rows h that were normalised (`sum`, or
+ * x where there was no residual): with d = h (centred: h - mean(h)), r = sqrt(mean(d * d) + epsilon), u = d / r, v = grad_y * gain,
+ *   grad_h    = round((v - u * mean(v * u) [centred: - mean(v)]) / r + grad_sum)
+ *   grad_gain = sum over the rows of grad_y * u,  grad_bias = that of grad_y (centred only); accumulate: added to what is there
+ * grad_h is the gradient of x and of residual alike; grad_sum (or NULL) what reaches `sum` by itself.
+ * h, grad_sum, grad_h: device [T, H] in_dtype; gain: device [H] gain_dtype; grad_y: device [T, H] out_dtype; grad_gain,
+ * grad_bias: device float [H].  Any of the three results may be NULL.  grad_h may be h or grad_sum itself, or grad_y where the
+ * types agree.  The sums over rows are added in an order that depends on T alone.
+ * The handle owns a workspace for the sums (up to 2 workgroups a CU by hidden floats, twice that for centred): calls with it
+ * share that, and may not overlap (one stream, or events between).  eep_norm_grad_destroy waits for the device. */
+typedef struct {
+  int32_t hidden;
+  int32_t in_dtype, gain_dtype, out_dtype; /* EEP_F32 or EEP_BF16 */
+  int32_t centred;
+  float epsilon;
+} eep_norm_grad_config;
+typedef struct eep_norm_grad eep_norm_grad;
+int eep_norm_grad_create(const eep_norm_grad_config* cfg, eep_norm_grad** out);
+int eep_norm_grad_destroy(eep_norm_grad* grad);
+int eep_norm_grad_run(eep_norm_grad* grad, const void* h, const void* gain, const void* grad_y, const void* grad_sum,
+                      void* grad_h, float* grad_gain, float* grad_bias, int32_t accumulate, int32_t T, void* stream);
+
+/* The gradient of eep_route's weights with respect to the logits, from what it returned: with inner = sum over the chosen j of
+ * topk_w[j] * grad_w[j] (topk_idx -1: not chosen),
+ *   over_all == 0: grad_logits[topk_idx[j]] = topk_w[j] * (grad_w[j] - inner), the others 0
+ *   over_all != 0: grad_logits[e] = -p[e] * inner, and topk_w[j] * grad_w[j] more where e is chosen; p: the softmax over all logits
+ * Logits of -infinity and NaN get 0.  logits: as eep_route's, only for over_all (else NULL); grad_w: device float [T, topk];
+ * grad_logits: device [T, num_logical] in_dtype, all of it written. */
+int eep_route_grad(const eep_router_shape* shape, const void* logits, const int32_t* topk_idx, const float* topk_w,
+                   const float* grad_w, void* grad_logits, int32_t T, void* stream);
+
+/* The gradients of eep_expert_product for fp32 and bf16 operands: with g = grad_y (without a gate),
+ *   grad_x[i, k]     = round(sum over n of g[i, n] * w[p][n, k])          for offset[p] <= i < offset[p+1]
+ *   grad_w[p][n, k]  = round(sum over the slot's rows i of g[i, n] * x[i, k])   (0 for a slot without rows)
+ *                      accumulate: round(that + what is there)
+ *   gate EEP_GATE_SILU: with a = sums[i, n], b = sums[i, out_features + n], the product's sums before the gate (those of an
+ *   eep_expert_product without a gate and 2 * out_features), s = 1 / (1 + exp(-a)),
+ *     grad_sums[i, n] = round(grad_y[i, n] * b * s * (1 + a * (1 - s))), grad_sums[i, out_features + n] = round(grad_y[i, n] * a * s)
+ *   and g is grad_sums, as rounded.
+ * Rows outside every slot are left untouched in grad_sums and grad_x, and are read nowhere.
+ *   dtype         EEP_F32 or EEP_BF16: of grad_y, sums, grad_sums, x, w and grad_x
+ *   grad_w_dtype  EEP_F32 or EEP_BF16
+ *   grad_y   device [rows, out_features];  sums, grad_sums  device [rows, 2 * out_features], NULL without a gate
+ *            (grad_sums may be sums itself)
+ *   x        device [rows, in_features], needed for grad_w;  w  as eep_expert_product's, needed for grad_x
+ *   grad_x   device [rows, in_features] or NULL;  grad_w  device, slot p's begins p * grad_stride bytes in, or NULL.  Results may not
+ *            overlap an operand; with a gate both may be NULL.
+ * Row sizes, strides, limits and offsets are treated as eep_product_create and eep_expert_product treat them; rows 0 with grad_w
+ * writes its zeros.  Calls with one handle may overlap. */
+typedef struct {
+  int32_t num_slots, in_features, out_features;
+  int32_t dtype, grad_w_dtype;
+  int32_t gate;
+  int32_t max_rows;
+  int64_t slot_stride, grad_stride;
+} eep_product_grad_config;
+typedef struct eep_product_grad eep_product_grad;
+int eep_product_grad_create(const eep_product_grad_config* cfg, eep_product_grad** out);
+int eep_product_grad_destroy(eep_product_grad* grad);
+int eep_product_grad_run(eep_product_grad* grad, const void* grad_y, const void* sums, const void* x, const void* w,
+                         const int32_t* offset, void* grad_sums, void* grad_x, void* grad_w, int32_t accumulate, int32_t rows,
+                         void* stream);
+
 /* ---- hipGraph helper (Sec. 2.3, Fig. 4: capture once, replay, patch table
  * contents only) ------------------------------------------------------------
  * eep_graph_begin puts `stream` (not the default stream) into capture mode;

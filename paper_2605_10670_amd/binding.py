@@ -113,6 +113,8 @@ def load():
         "eep_dispatch": [vp, vp, vp, vp, vp, i32, vp],
         "eep_dispatch_quant": [vp, vp, vp, vp, i32, vp],
         "eep_combine": [vp, vp, vp, vp, i32, vp],
+        "eep_combine_grad": [vp, vp, vp, vp, vp, vp, i32, vp],
+        "eep_dispatch_grad": [vp, vp, vp, i32, vp],
         "eep_expert_stub": [vp, i32, vp, vp, vp, vp, i32, vp],
         "eep_debug_check_layout": [vp, i32, vp, vp],
         "eep_get_view": [vp, ctypes.POINTER(_View)],
@@ -324,6 +326,10 @@ class Graph:
             self._h = None
 
 
+# Kinds of the arguments of the backward pass's calls.
+GRAD_KINDS = {"eep_combine_grad": "hpppppis", "eep_dispatch_grad": "hppis"}
+
+
 class Context:
     """One EP instance on the current GPU."""
 
@@ -431,6 +437,13 @@ class Context:
 
     def combine(self, y, topk_w, out, T, stream=None):
         self._step("eep_combine", "hpppis", y, topk_w, out, T, stream)
+
+    def combine_grad(self, y, topk_w, grad_out, grad_y, grad_w, T, stream=None):
+        """Gradients of combine by the last layout of T tokens; y, topk_w, grad_y or grad_w may be None (eep.h)."""
+        self._step("eep_combine_grad", GRAD_KINDS["eep_combine_grad"], y, topk_w, grad_out, grad_y, grad_w, T, stream)
+
+    def dispatch_grad(self, grad_recv, grad_x, T, stream=None):
+        self._step("eep_dispatch_grad", GRAD_KINDS["eep_dispatch_grad"], grad_recv, grad_x, T, stream)
 
     def expert_stub(self, kind, recv_x, y, T, recv_scale=None, expert_scale=None, stream=None):
         kind = STUBS[kind] if isinstance(kind, str) else kind

@@ -27,8 +27,6 @@ hipError_t set_shared_word(eep_membership* m, int32_t several) {
   return e;
 }
 
-bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
-
 bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
   return a != nullptr && b != nullptr && (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
 }
@@ -553,6 +551,28 @@ int eep_combine(eep_ctx* c, const void* y, const float* topk_w, void* out, int32
   if (c->detect_timeout_ticks > 0) c->mem->unread_round = true;  // until eep_read_failures
   hold_rows(c, y, holds_for_combine, (hipStream_t)stream);
   hipError_t e = launch_combine(c, y, topk_w, out, T, (hipStream_t)stream);
+  return e == hipSuccess ? EEP_OK : fail_hip(c, e);
+}
+
+int eep_combine_grad(eep_ctx* c, const void* y, const float* topk_w, const void* grad_out, void* grad_y, float* grad_w,
+                     int32_t T, void* stream) {
+  if (!c || T < 0 || T > c->T_max) return EEP_ERR_INVALID_ARG;
+  if (c->layout_T != T) return EEP_ERR_STATE;
+  if (T == 0) return EEP_OK;
+  if (!grad_out || (!grad_y && !grad_w) || (grad_y && !topk_w) || (grad_w && !y)) return EEP_ERR_INVALID_ARG;
+  if (!aligned16(y) || !aligned16(grad_out) || !aligned16(grad_y) || ((uintptr_t)topk_w & 3u) || ((uintptr_t)grad_w & 3u))
+    return EEP_ERR_ALIGN;
+  const hipError_t e = launch_combine_grad(c, y, topk_w, grad_out, grad_y, grad_w, T, (hipStream_t)stream);
+  return e == hipSuccess ? EEP_OK : fail_hip(c, e);
+}
+
+int eep_dispatch_grad(eep_ctx* c, const void* grad_recv, void* grad_x, int32_t T, void* stream) {
+  if (!c || T < 0 || T > c->T_max) return EEP_ERR_INVALID_ARG;
+  if (c->layout_T != T) return EEP_ERR_STATE;
+  if (T == 0) return EEP_OK;
+  if (!grad_recv || !grad_x) return EEP_ERR_INVALID_ARG;
+  if (!aligned16(grad_recv) || !aligned16(grad_x)) return EEP_ERR_ALIGN;
+  const hipError_t e = launch_dispatch_grad(c, grad_recv, grad_x, T, (hipStream_t)stream);
   return e == hipSuccess ? EEP_OK : fail_hip(c, e);
 }
 

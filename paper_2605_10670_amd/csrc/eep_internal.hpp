@@ -54,6 +54,8 @@ inline size_t map_lds_bytes(int E, int P, int R, int tile_tokens, int k) {
                             (size_t)2 * tile_tokens * k);
 }
 
+inline bool f32_or_bf16(int dtype) { return dtype == EEP_F32 || dtype == EEP_BF16; }
+inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 inline int dtype_bytes(int dt) { return dt == EEP_F32 ? 4 : dt == EEP_BF16 ? 2 : 1; }
 
 // Workgroups that one launch may have: a grid of 2^32 lanes or more loses its upper bits without
@@ -216,6 +218,10 @@ hipError_t launch_combine(eep_ctx* c, const void* y, const float* w, void* out, 
                           hipStream_t st);
 hipError_t launch_stub(eep_ctx* c, int kind, const void* recv_x, const float* recv_scale,
                        const float* expert_scale, void* y, int T, hipStream_t st);
+// tokens_grad.hip
+hipError_t launch_combine_grad(eep_ctx* c, const void* y, const float* topk_w, const void* grad_out, void* grad_y, float* grad_w,
+                               int T, hipStream_t st);
+hipError_t launch_dispatch_grad(eep_ctx* c, const void* grad_recv, void* grad_x, int T, hipStream_t st);
 // detect.hip
 hipError_t launch_signal(eep_ctx* c, hipStream_t st);
 // api.hip

@@ -28,44 +28,6 @@ struct NormArgs {
   float epsilon;
 };
 
-template <bool BF16>
-__device__ __forceinline__ void load8(const void* base, int64_t vec, float (&v)[8]) {
-  if constexpr (BF16) {
-    const u32x4 d = ((const u32x4*)base)[vec];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[2 * i] = bf16_lo(d[i]);
-      v[2 * i + 1] = bf16_hi(d[i]);
-    }
-  } else {
-    const f32x4 a = ((const f32x4*)base)[2 * vec], b = ((const f32x4*)base)[2 * vec + 1];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[i] = a[i];
-      v[4 + i] = b[i];
-    }
-  }
-}
-
-template <bool BF16>
-__device__ __forceinline__ void store8(void* base, int64_t vec, const float (&v)[8]) {
-  if constexpr (BF16) {
-    u32x4 d;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) d[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
-    __builtin_nontemporal_store(d, &((u32x4*)base)[vec]);
-  } else {
-    __builtin_nontemporal_store(f32x4{v[0], v[1], v[2], v[3]}, &((f32x4*)base)[2 * vec]);
-    __builtin_nontemporal_store(f32x4{v[4], v[5], v[6], v[7]}, &((f32x4*)base)[2 * vec + 1]);
-  }
-}
-
-// The sum over groups of 16 or all 64 lanes, in every lane.
-template <int LANES>
-__device__ __forceinline__ float lane_sum(float v) {
-  return fold<LANES>(v, [](float a, float b) { return a + b; });
-}
-
 template <bool IN_BF16, bool GAIN_BF16, bool OUT_BF16, int NV>
 __global__ __launch_bounds__(1024) void k_norm(NormArgs a, int64_t first) {
   __shared__ float s_part[16];
@@ -326,8 +288,128 @@ hipError_t launch_route(const eep_router_shape& s, const void* logits, int32_t* 
   return hipErrorInvalidValue;
 }
 
-bool f32_or_bf16(int dtype) { return dtype == EEP_F32 || dtype == EEP_BF16; }
-bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+// ---------------------------------------------------------------------------
+// the router's gradient: with inner = sum over the chosen j of w_j * grad_w_j, a chosen logit gets w_j * (grad_w_j - inner) and the
+// others nothing; over all logits every one gets -p * inner, p its share, and a chosen one w_j * grad_w_j more.
+//
+// A group of LANES lanes has a token, four neighbouring logits a lane at a time, to which the lane adds those of the k choices that are
+// among them.  Bound by memory at many tokens, by one trip at few.
+// ---------------------------------------------------------------------------
+template <bool BF16, int LANES, bool FOURS>
+__global__ __launch_bounds__(256) void k_route_grad(const void* __restrict__ logits, const int32_t* __restrict__ topk_idx,
+                                                    const float* __restrict__ topk_w, const float* __restrict__ grad_w,
+                                                    void* __restrict__ grad_logits, int E, int k, int over_all, int64_t first,
+                                                    int64_t end) {
+  constexpr int kTokens = 256 / LANES;
+  const int lane = threadIdx.x & (LANES - 1);
+  const int64_t t = first + (int64_t)blockIdx.x * kTokens + threadIdx.x / LANES;
+  if (t >= end) return;  // (a group's lanes go together)
+  const auto load4 = [&](int e, float (&v)[4]) {
+    if constexpr (FOURS) {
+      if constexpr (BF16) {
+        const u32x2 d = *(const u32x2*)((const uint16_t*)logits + t * E + e);
+        v[0] = bf16_lo(d[0]), v[1] = bf16_hi(d[0]), v[2] = bf16_lo(d[1]), v[3] = bf16_hi(d[1]);
+      } else {
+        const f32x4 d = *(const f32x4*)((const float*)logits + t * E + e);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = d[i];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        v[i] = e + i >= E ? -INFINITY
+                          : BF16 ? __uint_as_float((uint32_t)((const uint16_t*)logits)[t * E + e + i] << 16)
+                                 : ((const float*)logits)[t * E + e + i];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = v[i] > -INFINITY ? v[i] : -INFINITY;  // (NaN weighs nothing either)
+  };
+  // the choices, LANES of them at a time; top-32 of groups of 16 lanes takes two
+  constexpr int kRounds = 32 / LANES > 0 ? 32 / LANES : 1;
+  int idx[kRounds];
+  float part[kRounds], inner = 0.0f;
+#pragma unroll
+  for (int r = 0; r < kRounds; ++r) {
+    const int j = r * LANES + lane;
+    idx[r] = j < k ? topk_idx[t * k + j] : -1;
+    part[r] = 0.0f;
+    if (idx[r] >= 0) part[r] = topk_w[t * k + j] * grad_w[t * k + j];
+    inner += part[r];
+  }
+  inner = lane_sum<LANES>(inner);
+  float top = -INFINITY, all = 0.0f;
+  if (over_all == 0) {
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r)
+      if (idx[r] >= 0) {
+        const int64_t at = t * k + r * LANES + lane;
+        part[r] = topk_w[at] * (grad_w[at] - inner);
+      }
+  } else {
+    float v[4];
+    for (int e = lane * 4; e < E; e += LANES * 4) {
+      load4(e, v);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top = fmaxf(top, v[i]);
+    }
+    top = fold<LANES>(top, [](float a, float b) { return fmaxf(a, b); });
+    for (int e = lane * 4; e < E; e += LANES * 4) {
+      load4(e, v);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) all += v[i] > -INFINITY ? exp_below(v[i], top) : 0.0f;
+    }
+    all = lane_sum<LANES>(all);
+  }
+  const int group = threadIdx.x & 63 & ~(LANES - 1);
+  for (int e = lane * 4; e < (E + LANES * 4 - 1) / (LANES * 4) * (LANES * 4); e += LANES * 4) {
+    float g[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (over_all != 0 && e < E) {
+      float v[4];
+      load4(e, v);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) g[i] = v[i] > -INFINITY ? -(exp_below(v[i], top) / all) * inner : 0.0f;
+    }
+    // (all lanes take part: each brings its choices)
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r)
+      for (int j = 0; j < LANES && r * LANES + j < k; ++j) {
+        const int chosen = __shfl(idx[r], group + j, 64);
+        const float more = __shfl(part[r], group + j, 64);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) g[i] += chosen == e + i ? more : 0.0f;
+      }
+    if (e >= E) continue;
+    if constexpr (FOURS) {
+      if constexpr (BF16)
+        *(u32x2*)((uint16_t*)grad_logits + t * E + e) = u32x2{pack_bf16x2(g[0], g[1]), pack_bf16x2(g[2], g[3])};
+      else
+        *(f32x4*)((float*)grad_logits + t * E + e) = f32x4{g[0], g[1], g[2], g[3]};
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (e + i >= E) continue;
+        if constexpr (BF16)
+          ((uint16_t*)grad_logits)[t * E + e + i] = (uint16_t)pack_bf16x2(g[i], 0.0f);
+        else
+          ((float*)grad_logits)[t * E + e + i] = g[i];
+      }
+    }
+  }
+}
+
+template <bool BF16, int LANES>
+hipError_t launch_route_grad(const eep_router_shape& s, const void* logits, const int32_t* topk_idx, const float* topk_w,
+                             const float* grad_w, void* grad_logits, int T, hipStream_t st) {
+  constexpr int kTokens = 256 / LANES;
+  const uintptr_t four = 4 * dtype_bytes(s.in_dtype);
+  const bool fours = s.num_logical % 4 == 0 && (uintptr_t)logits % four == 0 && (uintptr_t)grad_logits % four == 0;
+  return in_launches(T, max_blocks(256) * kTokens, [&](int64_t first, int64_t n) {
+    hipLaunchKernelGGL((fours ? k_route_grad<BF16, LANES, true> : k_route_grad<BF16, LANES, false>),
+                       dim3((unsigned)((n + kTokens - 1) / kTokens)), dim3(256), 0, st, logits, topk_idx, topk_w, grad_w, grad_logits,
+                       s.num_logical, s.topk, s.over_all, first, first + n);
+    return hipGetLastError();
+  });
+}
 
 }  // namespace eep
 
@@ -382,6 +464,26 @@ int eep_route(const eep_router_shape* shape, const void* logits, int32_t* topk_i
     return EEP_ERR_ALIGN;
   const hipError_t e = s.in_dtype == EEP_BF16 ? launch_route<true>(s, logits, topk_idx, topk_w, T, (hipStream_t)stream)
                                               : launch_route<false>(s, logits, topk_idx, topk_w, T, (hipStream_t)stream);
+  return e == hipSuccess ? EEP_OK : EEP_ERR_HIP;
+}
+
+int eep_route_grad(const eep_router_shape* shape, const void* logits, const int32_t* topk_idx, const float* topk_w,
+                   const float* grad_w, void* grad_logits, int32_t T, void* stream) {
+  if (!shape || T < 0) return EEP_ERR_INVALID_ARG;
+  const eep_router_shape& s = *shape;
+  if (s.num_logical < 1 || s.num_logical > kRouteMaxExperts || s.topk < 1 || s.topk > kMaxTopk ||
+      s.topk > s.num_logical || !f32_or_bf16(s.in_dtype))
+    return EEP_ERR_INVALID_ARG;
+  if (T == 0) return EEP_OK;
+  if (!topk_idx || !topk_w || !grad_w || !grad_logits || (s.over_all != 0) != (logits != nullptr)) return EEP_ERR_INVALID_ARG;
+  const uintptr_t element = dtype_bytes(s.in_dtype);
+  if ((uintptr_t)logits % element || (uintptr_t)grad_logits % element || ((uintptr_t)topk_idx & 3u) || ((uintptr_t)topk_w & 3u) ||
+      ((uintptr_t)grad_w & 3u))
+    return EEP_ERR_ALIGN;
+  hipStream_t st = (hipStream_t)stream;
+  const hipError_t e = s.in_dtype == EEP_BF16
+                           ? launch_route_grad<true, 64>(s, logits, topk_idx, topk_w, grad_w, grad_logits, T, st)
+                           : launch_route_grad<false, 64>(s, logits, topk_idx, topk_w, grad_w, grad_logits, T, st);
   return e == hipSuccess ? EEP_OK : EEP_ERR_HIP;
 }
 

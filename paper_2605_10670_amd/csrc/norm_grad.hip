@@ -1,0 +1,473 @@
+// The layer norm, and the gradients of both norms: of their rows, gain and bias.
+#include <new>
+
+#include "eep_internal.hpp"
+#include "numbers.hpp"
+
+struct eep_norm_grad {
+  eep_norm_grad_config cfg;
+  int groups;      // rows of partial sums
+  float* partial;  // [groups][hidden] of the gain, behind them as many of the bias
+};
+
+namespace eep {
+
+constexpr int kNormMaxWidth = 65536;
+
+// Sums over the workgroup of up to two values, in every thread, added in the order of the wavefronts.
+__device__ __forceinline__ void block_sum(float& a, float& b, float (*part)[2]) {
+  const int threads = blockDim.x;
+  a = lane_sum<64>(a);
+  b = lane_sum<64>(b);
+  if (threads > 64) {
+    __syncthreads();  // (the sums before are read)
+    if ((threadIdx.x & 63) == 0) {
+      part[threadIdx.x >> 6][0] = a;
+      part[threadIdx.x >> 6][1] = b;
+    }
+    __syncthreads();
+    a = b = 0.0f;
+    for (int w = 0; w < threads / 64; ++w) {
+      a += part[w][0];
+      b += part[w][1];
+    }
+  }
+}
+
+__device__ __forceinline__ void load8_any(bool bf16, const void* base, int64_t vec, float (&v)[8]) {
+  if (bf16)
+    load8<true>(base, vec, v);
+  else
+    load8<false>(base, vec, v);
+}
+
+// What a row's squares leave of fp32's range: a factor for the row by which they fit it (1 for nearly every row).
+__device__ __forceinline__ float fitting(float mean_square, float epsilon) {
+  if (!(mean_square < INFINITY)) return 0x1p-80f;
+  return mean_square + epsilon < 0x1p-100f ? 0x1p100f : 1.0f;
+}
+
+// ---------------------------------------------------------------------------
+// layer norm: h = x + r;  d = h - mean(h);  y = d / sqrt(mean(d^2) + eps) * g + b.
+//
+// A workgroup has a row, all of it in registers, as the residual norm's kernel does; the mean and the sum of squares are two
+// trips through LDS.  Bound by memory at many rows.
+// ---------------------------------------------------------------------------
+struct LayerNormArgs {
+  const void *x, *residual, *gain, *bias;
+  void *sum, *y;
+  int H;
+  bool gain_bf16;
+  float epsilon;
+};
+
+// Takes the mean out of h, times `by`: a row whose sum leaves fp32 is scaled first.  Returns the factor that h then holds.
+template <int NV>
+__device__ __forceinline__ float centre(float (&h)[NV][8], int H, int vecs, float (*part)[2]) {
+  const int threads = blockDim.x, tid = threadIdx.x;
+  float by = 1.0f;
+  for (int round = 0; round < 2; ++round) {
+    float sum = 0.0f, top = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum += h[j][i];
+    block_sum(sum, top, part);
+    if (round == 0 && !(fabsf(sum) < INFINITY)) {
+      by = 0x1p-80f;
+      sum = 0.0f;
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          h[j][i] *= by;
+          sum += h[j][i];
+        }
+      block_sum(sum, top, part);
+    }
+    const float mean = sum / (float)H;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      if (j * threads + tid >= vecs) continue;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) h[j][i] -= mean;
+    }
+  }
+  return by;
+}
+
+template <bool IN_BF16, bool OUT_BF16, int NV>
+__global__ __launch_bounds__(1024) void k_layer_norm(LayerNormArgs a, int64_t first) {
+  __shared__ float s_part[16][2];
+  const int64_t row = first + blockIdx.x;
+  const int vecs = a.H / 8, threads = blockDim.x, tid = threadIdx.x;
+  const int64_t row_vec = row * vecs;
+  float h[NV][8];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int v = j * threads + tid;
+    if (v < vecs) {
+      load8<IN_BF16>(a.x, row_vec + v, h[j]);
+      if (a.residual != nullptr) {
+        float r[8];
+        load8<IN_BF16>(a.residual, row_vec + v, r);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[j][i] += r[i];
+      }
+      if (a.sum != nullptr) store8<IN_BF16>(a.sum, row_vec + v, h[j]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) h[j][i] = 0.0f;
+    }
+  }
+  float by = centre<NV>(h, a.H, vecs, s_part);
+  auto mean_square = [&]() {
+    float squares = 0.0f, none = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) squares = fmaf(h[j][i], h[j][i], squares);
+    block_sum(squares, none, s_part);
+    return squares / (float)a.H;
+  };
+  float mean = mean_square();
+  const float more = by == 1.0f ? fitting(mean, a.epsilon) : 1.0f;
+  if (more != 1.0f) {
+    by = more;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) h[j][i] *= by;
+    mean = mean_square();
+  }
+  const float inv = 1.0f / sqrtf(mean + a.epsilon * by * by);
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int v = j * threads + tid;
+    if (v >= vecs) continue;
+    float g[8], b[8];
+    load8_any(a.gain_bf16, a.gain, v, g);
+    if (a.bias != nullptr)
+      load8_any(a.gain_bf16, a.bias, v, b);
+    else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) b[i] = 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) h[j][i] = fmaf(h[j][i] * inv, g[i], b[i]);
+    store8<OUT_BF16>(a.y, row_vec + v, h[j]);
+  }
+}
+
+template <bool IN_BF16, bool OUT_BF16>
+static hipError_t launch_layer_norm(const LayerNormArgs& a, int T, hipStream_t st) {
+  const int vecs = a.H / 8;
+  int nv = 1;  // vectors a thread, as the residual norm has them
+  while (nv < 8 && (vecs > nv * 1024 || (T >= 1024 && vecs > nv * 512))) nv *= 2;
+  const int threads = ((vecs + nv - 1) / nv + 63) / 64 * 64;
+  return in_launches(T, max_blocks(threads), [&](int64_t first, int64_t n) {
+    const dim3 grid((unsigned)n), block((unsigned)threads);
+    switch (nv) {
+      case 1: hipLaunchKernelGGL((k_layer_norm<IN_BF16, OUT_BF16, 1>), grid, block, 0, st, a, first); break;
+      case 2: hipLaunchKernelGGL((k_layer_norm<IN_BF16, OUT_BF16, 2>), grid, block, 0, st, a, first); break;
+      case 4: hipLaunchKernelGGL((k_layer_norm<IN_BF16, OUT_BF16, 4>), grid, block, 0, st, a, first); break;
+      default: hipLaunchKernelGGL((k_layer_norm<IN_BF16, OUT_BF16, 8>), grid, block, 0, st, a, first);
+    }
+    return hipGetLastError();
+  });
+}
+
+// ---------------------------------------------------------------------------
+// the norms' gradients: with d = h (or h - mean(h)), u = d / sqrt(mean(d^2) + eps), v = grad_y * gain,
+//   grad_h = (v - u * mean(v * u) [- mean(v)]) / sqrt(mean(d^2) + eps) + grad_sum,
+//   grad_gain = the sum over rows of grad_y * u, grad_bias = that of grad_y.
+//
+// A workgroup goes over every so manieth row; a thread has the same channels of each, whose gain and bias sums stay in its
+// registers, and the next row's loads are under way while this one's sums cross the workgroup.  The sums of the workgroups
+// are left in the workspace and added up, in their order, by a second kernel.
+// ---------------------------------------------------------------------------
+struct NormGradArgs {
+  const void *h, *gain, *grad_y, *grad_sum;
+  void* grad_h;
+  float* partial;  // [gridDim.x][H], behind gridDim.x of them those of the bias; NULL: none wanted
+  int H, T;
+  bool gain_bf16;
+  float epsilon;
+};
+
+template <bool BF16>
+struct Raw8 {
+  u32x4 d[BF16 ? 1 : 2];
+  __device__ __forceinline__ void load(const void* base, int64_t vec) {
+    const u32x4* from = (const u32x4*)base + vec * (BF16 ? 1 : 2);
+#pragma unroll
+    for (int i = 0; i < (BF16 ? 1 : 2); ++i) d[i] = __builtin_nontemporal_load(from + i);
+  }
+  __device__ __forceinline__ float at(int i) const {
+    if constexpr (BF16)
+      return i & 1 ? bf16_hi(d[0][i >> 1]) : bf16_lo(d[0][i >> 1]);
+    else
+      return __uint_as_float(d[i >> 2][i & 3]);
+  }
+};
+
+constexpr int norm_grad_threads(int nv) { return nv == 8 ? 1024 : 512; }
+
+template <bool IN_BF16, bool OUT_BF16, bool CENTRED, int NV>
+__global__ __launch_bounds__(norm_grad_threads(NV)) void k_norm_grad(NormGradArgs a) {
+  __shared__ float s_part[16][2];
+  const int vecs = a.H / 8, threads = blockDim.x, tid = threadIdx.x;
+  const float count = (float)a.H;
+  Raw8<IN_BF16> h_raw[NV], stream_raw[NV];
+  Raw8<OUT_BF16> grad_raw[NV];
+  float gain_sum[NV][8], bias_sum[CENTRED ? NV : 1][8];
+  const auto fetch = [&](int64_t row) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int v = j * threads + tid;
+      if (v >= vecs) continue;
+      h_raw[j].load(a.h, row * vecs + v);
+      grad_raw[j].load(a.grad_y, row * vecs + v);
+      if (a.grad_sum != nullptr) stream_raw[j].load(a.grad_sum, row * vecs + v);
+    }
+  };
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      gain_sum[j][i] = 0.0f;
+      if constexpr (CENTRED) bias_sum[j][i] = 0.0f;
+    }
+  int64_t row = blockIdx.x;
+  fetch(row);
+  for (; row < a.T; row += gridDim.x) {
+    float d[NV][8], v[NV][8];  // v: grad_y until the gain's sums have it, then grad_y * gain
+    Raw8<IN_BF16> stream[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const bool in = j * threads + tid < vecs;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        d[j][i] = in ? h_raw[j].at(i) : 0.0f;
+        v[j][i] = in ? grad_raw[j].at(i) : 0.0f;
+      }
+      stream[j] = stream_raw[j];
+    }
+    if (row + gridDim.x < a.T) fetch(row + gridDim.x);
+    float by = 1.0f;
+    if constexpr (CENTRED) by = centre<NV>(d, a.H, vecs, s_part);
+    float squares, along;
+    const auto sums = [&]() {
+      squares = along = 0.0f;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const int at = j * threads + tid;
+        if (at >= vecs) continue;
+        float g[8];
+        load8_any(a.gain_bf16, a.gain, at, g);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          squares = fmaf(d[j][i], d[j][i], squares);
+          along = fmaf(v[j][i] * g[i], d[j][i], along);
+        }
+      }
+      block_sum(squares, along, s_part);
+    };
+    sums();
+    const float more = by == 1.0f ? fitting(squares / count, a.epsilon) : 1.0f;
+    if (more != 1.0f) {
+      by = more;
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[j][i] *= by;
+      sums();
+    }
+    const float inv = 1.0f / sqrtf(squares / count + a.epsilon * by * by);
+    along = along * inv / count;  // mean(v * u)
+    float mean = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int at = j * threads + tid;
+      if (at >= vecs) continue;
+      float g[8];
+      load8_any(a.gain_bf16, a.gain, at, g);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        d[j][i] *= inv;  // u
+        gain_sum[j][i] = fmaf(v[j][i], d[j][i], gain_sum[j][i]);
+        if constexpr (CENTRED) bias_sum[j][i] += v[j][i];
+        v[j][i] *= g[i];
+        if constexpr (CENTRED) mean += v[j][i];
+      }
+    }
+    if (a.grad_h != nullptr) {
+      if constexpr (CENTRED) {
+        float none = 0.0f;
+        block_sum(mean, none, s_part);
+        mean /= count;
+      }
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const int at = j * threads + tid;
+        if (at >= vecs) continue;
+        float o[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          o[i] = (fmaf(-d[j][i], along, v[j][i]) - mean) * inv * by;
+          if (a.grad_sum != nullptr) o[i] += stream[j].at(i);
+        }
+        store8<IN_BF16>(a.grad_h, row * vecs + at, o);
+      }
+    }
+  }
+  if (a.partial == nullptr) return;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int at = j * threads + tid;
+    if (at >= vecs) continue;
+    f32x4* to = (f32x4*)(a.partial + (int64_t)blockIdx.x * a.H) + 2 * at;
+    to[0] = f32x4{gain_sum[j][0], gain_sum[j][1], gain_sum[j][2], gain_sum[j][3]};
+    to[1] = f32x4{gain_sum[j][4], gain_sum[j][5], gain_sum[j][6], gain_sum[j][7]};
+    if constexpr (CENTRED) {
+      f32x4* bias_to = to + (int64_t)gridDim.x * a.H / 4;
+      bias_to[0] = f32x4{bias_sum[j][0], bias_sum[j][1], bias_sum[j][2], bias_sum[j][3]};
+      bias_to[1] = f32x4{bias_sum[j][4], bias_sum[j][5], bias_sum[j][6], bias_sum[j][7]};
+    }
+  }
+}
+
+// The sums of the workgroups, column by column; 64 columns and 16 runs of rows a workgroup.
+constexpr int kColumnRuns = 16;
+__global__ __launch_bounds__(64 * kColumnRuns) void k_norm_columns(const float* partial, float* grad_gain, float* grad_bias, int H,
+                                                                   int groups, int accumulate) {
+  __shared__ float s_sum[kColumnRuns][64];
+  const int lane = threadIdx.x & 63, run = threadIdx.x >> 6;
+  const int column = blockIdx.x * 64 + lane;
+  const bool bias = blockIdx.y != 0;
+  float* to = bias ? grad_bias : grad_gain;
+  const float* from = partial + (bias ? (int64_t)groups * H : 0);
+  float sum = 0.0f;
+  if (column < H) {
+    const int end = (int)((int64_t)groups * (run + 1) / kColumnRuns);
+#pragma unroll 8
+    for (int g = (int)((int64_t)groups * run / kColumnRuns); g < end; ++g) sum += from[(int64_t)g * H + column];
+  }
+  s_sum[run][lane] = sum;
+  __syncthreads();
+  if (run != 0 || column >= H || to == nullptr) return;
+  for (int r = 1; r < kColumnRuns; ++r) sum += s_sum[r][lane];
+  to[column] = accumulate != 0 ? to[column] + sum : sum;
+}
+
+template <bool IN_BF16, bool OUT_BF16, bool CENTRED>
+static hipError_t launch_norm_grad(const NormGradArgs& a, int groups, hipStream_t st) {
+  const int vecs = a.H / 8;
+  int nv = 1;
+  while (nv < 8 && vecs > nv * 512) nv *= 2;
+  const dim3 grid((unsigned)groups), block((unsigned)(((vecs + nv - 1) / nv + 63) / 64 * 64));
+  switch (nv) {
+    case 1: hipLaunchKernelGGL((k_norm_grad<IN_BF16, OUT_BF16, CENTRED, 1>), grid, block, 0, st, a); break;
+    case 2: hipLaunchKernelGGL((k_norm_grad<IN_BF16, OUT_BF16, CENTRED, 2>), grid, block, 0, st, a); break;
+    case 4: hipLaunchKernelGGL((k_norm_grad<IN_BF16, OUT_BF16, CENTRED, 4>), grid, block, 0, st, a); break;
+    default: hipLaunchKernelGGL((k_norm_grad<IN_BF16, OUT_BF16, CENTRED, 8>), grid, block, 0, st, a);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace eep
+
+using namespace eep;
+
+extern "C" {
+
+int eep_layer_norm(const eep_norm_shape* shape, const void* x, const void* residual, const void* gain, const void* bias, void* sum,
+                   void* y, int32_t T, void* stream) {
+  if (!shape || T < 0) return EEP_ERR_INVALID_ARG;
+  const eep_norm_shape& s = *shape;
+  if (s.hidden < 8 || s.hidden > kNormMaxWidth || !f32_or_bf16(s.in_dtype) || !f32_or_bf16(s.gain_dtype) ||
+      !f32_or_bf16(s.out_dtype) || s.scale_group != 0 || !(s.epsilon >= 0.0f))
+    return EEP_ERR_INVALID_ARG;
+  if (s.hidden % 8 != 0) return EEP_ERR_ALIGN;
+  if (T == 0) return EEP_OK;
+  if (!x || !gain || !y) return EEP_ERR_INVALID_ARG;
+  if (!aligned16(x) || !aligned16(residual) || !aligned16(gain) || !aligned16(bias) || !aligned16(sum) || !aligned16(y)) return EEP_ERR_ALIGN;
+  const LayerNormArgs a = {x, residual, gain, bias, sum, y, s.hidden, s.gain_dtype == EEP_BF16, s.epsilon};
+  hipStream_t st = (hipStream_t)stream;
+  const bool in = s.in_dtype == EEP_BF16, out = s.out_dtype == EEP_BF16;
+  const hipError_t e = in ? (out ? launch_layer_norm<true, true>(a, T, st) : launch_layer_norm<true, false>(a, T, st))
+                          : (out ? launch_layer_norm<false, true>(a, T, st) : launch_layer_norm<false, false>(a, T, st));
+  return e == hipSuccess ? EEP_OK : EEP_ERR_HIP;
+}
+
+int eep_norm_grad_create(const eep_norm_grad_config* cfg, eep_norm_grad** out) {
+  if (!out) return EEP_ERR_INVALID_ARG;
+  *out = nullptr;
+  if (!cfg) return EEP_ERR_INVALID_ARG;
+  const eep_norm_grad_config& f = *cfg;
+  if (f.hidden < 8 || f.hidden > kNormMaxWidth || !f32_or_bf16(f.in_dtype) || !f32_or_bf16(f.gain_dtype) ||
+      !f32_or_bf16(f.out_dtype) || (f.centred != 0 && f.centred != 1) || !(f.epsilon >= 0.0f))
+    return EEP_ERR_INVALID_ARG;
+  if (f.hidden % 8 != 0) return EEP_ERR_ALIGN;
+  eep_norm_grad* g = new (std::nothrow) eep_norm_grad();
+  if (!g) return EEP_ERR_INVALID_ARG;
+  g->cfg = f;
+  int device = 0, cus = 0;
+  hipError_t e = hipGetDevice(&device);
+  if (e == hipSuccess) e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, device);
+  g->groups = 2 * cus;
+  if (e == hipSuccess)
+    e = hipMalloc((void**)&g->partial, (size_t)g->groups * f.hidden * sizeof(float) * (f.centred ? 2 : 1));
+  if (e != hipSuccess) {
+    (void)hipGetLastError();
+    delete g;
+    return EEP_ERR_HIP;
+  }
+  *out = g;
+  return EEP_OK;
+}
+
+int eep_norm_grad_destroy(eep_norm_grad* grad) {
+  if (!grad) return EEP_OK;
+  const hipError_t e = hipDeviceSynchronize(), e2 = hipFree(grad->partial);
+  delete grad;
+  return e == hipSuccess && e2 == hipSuccess ? EEP_OK : EEP_ERR_HIP;
+}
+
+int eep_norm_grad_run(eep_norm_grad* grad, const void* h, const void* gain, const void* grad_y, const void* grad_sum, void* grad_h,
+                      float* grad_gain, float* grad_bias, int32_t accumulate, int32_t T, void* stream) {
+  if (!grad || T < 0 || (accumulate != 0 && accumulate != 1)) return EEP_ERR_INVALID_ARG;
+  const eep_norm_grad_config& f = grad->cfg;
+  if ((grad_bias != nullptr && !f.centred) || (!grad_h && !grad_gain && !grad_bias) || (grad_sum != nullptr && grad_h == nullptr))
+    return EEP_ERR_INVALID_ARG;
+  if (T > 0 && (!h || !gain || !grad_y)) return EEP_ERR_INVALID_ARG;
+  if (!aligned16(h) || !aligned16(gain) || !aligned16(grad_y) || !aligned16(grad_sum) || !aligned16(grad_h) || ((uintptr_t)grad_gain & 3u) ||
+      ((uintptr_t)grad_bias & 3u))
+    return EEP_ERR_ALIGN;
+  hipStream_t st = (hipStream_t)stream;
+  const bool columns = grad_gain != nullptr || grad_bias != nullptr;
+  const int groups = T < grad->groups ? T : grad->groups;
+  const NormGradArgs a = {h, gain, grad_y, grad_sum, grad_h, columns ? grad->partial : nullptr, f.hidden, T, f.gain_dtype == EEP_BF16,
+                          f.epsilon};
+  hipError_t e = hipSuccess;
+  if (T > 0) {
+    switch ((f.in_dtype == EEP_BF16) * 4 + (f.out_dtype == EEP_BF16) * 2 + f.centred) {
+      case 0: e = launch_norm_grad<false, false, false>(a, groups, st); break;
+      case 1: e = launch_norm_grad<false, false, true>(a, groups, st); break;
+      case 2: e = launch_norm_grad<false, true, false>(a, groups, st); break;
+      case 3: e = launch_norm_grad<false, true, true>(a, groups, st); break;
+      case 4: e = launch_norm_grad<true, false, false>(a, groups, st); break;
+      case 5: e = launch_norm_grad<true, false, true>(a, groups, st); break;
+      case 6: e = launch_norm_grad<true, true, false>(a, groups, st); break;
+      default: e = launch_norm_grad<true, true, true>(a, groups, st);
+    }
+  }
+  if (e == hipSuccess && columns) {  // (of no rows: zeros)
+    hipLaunchKernelGGL(k_norm_columns, dim3((unsigned)(f.hidden + 63) / 64, f.centred ? 2 : 1), dim3(64 * kColumnRuns), 0, st,
+                       grad->partial, grad_gain, grad_bias, f.hidden, groups, accumulate);
+    e = hipGetLastError();
+  }
+  return e == hipSuccess ? EEP_OK : EEP_ERR_HIP;
+}
+
+}  // extern "C"

@@ -6,6 +6,7 @@
 namespace eep {
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
@@ -52,6 +53,45 @@ __device__ __forceinline__ T fold(T v, Op op) {
     v = op(__builtin_bit_cast(T, low), __builtin_bit_cast(T, high));
   }
   return v;
+}
+
+// Eight neighbouring values of an array, fp32 or bf16.
+template <bool BF16>
+__device__ __forceinline__ void load8(const void* base, int64_t vec, float (&v)[8]) {
+  if constexpr (BF16) {
+    const u32x4 d = ((const u32x4*)base)[vec];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = bf16_lo(d[i]);
+      v[2 * i + 1] = bf16_hi(d[i]);
+    }
+  } else {
+    const f32x4 a = ((const f32x4*)base)[2 * vec], b = ((const f32x4*)base)[2 * vec + 1];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[i] = a[i];
+      v[4 + i] = b[i];
+    }
+  }
+}
+
+template <bool BF16>
+__device__ __forceinline__ void store8(void* base, int64_t vec, const float (&v)[8]) {
+  if constexpr (BF16) {
+    u32x4 d;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) d[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+    __builtin_nontemporal_store(d, &((u32x4*)base)[vec]);
+  } else {
+    __builtin_nontemporal_store(f32x4{v[0], v[1], v[2], v[3]}, &((f32x4*)base)[2 * vec]);
+    __builtin_nontemporal_store(f32x4{v[4], v[5], v[6], v[7]}, &((f32x4*)base)[2 * vec + 1]);
+  }
+}
+
+// The sum over groups of 16 or all 64 lanes, in every lane.
+template <int LANES>
+__device__ __forceinline__ float lane_sum(float v) {
+  return fold<LANES>(v, [](float a, float b) { return a + b; });
 }
 
 // The largest magnitude of N fp32 values as its bits, which are ordered as the values are, NaN above everything.

@@ -1,5 +1,5 @@
-"""The layer around dispatch and combine (include/eep.h): the residual norm with its 8-bit codes, the router's choice,
-the experts' products.  Each class is a shape that was checked once, like `binding.Context`; its `run` queues the
+"""The layer around dispatch and combine (include/eep.h): the residual norm with its 8-bit codes, the layer norm, the
+router's choice, the experts' products, and their gradients.  Each class is a shape that was checked once, like `binding.Context`; its `run` queues the
 call.  Device buffers are torch tensors (or raw integer addresses, such as those of `Context.view_pointers`), bf16 as
 bfloat16 or 16-bit integers, e4m3 codes as float8_e4m3fn or bytes; streams are raw handles or torch streams.
 
@@ -9,6 +9,13 @@ bfloat16 or 16-bit integers, e4m3 codes as float8_e4m3fn or bytes; streams are r
                              gate=True, max_rows=T * k)
     down = layer.ExpertProduct(num_slots=P, in_features=I, out_features=H, x_dtype="fp8", max_rows=T * k)
     logits = layer.ExpertProduct(num_slots=1, in_features=H, out_features=E, y_dtype="f32", max_rows=T)
+
+and for fine-tuning, in bf16 or fp32:
+
+    norm_grad = layer.NormGrad(hidden=H)
+    up_grad = layer.ExpertProductGrad(num_slots=P, in_features=H, out_features=I, gate=True, max_rows=T * k)
+    down_grad = layer.ExpertProductGrad(num_slots=P, in_features=I, out_features=H, max_rows=T * k)
+    router.grad(...)    # and Context.combine_grad, Context.dispatch_grad
 """
 import ctypes
 
@@ -47,6 +54,14 @@ def load():
         sig = {
             "eep_residual_norm": [ctypes.POINTER(_NormShape), vp, vp, vp, vp, vp, vp, vp, i32, vp],
             "eep_route": [ctypes.POINTER(_RouterShape), vp, vp, vp, i32, vp],
+            "eep_layer_norm": [ctypes.POINTER(_NormShape), vp, vp, vp, vp, vp, vp, i32, vp],
+            "eep_route_grad": [ctypes.POINTER(_RouterShape), vp, vp, vp, vp, vp, i32, vp],
+            "eep_norm_grad_create": [vp, ctypes.POINTER(vp)],
+            "eep_norm_grad_destroy": [vp],
+            "eep_norm_grad_run": [vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, vp],
+            "eep_product_grad_create": [vp, ctypes.POINTER(vp)],
+            "eep_product_grad_destroy": [vp],
+            "eep_product_grad_run": [vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, vp],
             "eep_product_create": [ctypes.POINTER(_ProductConfig), ctypes.POINTER(vp)],
             "eep_product_destroy": [vp],
             "eep_expert_product": [vp, vp, vp, vp, vp, vp, vp, vp, i32, vp],
@@ -116,6 +131,10 @@ class Router:
         if rc:
             _refuse(rc, "eep_route", ("shape", "logits", "topk_idx", "topk_w"))
 
+    def grad(self, topk_idx, topk_w, grad_w, grad_logits, T, *, logits=None, stream=None):
+        """eep_route_grad: of what run returned; logits, as run had them, only with over_all."""
+        _backward.route_grad(self, topk_idx, topk_w, grad_w, grad_logits, T, logits, stream)
+
 
 class ExpertProduct:
     """eep_expert_product.  gate: w has the gate's out_features rows, then the other factor's.  slot_stride and
@@ -159,3 +178,7 @@ class ExpertProduct:
             self.destroy()
         except Exception:
             pass
+
+
+from . import _backward  # noqa: E402  (which needs what is above)
+from ._backward import ExpertProductGrad, LayerNorm, NormGrad  # noqa: E402, F401

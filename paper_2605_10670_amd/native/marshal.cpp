@@ -53,11 +53,11 @@ bool stream_of(PyObject* o, uint64_t* out) {
 // call(entry point's address, "kinds of its arguments", arguments...) -> its return code.  Kinds: p a device
 // address (tensor, int or None), i an int32, h a handle as an int, s the stream.  Every argument is of the
 // integer class, so it travels in a 64-bit register or stack slot whatever its width.
-// call_sized(address, kinds, needs, count, arguments...): the same for entry points of up to ten arguments that read and write
+// call_sized(address, kinds, needs, count, arguments...): the same for entry points of up to twelve arguments that read and write
 // tensors of known sizes.  needs: for every p in turn the bytes that it has to hold for each of `count`, or as a negative
 // number for all; what is not a tensor is not looked at.  -(kTooSmall + i) where the i-th argument holds fewer, and
 // nothing is called.  (Host time of a call with the norm's seven tensors: 3.0 us checked in Python, 2.2 here.)
-constexpr int kMost = 9, kMostSized = 10, kTooSmall = 1000;
+constexpr int kMost = 9, kMostSized = 12, kTooSmall = 1000;
 PyObject* call_any(PyObject* const* args, Py_ssize_t nargs, int most, PyObject* needs, PyObject* count) {
   Py_ssize_t n = 0;
   const char* kinds = nargs >= 2 ? PyUnicode_AsUTF8AndSize(args[1], &n) : nullptr;
@@ -116,12 +116,13 @@ PyObject* call_any(PyObject* const* args, Py_ssize_t nargs, int most, PyObject* 
   int code;
   typedef uint64_t U;
   typedef int (*Entry)(U, U, U, U, U, U, U, U, U);
-  typedef int (*LongEntry)(U, U, U, U, U, U, U, U, U, U);
+  typedef int (*LongEntry)(U, U, U, U, U, U, U, U, U, U, U, U);
   Py_BEGIN_ALLOW_THREADS  // (arguments past the entry point's own are not looked at)
   if (n <= kMost)
     code = reinterpret_cast<Entry>(entry)(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8]);
   else
-    code = reinterpret_cast<LongEntry>(entry)(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9]);
+    code = reinterpret_cast<LongEntry>(entry)(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9], a[10],
+                                              a[11]);
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(code);
 }
