@@ -5,6 +5,8 @@
 // memory, a step of 128 bytes' worth of the sum deep, and is turned on the way to the registers: ds_read_b64_tr_b16 gives a lane four
 // values of ONE column from four rows (fp32 values are read one by one).  What a lane holds then is what product.hip's kernels have:
 // lane l has row (column) l % 16 and terms 16 * (l / 16) bytes into each half step.
+#include <math.h>
+
 #include <new>
 #include <type_traits>
 
@@ -79,8 +81,8 @@ __global__ __launch_bounds__(256) void k_gate_grad(GateGradArgs a, int64_t first
 // weights' rows) or weight rows (OF_W: the weights' gradient, summed over a slot's tokens).
 //
 // As in product.hip the in_features are the matrix cores' rows, so that a lane has four neighbouring ones of one row of the
-// result.  Eight wavefronts; every step's operands come through LDS by direct loads, a step ahead, past the end of a tile into the
-// next one's first step.
+// result.  Eight wavefronts; the steps of all tiles are one stream, of which some are under way to LDS while one is
+// multiplied, and the operands that a step begins with are read while the one before ends.
 // ---------------------------------------------------------------------------
 struct TileArgs {
   const uint8_t *g, *other;  // g: of the sums; other: the weights, or the rows x
@@ -94,17 +96,70 @@ struct TileArgs {
   int accumulate;
 };
 
-constexpr int kGradWaves = 8, kGradCols = 256;
-constexpr int grad_across(int tt) { return tt == 4 ? 2 : 4; }  // wavefronts side by side on the columns
-constexpr int grad_lds_bytes(int tt) { return 2 * (kGradCols + 64 * tt) * kStepBytes; }
+constexpr int kGradCols = 256, kGradStep = 64;  // bytes along the sum
+constexpr int grad_waves(int tt) { return tt == 4 ? 8 : 4; }
+constexpr int grad_across(int tt) { return tt == 1 ? 4 : 2; }  // wavefronts side by side on the columns
+constexpr int grad_stages(int tt) { return tt == 2 ? 3 : 4; }
+constexpr int grad_stage_bytes(int tt) { return (kGradCols + 64 * tt) * kGradStep; }
+constexpr int grad_lds_bytes(int tt) { return grad_stages(tt) * grad_stage_bytes(tt); }
+constexpr int grad_per_cu(int tt) { return tt == 4 ? 1 : 2; }  // workgroups
+
+// One step of 16 rows (columns): lane l has four dwords of row l % 16, terms from 16 * (l / 16) bytes on.
+template <int DT>
+__device__ __forceinline__ f32x4 mma_step(const u32x4& a, const u32x4& b, f32x4 acc) {
+  if constexpr (DT == EEP_BF16) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[i]), __uint_as_float(b[i]), acc, 0, 0, 0);
+    return acc;
+  }
+}
+
+// 16 bytes a lane from `offset` behind base, into LDS: the lanes' one behind the other.  The compiler, which cannot tell the turning
+// reads of one stage from the loads into another, waits for its own loads of this kind before every such read; it does not know of
+// these, and the kernel waits for them itself.  (The distance is that between a vector instruction that wrote a scalar register
+// and the load that reads it, which is not kept for asm either.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"  // (m0 on the clobber list: nothing else here uses it)
+__device__ __forceinline__ void load_to_lds(const uint8_t* base, uint32_t offset, uint32_t to) {
+  const uint32_t at = __builtin_amdgcn_readfirstlane(to);
+  const uint32_t low = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)base);
+  const uint32_t high = __builtin_amdgcn_readfirstlane((uint32_t)((uintptr_t)base >> 32));
+  const uint64_t from = (uint64_t)high << 32 | low;
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(offset), "s"(from) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+// 16 bytes a lane to `offset` behind base: one store, whatever the compiler makes of what is around it.  (The distances are those
+// to the scalar registers before it and from its data, as rows.hpp has them.)
+__device__ __forceinline__ void store_counted(uint8_t* base, uint32_t offset, u32x4 v) {
+  const uint32_t low = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)base);
+  const uint32_t high = __builtin_amdgcn_readfirstlane((uint32_t)((uintptr_t)base >> 32));
+  const uint64_t to = (uint64_t)high << 32 | low;
+  asm volatile("s_nop 4\n\tglobal_store_dwordx4 %0, %1, %2 nt\n\ts_nop 1" ::"v"(offset), "v"(v), "s"(to) : "memory");
+}
+
+// 64 bytes each of 16 rows in p, lane l a piece of row l % 16, and the next 64 of them in q: afterwards p has 128 of the first
+// eight rows and q of the last.  (With stores of 64 bytes of a row, and these not non-temporal: 144 slots of 1024 x 4096 bf16
+// of 512 rows 243 us, now 202.)
+__device__ __forceinline__ void whole_lines(u32x4& p, u32x4& q) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t a = p[i], b = q[i];  // lanes 8 away change places, in the upper half of a row of lanes, then in the lower
+    p[i] = __builtin_amdgcn_update_dpp(a, b, 0x128, 0xf, 0xc, false);
+    q[i] = __builtin_amdgcn_update_dpp(b, a, 0x128, 0xf, 0x3, false);
+  }
+}
 
 // An operand that lies across the sum: rows of COLS values, in LDS one behind the other.  Its 16-byte chunks change places within a
 // row, by a number that differs between the rows that are read at a time, so that these do not meet in the banks.
-template <int DT, int COLS>
+template <int DT, int COLS, int WAVES>
 struct Across {
-  static constexpr int kSize = DT == EEP_BF16 ? 2 : 4, kDepth = kStepBytes / kSize;
+  static constexpr int kSize = DT == EEP_BF16 ? 2 : 4, kDepth = kGradStep / kSize;
   static constexpr int kRowBytes = COLS * kSize, kChunks = kRowBytes / 16;
-  static constexpr int kLoads = kDepth * kRowBytes / 1024 / kGradWaves;  // a wavefront's, of 1 KiB
+  static constexpr int kLoads = kDepth * kRowBytes / 1024 / WAVES;  // a wavefront's, of 1 KiB
   static_assert(kChunks >= 16 && kLoads >= 1, "");
   __device__ __forceinline__ static int places(int row) {
     return DT == EEP_BF16 ? 2 * ((row & 3) | ((row >> 1) & 4)) : 4 * ((row >> 2) & 3);
@@ -117,76 +172,56 @@ struct Across {
     return ((lane % kChunks) ^ places(row(wave, lane, i))) * (16 / kSize);
   }
   // 16 columns from `tile` * 16 on.
-  __device__ __forceinline__ static Frag read(const uint8_t* lds, int lane, int tile) {
+  __device__ __forceinline__ static u32x4 read(const uint8_t* lds, int lane, int tile) {
     const int part = lane >> 4;
-    Frag f;
+    u32x4 f;
     if constexpr (DT == EEP_BF16) {
       typedef int16_t i16x4 __attribute__((ext_vector_type(4)));
       typedef __attribute__((address_space(3))) i16x4 lds_quad;
       const int row = 8 * part + ((lane >> 2) & 3);
       const uint8_t* from = lds + row * kRowBytes + (((2 * tile + ((lane >> 1) & 1)) ^ places(row)) << 4) + (lane & 1) * 8;
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const u32x2 d = __builtin_bit_cast(
-              u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_quad*)(from + (32 * j + 4 * h) * kRowBytes)));
-          f.c[j][2 * h] = d[0];
-          f.c[j][2 * h + 1] = d[1];
-        }
+      for (int h = 0; h < 2; ++h) {
+        const u32x2 d =
+            __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_quad*)(from + 4 * h * kRowBytes)));
+        f[2 * h] = d[0];
+        f[2 * h + 1] = d[1];
+      }
     } else {
       const uint8_t* from =
           lds + 4 * part * kRowBytes + (((4 * tile + ((lane >> 2) & 3)) ^ places(4 * part)) << 4) + (lane & 3) * 4;
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) f.c[j][i] = *(const uint32_t*)(from + (16 * j + i) * kRowBytes);
+      for (int i = 0; i < 4; ++i) f[i] = *(const uint32_t*)(from + i * kRowBytes);
     }
     return f;
   }
 };
 
-// 16 bytes a lane from `offset` behind base, into LDS: the lanes' one behind the other.  The compiler, which cannot tell the turning
-// reads of one stage from the loads into another, waits for its own loads of this kind before every such read; it does not know of
-// these, and the kernel waits for them itself.  (The distance is that between a vector instruction that wrote a scalar register
-// and the load that reads it, which is not kept for asm either.)
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"  // (m0 on the clobber list: nothing else here uses it)
-__device__ __forceinline__ void load_to_lds(const uint8_t* base, uint32_t offset, uint8_t* to) {
-  const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void*)to);
-  const uint32_t low = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)base);
-  const uint32_t high = __builtin_amdgcn_readfirstlane((uint32_t)((uintptr_t)base >> 32));
-  const uint64_t from = (uint64_t)high << 32 | low;
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(offset), "s"(from) : "memory", "m0");
-}
-#pragma clang diagnostic pop
-
 // Zeros in the place of the terms from `left` on.
 template <int DT>
-__device__ __forceinline__ void cut(Frag& f, int part, int left) {
+__device__ __forceinline__ void cut(u32x4& f, int part, int left) {
 #pragma unroll
-  for (int j = 0; j < 2; ++j)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (DT == EEP_BF16) {
-        const int term = 32 * j + 8 * part + 2 * i;
-        f.c[j][i] &= term + 1 < left ? 0xffffffffu : term < left ? 0xffffu : 0u;
-      } else {
-        f.c[j][i] = 16 * j + 4 * part + i < left ? f.c[j][i] : 0u;
-      }
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (DT == EEP_BF16) {
+      const int term = 8 * part + 2 * i;
+      f[i] &= term + 1 < left ? 0xffffffffu : term < left ? 0xffffu : 0u;
+    } else {
+      f[i] = 4 * part + i < left ? f[i] : 0u;
     }
+  }
 }
 
 template <int DT, int OT, bool OF_W, int TT>
-__global__ __launch_bounds__(64 * kGradWaves, 2) void k_grad_tiled(TileArgs a) {
-  constexpr int kWM = grad_across(TT), kWN = kGradWaves / kWM;
+__global__ __launch_bounds__(64 * grad_waves(TT), 2) void k_grad_tiled(TileArgs a) {
+  constexpr int kWaves = grad_waves(TT), kWM = grad_across(TT), kWN = kWaves / kWM;
   constexpr int kA = kGradCols / 16 / kWM, kB = 4 * TT / kWN;  // tiles of 16 columns and of 16 rows a wavefront
-  constexpr int kRows = 64 * TT;
-  typedef Across<DT, kGradCols> Other;
-  typedef Across<DT, OF_W ? kRows : kGradCols> Grads;  // (where they lie across too)
+  constexpr int kRows = 64 * TT, kStages = grad_stages(TT), kStage = grad_stage_bytes(TT);
+  typedef Across<DT, kGradCols, kWaves> Other;
+  typedef Across<DT, OF_W ? kRows : kGradCols, kWaves> Grads;  // (where they lie across too)
   constexpr int kSize = Other::kSize, kDepth = Other::kDepth;
-  constexpr int kOtherStage = kGradCols * kStepBytes, kStage = kOtherStage + kRows * kStepBytes;
-  constexpr int kLoads = kRows / 8 / kGradWaves;  // of g where its rows lie along the sum: 8 rows each
+  constexpr int kOtherStage = kGradCols * kGradStep;
+  constexpr int kGradLoads = OF_W ? Grads::kLoads : kRows / 16 / kWaves;  // of g, a wavefront's; 16 rows each where they lie along
+  constexpr int kLoads = Other::kLoads + kGradLoads;  // of a step
   extern __shared__ __align__(1024) uint8_t lds[];
 
   const int lane = threadIdx.x & 63;
@@ -195,7 +230,7 @@ __global__ __launch_bounds__(64 * kGradWaves, 2) void k_grad_tiled(TileArgs a) {
   const int col = lane & 15, part = lane >> 4;
 
   struct Tile {
-    int slot, column0, row0, first, end, steps;  // row0: of the result; first, end: the slot's rows (OF_W) or the tile's
+    int slot, column0, row0, first, end, terms;  // row0: of the result; first, end: the slot's rows (OF_W) or the tile's
   };
   TileMap<kRows> map;
   int64_t items, per_slot = 0;
@@ -206,11 +241,11 @@ __global__ __launch_bounds__(64 * kGradWaves, 2) void k_grad_tiled(TileArgs a) {
     map.make(a);
     items = (int64_t)map.total * a.feature_tiles;
   }
-  // The items go to the XCDs in turn, 32 neighbouring ones at a time (as many as one has CUs), which share rows of the
+  // The items go to the XCDs in turn, as many neighbouring ones at a time as one has workgroups, which share rows of the
   // operands in its L2.
   const int xcds = gridDim.x % 8 == 0 ? 8 : 1;
-  const int xcd = blockIdx.x % xcds, seat = blockIdx.x / xcds, seats = gridDim.x / xcds;
-  const auto item_of = [&](int64_t turn) { return turn / seats * seats * xcds + (int64_t)xcd * seats + turn % seats; };
+  const int xcd = blockIdx.x % xcds, seats = gridDim.x / xcds;
+  const int64_t first_item = (int64_t)xcd * seats + blockIdx.x / xcds;
   const auto find = [&](int64_t item) {
     Tile t;
     if constexpr (OF_W) {
@@ -224,193 +259,300 @@ __global__ __launch_bounds__(64 * kGradWaves, 2) void k_grad_tiled(TileArgs a) {
       t.first = 0;
       t.end = a.rows;
       if (a.offset != nullptr) {
-        t.first = clamp_row(a.offset[t.slot], a.rows);
-        t.end = clamp_row(a.offset[t.slot + 1], a.rows);
+        // (scalar loads, for which nothing but themselves is awaited)
+        const auto* offset = (const __attribute__((address_space(4))) int32_t*)a.offset;
+        t.first = clamp_row(offset[t.slot], a.rows);
+        t.end = clamp_row(offset[t.slot + 1], a.rows);
       }
-      t.steps = t.end > t.first ? (t.end - t.first + kDepth - 1) / kDepth : 0;
+      t.terms = t.end > t.first ? t.end - t.first : 0;
     } else {
       int feature_tile;
       map.find(a, item, &t.slot, &feature_tile, &t.first, &t.end);
       t.column0 = feature_tile * kGradCols;
       t.row0 = t.first;
-      t.steps = (a.n + kDepth - 1) / kDepth;
+      t.terms = a.n;
     }
     return t;
   };
 
   const int64_t k_bytes = (int64_t)a.k * kSize, n_bytes = (int64_t)a.n * kSize;
-  // what the lane loads of g where its rows lie along the sum: 16 bytes of row `lane / 8` of eight
-  const int load_row = lane >> 3, load_chunk = (lane & 7) ^ load_row;
-  const auto fetch = [&](const Tile& t, int step, uint8_t* stage) {
-    const int64_t at = (int64_t)step * kDepth;
-    // terms past the end are read as the last ones, and cut off in the registers; columns likewise, and not stored
-    const int left = (int)((OF_W ? t.end - t.first : a.n) - at);
-    const uint8_t* other = OF_W ? a.other + (t.first + at) * k_bytes : a.other + t.slot * a.stride + at * k_bytes;
+  // what the lane loads of g where its rows lie along the sum: 16 bytes of row `lane / 4` of 16
+  const int load_row = lane >> 2, load_chunk = (lane & 3) ^ ((load_row >> 2) & 3);
+
+  // The stream of steps: the tile that is fetched, its terms left, where its operands are and the lane's places there.
+  int64_t fetch_item = first_item;
+  int fetch_left = 0;
+  const uint8_t *other_at = nullptr, *grads_at[kGradLoads] = {};
+  uint32_t other_off[Other::kLoads] = {}, grads_off[kGradLoads] = {};
+  int stage_at = 0;  // of the next fetch
+  const uint32_t lds_base = (uint32_t)(uintptr_t)(lds_void*)lds;
+  // (terms past the end are read as the last ones, and cut off in the registers; columns likewise, and not stored)
+  const auto aim = [&](const Tile& t) {
+    fetch_left = t.terms;
+    other_at = OF_W ? a.other + t.first * k_bytes : a.other + t.slot * a.stride;
+    other_at += (int64_t)t.column0 * kSize;
 #pragma unroll
     for (int i = 0; i < Other::kLoads; ++i) {
-      int r = Other::row(wave, lane, i), c = t.column0 + Other::column(wave, lane, i);
-      r = r < left ? r : left - 1;
-      c = c < a.k ? c : a.k - 16 / kSize;
-      load_to_lds(other, (uint32_t)r * (uint32_t)k_bytes + (uint32_t)c * kSize, stage + (wave * Other::kLoads + i) * 1024);
+      const int r = Other::row(wave, lane, i), c = Other::column(wave, lane, i), most = a.k - t.column0 - 16 / kSize;
+      other_off[i] = (uint32_t)r * (uint32_t)k_bytes + (uint32_t)(c < most ? c : most) * kSize;
     }
     if constexpr (OF_W) {
-      const uint8_t* grads = a.g + (t.first + at) * n_bytes;
 #pragma unroll
-      for (int i = 0; i < Grads::kLoads; ++i) {
-        int r = Grads::row(wave, lane, i), c = t.row0 + Grads::column(wave, lane, i);
-        r = r < left ? r : left - 1;
-        c = c < a.n ? c : a.n - 16 / kSize;
-        load_to_lds(grads, (uint32_t)r * (uint32_t)n_bytes + (uint32_t)c * kSize,
-                    stage + kOtherStage + (wave * Grads::kLoads + i) * 1024);
+      for (int i = 0; i < kGradLoads; ++i) {
+        const int r = Grads::row(wave, lane, i), c = Grads::column(wave, lane, i), most = a.n - t.row0 - 16 / kSize;
+        grads_at[i] = a.g + t.first * n_bytes + (int64_t)t.row0 * kSize;
+        grads_off[i] = (uint32_t)r * (uint32_t)n_bytes + (uint32_t)(c < most ? c : most) * kSize;
       }
     } else {
-      const uint8_t* grads = a.g + t.first * n_bytes + at * kSize;
-      const int chunk = load_chunk * (16 / kSize) < left ? load_chunk : 0;
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        // (eight rows at a time are within 32 bits, all of them may not be)
-        const int r0 = (wave * kLoads + i) * 8, most = t.end - 1 - t.first;
+      for (int i = 0; i < kGradLoads; ++i) {
+        // (16 rows at a time are within 32 bits, all of them may not be)
+        const int r0 = (wave * kGradLoads + i) * 16, most = t.end > t.first ? t.end - 1 - t.first : 0;
         const int from = r0 < most ? r0 : most, r = r0 + load_row < most ? r0 + load_row : most;
-        load_to_lds(grads + from * n_bytes, (uint32_t)(r - from) * (uint32_t)n_bytes + chunk * 16,
-                    stage + kOtherStage + (wave * kLoads + i) * 1024);
+        grads_at[i] = a.g + (t.first + from) * n_bytes;
+        grads_off[i] = (uint32_t)(r - from) * (uint32_t)n_bytes + load_chunk * 16;
       }
     }
   };
-  const int read_at = col * kStepBytes + ((part ^ (col & 7)) << 4);
+  bool more = true;
+  const auto fetch = [&]() {
+    // (behind the stream's end nothing new: the last step again, so that as many loads are under way as ever)
+    if (fetch_left <= 0 && more) {
+      for (;;) {
+        fetch_item += gridDim.x;
+        if (fetch_item >= items) {
+          more = false;
+          break;
+        }
+        const Tile t = find(fetch_item);
+        if (t.terms == 0) continue;
+        aim(t);
+        break;
+      }
+    }
+    if (other_at == nullptr) return;  // (no tile has terms)
+    const uint32_t to = lds_base + stage_at * kStage + wave * 1024;
+    const bool again = !more && fetch_left <= 0;
+    if (!again && fetch_left < kDepth) {
+#pragma unroll
+      for (int i = 0; i < Other::kLoads; ++i) {
+        const int r = Other::row(wave, lane, i), last = fetch_left - 1;
+        if (r > last) other_off[i] -= (uint32_t)(r - last) * (uint32_t)k_bytes;
+      }
+#pragma unroll
+      for (int i = 0; i < kGradLoads; ++i) {
+        if constexpr (OF_W) {
+          const int r = Grads::row(wave, lane, i), last = fetch_left - 1;
+          if (r > last) grads_off[i] -= (uint32_t)(r - last) * (uint32_t)n_bytes;
+        } else if (load_chunk * (16 / kSize) >= fetch_left) {
+          grads_off[i] -= load_chunk * 16;
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < Other::kLoads; ++i) load_to_lds(other_at, other_off[i], to + wave * (Other::kLoads - 1) * 1024 + i * 1024);
+#pragma unroll
+    for (int i = 0; i < kGradLoads; ++i)
+      load_to_lds(grads_at[i], grads_off[i], to + kOtherStage + wave * (kGradLoads - 1) * 1024 + i * 1024);
+    stage_at = stage_at + 1 < kStages ? stage_at + 1 : 0;
+    if (!again) {
+      fetch_left -= kDepth;
+      if (fetch_left > 0) {
+        other_at += kDepth * k_bytes;
+#pragma unroll
+        for (int i = 0; i < kGradLoads; ++i) grads_at[i] += OF_W ? kDepth * n_bytes : kGradStep;
+      }
+    }
+  };
+  const int read_at = col * kGradStep + ((part ^ ((col >> 2) & 3)) << 4);
   const auto read_other = [&](const uint8_t* stage, int f) { return Other::read(stage, lane, wm * kA + f); };
   const auto read_grads = [&](const uint8_t* stage, int j) {
-    if constexpr (OF_W) {
+    if constexpr (OF_W)
       return Grads::read(stage + kOtherStage, lane, wn * kB + j);
-    } else {
-      Frag f;
-      const uint8_t* from = stage + kOtherStage + (wn * kB + j) * 16 * kStepBytes;
-      f.c[0] = *(const u32x4*)(from + read_at);
-      f.c[1] = *(const u32x4*)(from + (read_at ^ 64));
-      return f;
-    }
+    else
+      return *(const u32x4*)(stage + kOtherStage + (wn * kB + j) * 16 * kGradStep + read_at);
   };
 
-  int64_t turn = seat;
-  int64_t item = item_of(turn);
-  if (item >= items) return;
-  Tile t = find(item);
-  uint8_t *stage = lds, *following = lds + kStage;
-  bool fetched = false;
-  for (;;) {
-    if (!fetched && t.steps > 0) fetch(t, 0, stage);
-    fetched = false;
-    const int64_t next_item = item_of(turn + seats);
-    const bool more = next_item < items;
-    Tile next = t;
-    if (more) next = find(next_item);
+  if (first_item >= items) return;
+  // the first tile that has terms at all
+  fetch_item = first_item - (int64_t)gridDim.x;
+#pragma unroll
+  for (int s = 0; s < kStages; ++s) fetch();
+  const uint8_t* stage = lds;
+  // What a step begins with: all of g's operands, the first ones of the other.
+  constexpr int kAhead = 3;
+  u32x4 b_head[kB], a_head[kAhead];
+  const auto read_heads = [&]() {
+    a_head[0] = read_other(stage, 0);
+#pragma unroll
+    for (int j = 0; j < kB; ++j) b_head[j] = read_grads(stage, j);
+#pragma unroll
+    for (int f = 1; f < kAhead; ++f) a_head[f] = read_other(stage, f);
+  };
+  const bool any = other_at != nullptr;
+  if (any) {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kStages - 1) * kLoads) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    read_heads();
+  }
+
+  constexpr int kStores = kA * kB / (OT == EEP_F32 ? 1 : 2);  // of a whole tile, a wavefront's
+  static_assert((kStages - 2) * kLoads + kStores < 64, "what the counter holds");
+  int behind_stores = kStages;  // steps since a whole tile was stored
+  for (int64_t item = first_item; item < items; item += gridDim.x) {
+    const Tile t = find(item);
     f32x4 acc[kA][kB];
 #pragma unroll
     for (int f = 0; f < kA; ++f)
 #pragma unroll
       for (int j = 0; j < kB; ++j) acc[f][j] = f32x4{0, 0, 0, 0};
-    const int whole = OF_W ? (t.end > t.first ? (t.end - t.first) / kDepth : 0) : a.n / kDepth;
-    const int left = OF_W ? t.end - t.first - whole * kDepth : a.n - whole * kDepth;
-    const auto step = [&](int s, auto is_cut) {
-      // This step's rows are there, and all wavefronts are done with the step before, whose place the next ones take.
-      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    const auto step = [&](int left, auto is_cut) {
+      const auto ready = [&](u32x4 f) {
+        if constexpr (decltype(is_cut)::value) cut<DT>(f, part, left);
+        return f;
+      };
+      u32x4 b[kB], v[kA];
+#pragma unroll
+      for (int j = 0; j < kB; ++j) b[j] = ready(b_head[j]);
+#pragma unroll
+      for (int f = 0; f < kAhead; ++f) v[f] = a_head[f];
+      const auto multiply = [&](int f) {
+        const u32x4 now = ready(v[f]);
+#pragma unroll
+        for (int j = 0; j < kB; ++j) acc[f][j] = mma_step<DT>(now, b[j], acc[f][j]);
+        __builtin_amdgcn_sched_barrier(0);
+      };
+#pragma unroll
+      for (int f = 0; f < kA - 2; ++f) {
+        if (f + kAhead < kA) v[f + kAhead] = read_other(stage, f + kAhead);
+        multiply(f);
+      }
+      // This wavefront has read all it needs of the stage.  Once all have, and the next step's rows are there (no more than
+      // the fetches behind them are under way), the stage may be filled again and the next step's first operands are read.
+      // (Loads and stores count together, in order: the last tile's stores are newer than the rows of the next kStages - 1 steps.)
+      if (behind_stores < kStages - 1)
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kStages - 2) * kLoads + kStores) : "memory");
+      else
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kStages - 2) * kLoads) : "memory");
+      ++behind_stores;
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
-      if (s + 1 < t.steps) {
-        fetch(t, s + 1, following);
-      } else if (more && next.steps > 0) {
-        fetch(next, 0, following);
-        fetched = true;
-      }
-      Frag b[kB];
-#pragma unroll
-      for (int j = 0; j < kB; ++j) {
-        b[j] = read_grads(stage, j);
-        if constexpr (decltype(is_cut)::value) cut<DT>(b[j], part, left);
-      }
-#pragma unroll
-      for (int f = 0; f < kA; ++f) {
-        Frag v = read_other(stage, f);
-        if constexpr (decltype(is_cut)::value) cut<DT>(v, part, left);
-#pragma unroll
-        for (int j = 0; j < kB; ++j) acc[f][j] = mma<DT>(v, b[j], acc[f][j]);
-      }
-      uint8_t* other = stage;
-      stage = following;
-      following = other;
+      stage = stage + kStage < lds + kStages * kStage ? stage + kStage : lds;
+      read_heads();
+      fetch();
+      multiply(kA - 2);
+      multiply(kA - 1);
     };
-    for (int s = 0; s < whole; ++s) step(s, std::false_type());
-    if (t.steps > whole) step(whole, std::true_type());
+    int left = t.terms;
+    for (; left >= kDepth; left -= kDepth) step(left, std::false_type());
+    if (left > 0) step(left, std::true_type());
 
     const int rows_end = OF_W ? a.n : t.end;
     uint8_t* out = OF_W ? a.out + t.slot * a.stride : a.out;
     const int n0 = t.column0 + wm * (kA * 16);
+    if (OF_W && a.accumulate != 0 && t.terms == 0) continue;  // (nothing to add)
+    constexpr int kOut = OT == EEP_F32 ? 4 : 2;
+    if (OF_W && a.accumulate != 0) {
 #pragma unroll
-    for (int j = 0; j < kB; ++j) {
-      const int64_t row = (int64_t)t.row0 + (wn * kB + j) * 16 + col;
-      const bool in = row < rows_end;
-      if constexpr (OF_W) {
-        if (a.accumulate != 0) {
-          if (t.steps == 0) continue;  // (nothing to add)
-#pragma unroll
-          for (int f = 0; f < kA; ++f) {
-            const int n = n0 + f * 16 + part * 4;
-            if (!in || n >= a.k) continue;
-            if constexpr (OT == EEP_F32) {
-              acc[f][j] += *(const f32x4*)(out + (row * a.k + n) * 4);
-            } else {
-              const u32x2 d = *(const u32x2*)(out + (row * a.k + n) * 2);
-              acc[f][j] += f32x4{bf16_lo(d[0]), bf16_hi(d[0]), bf16_lo(d[1]), bf16_hi(d[1])};
-            }
-          }
-        }
-      }
-      if constexpr (OT == EEP_BF16) {
-#pragma unroll
-        for (int f = 0; f < kA; f += 2) store_tiles(out, row, a.k, n0 + f * 16, part, in, acc[f][j], acc[f + 1][j]);
-      } else {
+      for (int j = 0; j < kB; ++j) {
+        const int64_t row = (int64_t)t.row0 + (wn * kB + j) * 16 + col;
 #pragma unroll
         for (int f = 0; f < kA; ++f) {
           const int n = n0 + f * 16 + part * 4;
-          const float v[4] = {acc[f][j][0], acc[f][j][1], acc[f][j][2], acc[f][j][3]};
-          if (in && n < a.k) store4<OT>(out, row * a.k + n, v);
+          if (row >= rows_end || n >= a.k) continue;
+          uint8_t* to = out + (row * a.k + n) * kOut;
+          if constexpr (OT == EEP_F32) {
+            *(f32x4*)to = acc[f][j] + *(const f32x4*)to;
+          } else {
+            const u32x2 d = *(const u32x2*)to;
+            *(u32x2*)to = u32x2{pack_bf16x2(acc[f][j][0] + bf16_lo(d[0]), acc[f][j][1] + bf16_hi(d[0])),
+                                pack_bf16x2(acc[f][j][2] + bf16_lo(d[1]), acc[f][j][3] + bf16_hi(d[1]))};
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      behind_stores = kStages;
+      continue;
+    }
+    // A whole tile is stored by a number of stores that the steps behind them count on.
+    const auto store = [&](auto is_whole) {
+      constexpr bool kWhole = decltype(is_whole)::value;
+      constexpr int kPiece = OT == EEP_F32 ? 1 : 2;  // tiles of 16 columns that make 64 bytes of a row
+      uint8_t* base = out + ((int64_t)t.row0 * a.k + n0) * kOut;
+      uint8_t* base8 = base + (int64_t)8 * a.k * kOut;
+#pragma unroll
+      for (int j = 0; j < kB; ++j) {
+        const int row = (wn * kB + j) * 16 + (col & 7);
+        const uint32_t in_row = (col >> 3) * 64 + (OT == EEP_F32 ? part * 16 : (part & 1) * 32 + (part >> 1) * 16);
+        const uint32_t at = (uint32_t)row * (uint32_t)a.k * kOut + in_row;
+#pragma unroll
+        for (int f = 0; f < kA; f += 2 * kPiece) {
+          u32x4 p[2];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if constexpr (OT == EEP_F32)
+              p[h] = __builtin_bit_cast(u32x4, acc[f + h][j]);
+            else
+              p[h] = side_by_side(acc[f + 2 * h][j], acc[f + 2 * h + 1][j]);
+          }
+          whole_lines(p[0], p[1]);
+          const bool in = kWhole || n0 + f * 16 + (int)(in_row / kOut) < a.k;
+          if (in && (kWhole || t.row0 + row < rows_end)) store_counted(base, at + f * 16 * kOut, p[0]);
+          if (in && (kWhole || t.row0 + row + 8 < rows_end)) store_counted(base8, at + f * 16 * kOut, p[1]);
         }
       }
+    };
+    if (t.row0 + kRows <= rows_end && t.column0 + kGradCols <= a.k) {
+      store(std::true_type());
+      behind_stores = 0;
+    } else {
+      store(std::false_type());
+      behind_stores = kStages;
     }
-    if (!more) break;
-    turn += seats;
-    item = next_item;
-    t = next;
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // nothing may still write to LDS when the workgroup is gone
 }
 
 template <int DT, int OT, bool OF_W, int TT>
 static hipError_t launch_grad_tiled(const TileArgs& a, int64_t work, int cus, hipStream_t st) {
-  hipLaunchKernelGGL((k_grad_tiled<DT, OT, OF_W, TT>), dim3((unsigned)(work < cus ? work : cus)), dim3(64 * kGradWaves),
+  const int64_t most = (int64_t)cus * grad_per_cu(TT);
+  hipLaunchKernelGGL((k_grad_tiled<DT, OT, OF_W, TT>), dim3((unsigned)(work < most ? work : most)), dim3(64 * grad_waves(TT)),
                      grad_lds_bytes(TT), st, a);
   return hipGetLastError();
+}
+
+// What the tiles of 64 * tt tokens cost, in time: what a step of one takes (us), as often as a CU has one.  A slot's last tile is half
+// empty on average.  Where there are two workgroups to a CU, a step of both.
+static float grad_x_cost(int tt, int64_t rows, int64_t slots, int64_t feature_tiles, int cus) {
+  const int64_t touched = rows < slots ? rows : slots;
+  float tiles = (float)rows / touched / (64 * tt) + 0.5f;
+  if (touched == 1) tiles = (float)((rows + 64 * tt - 1) / (64 * tt));
+  const float rounds = (tiles < 1.0f ? 1.0f : tiles) * touched * feature_tiles / (cus * grad_per_cu(tt));
+  const float step = tt == 4 ? 0.8f : tt == 2 ? 1.06f : 0.55f;
+  if (grad_per_cu(tt) == 2 && rounds <= 0.5f) return tt == 2 ? 0.62f : 0.4f;
+  return step * (rounds < 4.0f ? ceilf(rounds) : rounds);
 }
 
 template <int DT>
 static hipError_t launch_grad_x(TileArgs a, int cus, hipStream_t st) {
   a.feature_tiles = (a.k + kGradCols - 1) / kGradCols;
   const int64_t touched = a.rows < a.slots ? a.rows : a.slots;
-  const auto work = [&](int tokens) { return (a.rows + touched * (tokens - 1)) / tokens * a.feature_tiles; };
-  const int mean = (int)((a.rows + a.slots - 1) / a.slots);
-  if (mean <= 64) return launch_grad_tiled<DT, DT, false, 1>(a, work(64), cus, st);
-  if (mean <= 128) return launch_grad_tiled<DT, DT, false, 2>(a, work(128), cus, st);
-  return launch_grad_tiled<DT, DT, false, 4>(a, work(256), cus, st);
+  const auto tiled = [&](auto tt) {
+    constexpr int TT = decltype(tt)::value;
+    return launch_grad_tiled<DT, DT, false, TT>(a, (a.rows + touched * (64 * TT - 1)) / (64 * TT) * a.feature_tiles, cus, st);
+  };
+  const float one = grad_x_cost(1, a.rows, a.slots, a.feature_tiles, cus), two = grad_x_cost(2, a.rows, a.slots, a.feature_tiles, cus),
+              four = grad_x_cost(4, a.rows, a.slots, a.feature_tiles, cus);
+  if (four <= one && four <= two) return tiled(std::integral_constant<int, 4>());
+  return two <= one ? tiled(std::integral_constant<int, 2>()) : tiled(std::integral_constant<int, 1>());
 }
 
 template <int DT, int OT>
 static hipError_t launch_grad_w(TileArgs a, int cus, hipStream_t st) {
   a.feature_tiles = (a.k + kGradCols - 1) / kGradCols;
-  const auto tiled = [&](auto tt) {
-    constexpr int TT = decltype(tt)::value;
-    a.row_tiles = (a.n + 64 * TT - 1) / (64 * TT);
-    return launch_grad_tiled<DT, OT, true, TT>(a, (int64_t)a.row_tiles * a.feature_tiles * a.slots, cus, st);
-  };
-  return tiled(std::integral_constant<int, 4>());
+  a.row_tiles = (a.n + 255) / 256;
+  return launch_grad_tiled<DT, OT, true, 4>(a, (int64_t)a.row_tiles * a.feature_tiles * a.slots, cus, st);
 }
 
 // More LDS than a kernel may have by default, on the current device.

@@ -44,13 +44,19 @@ __device__ __forceinline__ void store4(uint8_t* y, int64_t element, const float 
 }
 
 // Two tiles of 16 features side by side, of which a lane has four neighbouring ones each, as bf16: rows of lanes exchange halves,
-// and each stores 16 bytes, so that a row of y gets 64 at once.  n: the first of the 32 features.
-__device__ __forceinline__ void store_tiles(uint8_t* y, int64_t row, int features, int n, int part, bool in_rows,
-                                            const f32x4& a, const f32x4& b) {
+// so that each has 16 bytes, the lanes of a row 64 at once: of feature (part & 1) * 16 + (part >> 1) * 8 on.
+__device__ __forceinline__ u32x4 side_by_side(const f32x4& a, const f32x4& b) {
   const auto low = __builtin_amdgcn_permlane16_swap(pack_bf16x2(a[0], a[1]), pack_bf16x2(b[0], b[1]), false, false);
   const auto high = __builtin_amdgcn_permlane16_swap(pack_bf16x2(a[2], a[3]), pack_bf16x2(b[2], b[3]), false, false);
+  return u32x4{low[0], high[0], low[1], high[1]};
+}
+
+// n: the first of the 32 features.
+__device__ __forceinline__ void store_tiles(uint8_t* y, int64_t row, int features, int n, int part, bool in_rows,
+                                            const f32x4& a, const f32x4& b) {
+  const u32x4 v = side_by_side(a, b);
   n += (part & 1) * 16 + (part >> 1) * 8;
-  if (in_rows && n < features) *(u32x4*)(y + (row * features + n) * 2) = u32x4{low[0], high[0], low[1], high[1]};
+  if (in_rows && n < features) *(u32x4*)(y + (row * features + n) * 2) = v;
 }
 
 typedef __attribute__((address_space(3))) void lds_void;
