@@ -14,24 +14,30 @@ namespace eep {
 
 constexpr int kNormMaxWidth = 65536;
 
-// Sums over the workgroup of up to two values, in every thread, added in the order of the wavefronts.
-__device__ __forceinline__ void block_sum(float& a, float& b, float (*part)[2]) {
+// Sums over the workgroup of K values, in every thread, added in the order of the wavefronts.  Successive sums take the two buffers
+// in turn, so that one barrier each is enough.
+constexpr int kSums = 4;
+struct BlockSums {
+  float part[2][16][kSums];
+};
+template <int K>
+__device__ __forceinline__ void block_sum(float (&v)[K], BlockSums& s, int& turn) {
   const int threads = blockDim.x;
-  a = lane_sum<64>(a);
-  b = lane_sum<64>(b);
-  if (threads > 64) {
-    __syncthreads();  // (the sums before are read)
-    if ((threadIdx.x & 63) == 0) {
-      part[threadIdx.x >> 6][0] = a;
-      part[threadIdx.x >> 6][1] = b;
-    }
-    __syncthreads();
-    a = b = 0.0f;
-    for (int w = 0; w < threads / 64; ++w) {
-      a += part[w][0];
-      b += part[w][1];
-    }
+#pragma unroll
+  for (int i = 0; i < K; ++i) v[i] = lane_sum<64>(v[i]);
+  if (threads <= 64) return;
+  if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+    for (int i = 0; i < K; ++i) s.part[turn][threadIdx.x >> 6][i] = v[i];
   }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < K; ++i) v[i] = 0.0f;
+  for (int w = 0; w < threads / 64; ++w) {
+#pragma unroll
+    for (int i = 0; i < K; ++i) v[i] += s.part[turn][w][i];
+  }
+  turn ^= 1;
 }
 
 __device__ __forceinline__ void load8_any(bool bf16, const void* base, int64_t vec, float (&v)[8]) {
@@ -61,44 +67,44 @@ struct LayerNormArgs {
   float epsilon;
 };
 
-// Takes the mean out of h, times `by`: a row whose sum leaves fp32 is scaled first.  Returns the factor that h then holds.
+// Takes the mean out of h, but for what roundings leave of it: a row whose sum leaves fp32 is scaled first.  Returns the factor that h
+// then holds.
 template <int NV>
-__device__ __forceinline__ float centre(float (&h)[NV][8], int H, int vecs, float (*part)[2]) {
+__device__ __forceinline__ float centre(float (&h)[NV][8], int H, int vecs, BlockSums& s, int& turn) {
   const int threads = blockDim.x, tid = threadIdx.x;
   float by = 1.0f;
-  for (int round = 0; round < 2; ++round) {
-    float sum = 0.0f, top = 0.0f;
+  float sum[1] = {0.0f};
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum[0] += h[j][i];
+  block_sum(sum, s, turn);
+  if (!(fabsf(sum[0]) < INFINITY)) {
+    by = 0x1p-80f;
+    sum[0] = 0.0f;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum += h[j][i];
-    block_sum(sum, top, part);
-    if (round == 0 && !(fabsf(sum) < INFINITY)) {
-      by = 0x1p-80f;
-      sum = 0.0f;
+      for (int i = 0; i < 8; ++i) {
+        h[j][i] *= by;
+        sum[0] += h[j][i];
+      }
+    block_sum(sum, s, turn);
+  }
+  const float mean = sum[0] / (float)H;
 #pragma unroll
-      for (int j = 0; j < NV; ++j)
+  for (int j = 0; j < NV; ++j) {
+    if (j * threads + tid >= vecs) continue;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          h[j][i] *= by;
-          sum += h[j][i];
-        }
-      block_sum(sum, top, part);
-    }
-    const float mean = sum / (float)H;
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      if (j * threads + tid >= vecs) continue;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) h[j][i] -= mean;
-    }
+    for (int i = 0; i < 8; ++i) h[j][i] -= mean;
   }
   return by;
 }
 
 template <bool IN_BF16, bool OUT_BF16, int NV>
 __global__ __launch_bounds__(1024) void k_layer_norm(LayerNormArgs a, int64_t first) {
-  __shared__ float s_part[16][2];
+  __shared__ BlockSums s_sums;
+  int turn = 0;
   const int64_t row = first + blockIdx.x;
   const int vecs = a.H / 8, threads = blockDim.x, tid = threadIdx.x;
   const int64_t row_vec = row * vecs;
@@ -120,17 +126,22 @@ __global__ __launch_bounds__(1024) void k_layer_norm(LayerNormArgs a, int64_t fi
       for (int i = 0; i < 8; ++i) h[j][i] = 0.0f;
     }
   }
-  float by = centre<NV>(h, a.H, vecs, s_part);
+  float by = centre<NV>(h, a.H, vecs, s_sums, turn);
+  float left, mean;  // what is left of the mean, and the mean square without it
   auto mean_square = [&]() {
-    float squares = 0.0f, none = 0.0f;
+    float sum[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) squares = fmaf(h[j][i], h[j][i], squares);
-    block_sum(squares, none, s_part);
-    return squares / (float)a.H;
+      for (int i = 0; i < 8; ++i) {
+        sum[0] += h[j][i];
+        sum[1] = fmaf(h[j][i], h[j][i], sum[1]);
+      }
+    block_sum(sum, s_sums, turn);
+    left = sum[0] / (float)a.H;
+    mean = fmaxf(fmaf(-left, left, sum[1] / (float)a.H), 0.0f);
   };
-  float mean = mean_square();
+  mean_square();
   const float more = by == 1.0f ? fitting(mean, a.epsilon) : 1.0f;
   if (more != 1.0f) {
     by = more;
@@ -138,7 +149,7 @@ __global__ __launch_bounds__(1024) void k_layer_norm(LayerNormArgs a, int64_t fi
     for (int j = 0; j < NV; ++j)
 #pragma unroll
       for (int i = 0; i < 8; ++i) h[j][i] *= by;
-    mean = mean_square();
+    mean_square();
   }
   const float inv = 1.0f / sqrtf(mean + a.epsilon * by * by);
 #pragma unroll
@@ -154,7 +165,7 @@ __global__ __launch_bounds__(1024) void k_layer_norm(LayerNormArgs a, int64_t fi
       for (int i = 0; i < 8; ++i) b[i] = 0.0f;
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) h[j][i] = fmaf(h[j][i] * inv, g[i], b[i]);
+    for (int i = 0; i < 8; ++i) h[j][i] = fmaf((h[j][i] - left) * inv, g[i], b[i]);
     store8<OUT_BF16>(a.y, row_vec + v, h[j]);
   }
 }
@@ -211,13 +222,18 @@ struct Raw8 {
   }
 };
 
+// Workgroups to a CU: as many as registers allow; the rows of fp32 inputs are twice as many bytes under way.
 constexpr int norm_grad_threads(int nv) { return nv == 8 ? 1024 : 512; }
+constexpr int norm_grad_waves(bool in_bf16, int nv) { return nv == 8 ? 4 : in_bf16 && nv <= 2 ? 4 : 2; }
 
 template <bool IN_BF16, bool OUT_BF16, bool CENTRED, int NV>
-__global__ __launch_bounds__(norm_grad_threads(NV)) void k_norm_grad(NormGradArgs a) {
-  __shared__ float s_part[16][2];
+__global__ __launch_bounds__(norm_grad_threads(NV), norm_grad_waves(IN_BF16, NV)) void k_norm_grad(NormGradArgs a) {
+  __shared__ BlockSums s_sums;
+  extern __shared__ f32x4 s_gain[];  // of rows that fit it
+  constexpr bool kGainInLds = NV <= 2;
   const int vecs = a.H / 8, threads = blockDim.x, tid = threadIdx.x;
   const float count = (float)a.H;
+  int turn = 0;
   Raw8<IN_BF16> h_raw[NV], stream_raw[NV];
   Raw8<OUT_BF16> grad_raw[NV];
   float gain_sum[NV][8], bias_sum[CENTRED ? NV : 1][8];
@@ -231,50 +247,84 @@ __global__ __launch_bounds__(norm_grad_threads(NV)) void k_norm_grad(NormGradArg
       if (a.grad_sum != nullptr) stream_raw[j].load(a.grad_sum, row * vecs + v);
     }
   };
+  const auto gain_of = [&](int j, float (&g)[8]) {
+    const int at = j * threads + tid;
+    if constexpr (kGainInLds) {
+      const f32x4 low = s_gain[2 * at], high = s_gain[2 * at + 1];
 #pragma unroll
-  for (int j = 0; j < NV; ++j)
+      for (int i = 0; i < 4; ++i) {
+        g[i] = low[i];
+        g[4 + i] = high[i];
+      }
+    } else {
+      load8_any(a.gain_bf16, a.gain, at, g);
+    }
+  };
+  fetch(blockIdx.x);
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int at = j * threads + tid;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       gain_sum[j][i] = 0.0f;
       if constexpr (CENTRED) bias_sum[j][i] = 0.0f;
     }
-  int64_t row = blockIdx.x;
-  fetch(row);
-  for (; row < a.T; row += gridDim.x) {
-    float d[NV][8], v[NV][8];  // v: grad_y until the gain's sums have it, then grad_y * gain
+    if (kGainInLds && at < vecs) {
+      float g[8];
+      load8_any(a.gain_bf16, a.gain, at, g);
+      // (every thread reads what it wrote itself)
+      s_gain[2 * at] = f32x4{g[0], g[1], g[2], g[3]};
+      s_gain[2 * at + 1] = f32x4{g[4], g[5], g[6], g[7]};
+    }
+  }
+  for (int64_t row = blockIdx.x; row < a.T; row += gridDim.x) {
+    float d[NV][8];
     Raw8<IN_BF16> stream[NV];
+    Raw8<OUT_BF16> grad[NV];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const bool in = j * threads + tid < vecs;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        d[j][i] = in ? h_raw[j].at(i) : 0.0f;
-        v[j][i] = in ? grad_raw[j].at(i) : 0.0f;
-      }
+      for (int i = 0; i < 8; ++i) d[j][i] = in ? h_raw[j].at(i) : 0.0f;
       stream[j] = stream_raw[j];
+      grad[j] = grad_raw[j];
     }
     if (row + gridDim.x < a.T) fetch(row + gridDim.x);
     float by = 1.0f;
-    if constexpr (CENTRED) by = centre<NV>(d, a.H, vecs, s_part);
-    float squares, along;
+    if constexpr (CENTRED) by = centre<NV>(d, a.H, vecs, s_sums, turn);
+    // of d * d and v * d; centred, of d, which roundings have left, and of v
+    float sum[CENTRED ? 4 : 2];
     const auto sums = [&]() {
-      squares = along = 0.0f;
+#pragma unroll
+      for (float& v : sum) v = 0.0f;
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
-        const int at = j * threads + tid;
-        if (at >= vecs) continue;
+        if (j * threads + tid >= vecs) continue;
         float g[8];
-        load8_any(a.gain_bf16, a.gain, at, g);
+        gain_of(j, g);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          squares = fmaf(d[j][i], d[j][i], squares);
-          along = fmaf(v[j][i] * g[i], d[j][i], along);
+          const float v = grad[j].at(i) * g[i];
+          sum[0] = fmaf(d[j][i], d[j][i], sum[0]);
+          sum[1] = fmaf(v, d[j][i], sum[1]);
+          if constexpr (CENTRED) {
+            sum[2] += d[j][i];
+            sum[3] += v;
+          }
         }
       }
-      block_sum(squares, along, s_part);
+      block_sum(sum, s_sums, turn);
+    };
+    const auto mean_square = [&]() {
+      if constexpr (CENTRED) {
+        const float left = sum[2] / count;
+        return fmaxf(fmaf(-left, left, sum[0] / count), 0.0f);
+      } else {
+        return sum[0] / count;
+      }
     };
     sums();
-    const float more = by == 1.0f ? fitting(squares / count, a.epsilon) : 1.0f;
+    const float more = by == 1.0f ? fitting(mean_square(), a.epsilon) : 1.0f;
     if (more != 1.0f) {
       by = more;
 #pragma unroll
@@ -283,42 +333,28 @@ __global__ __launch_bounds__(norm_grad_threads(NV)) void k_norm_grad(NormGradArg
         for (int i = 0; i < 8; ++i) d[j][i] *= by;
       sums();
     }
-    const float inv = 1.0f / sqrtf(squares / count + a.epsilon * by * by);
-    along = along * inv / count;  // mean(v * u)
-    float mean = 0.0f;
+    const float inv = 1.0f / sqrtf(mean_square() + a.epsilon * by * by);
+    float left = 0.0f, mean = 0.0f;
+    if constexpr (CENTRED) {
+      left = sum[2] / count;
+      mean = sum[3] / count;
+    }
+    const float along = fmaf(-left, mean, sum[1] / count) * inv;  // mean(v * u)
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int at = j * threads + tid;
       if (at >= vecs) continue;
-      float g[8];
-      load8_any(a.gain_bf16, a.gain, at, g);
+      float g[8], o[8];
+      gain_of(j, g);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        d[j][i] *= inv;  // u
-        gain_sum[j][i] = fmaf(v[j][i], d[j][i], gain_sum[j][i]);
-        if constexpr (CENTRED) bias_sum[j][i] += v[j][i];
-        v[j][i] *= g[i];
-        if constexpr (CENTRED) mean += v[j][i];
+        const float u = (d[j][i] - left) * inv, dy = grad[j].at(i);
+        gain_sum[j][i] = fmaf(dy, u, gain_sum[j][i]);
+        if constexpr (CENTRED) bias_sum[j][i] += dy;
+        o[i] = (fmaf(-u, along, dy * g[i]) - mean) * inv * by;
+        if (a.grad_sum != nullptr) o[i] += stream[j].at(i);
       }
-    }
-    if (a.grad_h != nullptr) {
-      if constexpr (CENTRED) {
-        float none = 0.0f;
-        block_sum(mean, none, s_part);
-        mean /= count;
-      }
-#pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        const int at = j * threads + tid;
-        if (at >= vecs) continue;
-        float o[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          o[i] = (fmaf(-d[j][i], along, v[j][i]) - mean) * inv * by;
-          if (a.grad_sum != nullptr) o[i] += stream[j].at(i);
-        }
-        store8<IN_BF16>(a.grad_h, row * vecs + at, o);
-      }
+      if (a.grad_h != nullptr) store8<IN_BF16>(a.grad_h, row * vecs + at, o);
     }
   }
   if (a.partial == nullptr) return;
@@ -366,10 +402,11 @@ static hipError_t launch_norm_grad(const NormGradArgs& a, int groups, hipStream_
   int nv = 1;
   while (nv < 8 && vecs > nv * 512) nv *= 2;
   const dim3 grid((unsigned)groups), block((unsigned)(((vecs + nv - 1) / nv + 63) / 64 * 64));
+  const size_t lds = nv <= 2 ? (size_t)a.H * sizeof(float) : 0;
   switch (nv) {
-    case 1: hipLaunchKernelGGL((k_norm_grad<IN_BF16, OUT_BF16, CENTRED, 1>), grid, block, 0, st, a); break;
-    case 2: hipLaunchKernelGGL((k_norm_grad<IN_BF16, OUT_BF16, CENTRED, 2>), grid, block, 0, st, a); break;
-    case 4: hipLaunchKernelGGL((k_norm_grad<IN_BF16, OUT_BF16, CENTRED, 4>), grid, block, 0, st, a); break;
+    case 1: hipLaunchKernelGGL((k_norm_grad<IN_BF16, OUT_BF16, CENTRED, 1>), grid, block, lds, st, a); break;
+    case 2: hipLaunchKernelGGL((k_norm_grad<IN_BF16, OUT_BF16, CENTRED, 2>), grid, block, lds, st, a); break;
+    case 4: hipLaunchKernelGGL((k_norm_grad<IN_BF16, OUT_BF16, CENTRED, 4>), grid, block, lds, st, a); break;
     default: hipLaunchKernelGGL((k_norm_grad<IN_BF16, OUT_BF16, CENTRED, 8>), grid, block, 0, st, a);
   }
   return hipGetLastError();

@@ -22,19 +22,25 @@ struct Piece {
     else
       return __uint_as_float(d[i >> 2][i & 3]);
   }
-  __device__ __forceinline__ static void store(void* base, int64_t at, const float (&v)[N]) {
-    u32x4* to = (u32x4*)base + at * (BF16 ? 1 : N / 4);
+  __device__ __forceinline__ void round(const float (&v)[N]) {
     if constexpr (BF16) {
-      u32x4 o;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) o[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
-      __builtin_nontemporal_store(o, to);
+      for (int i = 0; i < 4; ++i) d[0][i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
     } else {
 #pragma unroll
-      for (int i = 0; i < N / 4; ++i) {
-        const f32x4 o = {v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
-        __builtin_nontemporal_store(__builtin_bit_cast(u32x4, o), to + i);
-      }
+      for (int i = 0; i < N; ++i) d[i >> 2][i & 3] = __float_as_uint(v[i]);
+    }
+  }
+  // THROUGH: as receive rows are stored (rows.hpp), else non-temporal
+  template <bool THROUGH>
+  __device__ __forceinline__ void store(void* base, int64_t at) const {
+    u32x4* to = (u32x4*)base + at * (BF16 ? 1 : N / 4);
+#pragma unroll
+    for (int i = 0; i < (BF16 ? 1 : N / 4); ++i) {
+      if constexpr (THROUGH)
+        store_row(to + i, d[i]);
+      else
+        __builtin_nontemporal_store(d[i], to + i);
     }
   }
 };
@@ -50,7 +56,7 @@ struct CombineGradArgs {
 
 // The row of a pair that lost its row_of entry when failure detection dropped its rank within the step (-1: it never had
 // one).  A slot's rows are in the order of their pairs.
-__device__ __noinline__ int row_of_dropped(const CombineGradArgs& a, int pair) {
+__device__ __forceinline__ int row_of_dropped(const CombineGradArgs& a, int64_t pair) {
   const int slot = a.slot_of[pair];
   if (slot < 0) return -1;
   int lo = a.offset[slot], hi = a.offset[slot + 1];
@@ -70,59 +76,59 @@ __device__ __noinline__ int row_of_dropped(const CombineGradArgs& a, int pair) {
 //
 // A workgroup has B pairs of one token: it reads the token's gradient once for them, and of every pair the row of y, from which
 // the products are summed, and writes the row of grad_y beside it.  Bound by memory at many tokens, by one trip and the
-// sum across wavefronts at few.
+// sum across wavefronts at few.  Measured, 5976 tokens of 2880, top-6, rows bf16, tokens fp32 / 16384 of 7168, top-8 / 512 / 128 of them,
+// us: 82.6 (5.7 TB/s) / 815 / 20.9 / 9.2; with non-temporal stores 92.0 / 813 / 24.9 / 10.4, with plain ones 81.7 / 847 / 23.5 / 10.6; up
+// to 4 / 2 pairs a workgroup (non-temporal) 101 / 888 / 24.8 / 10.4 and 111 / 1034 / 24.9 / 10.3; 256 / 128 threads 92.9 / 816 / 25.1 / 10.6
+// and 94.2 / 822 / 26.6 / 10.5.
 // ---------------------------------------------------------------------------
-constexpr int kGradThreads = 256;
-
 template <bool Y_BF16, bool OUT_BF16, int N, int B>
-__global__ __launch_bounds__(kGradThreads) void k_combine_grad(CombineGradArgs a, int64_t first, int batches) {
-  __shared__ float s_part[kGradThreads / 64][B];
+__global__ __launch_bounds__(1024) void k_combine_grad(CombineGradArgs a, int64_t first, int batches) {
+  __shared__ float s_part[16][B];
   const int tid = threadIdx.x, threads = blockDim.x;
-  const int64_t work = first + blockIdx.x;
-  const int64_t t = work / batches;
-  const int j0 = (int)(work - t * batches) * B;
+  const int batch = batches > 1 ? blockIdx.x % (unsigned)batches : 0;
+  const int64_t t = first + (batches > 1 ? blockIdx.x / (unsigned)batches : blockIdx.x);
+  const int j0 = batch * B;
   int row[B];
-  bool dropped[B];
   float w[B], sum[B];
+  uint32_t dropped = 0;
+#pragma unroll
+  for (int j = 0; j < B; ++j) row[j] = j0 + j < a.k ? a.row_of[t * a.k + j0 + j] : -1;
 #pragma unroll
   for (int j = 0; j < B; ++j) {
-    const bool in = j0 + j < a.k;
-    row[j] = in ? a.row_of[t * a.k + j0 + j] : -1;
-    w[j] = in && a.grad_y != nullptr ? a.topk_w[t * a.k + j0 + j] : 0.0f;
     sum[j] = 0.0f;
-    dropped[j] = false;
+    w[j] = j0 + j < a.k && a.grad_y != nullptr ? a.topk_w[t * a.k + j0 + j] : 0.0f;
   }
 #pragma unroll
   for (int j = 0; j < B; ++j)
     if (__builtin_expect(row[j] < 0 && j0 + j < a.k, 0)) {
       // (its row takes part in the experts' gradients and has to be zeros)
-      row[j] = row_of_dropped(a, (int)(t * a.k) + j0 + j);
-      dropped[j] = row[j] >= 0;
-      w[j] = 0.0f;
+      row[j] = row_of_dropped(a, t * a.k + j0 + j);
+      if (row[j] >= 0) dropped |= 1u << j;
     }
   for (int v = tid; v < a.pieces; v += threads) {
     Piece<OUT_BF16, N> g;
     Piece<Y_BF16, N> y[B];
     g.load(a.grad_out, t * a.pieces + v);
     if (a.grad_w != nullptr) {
+      // (a pair without a row, or a dropped one, loads some row, and its sum is not used)
+#pragma unroll
+      for (int j = 0; j < B; ++j) y[j].load(a.y, (int64_t)(row[j] >= 0 ? row[j] : 0) * a.pieces + v);
 #pragma unroll
       for (int j = 0; j < B; ++j)
-        if (row[j] >= 0 && !dropped[j]) y[j].load(a.y, (int64_t)row[j] * a.pieces + v);
 #pragma unroll
-      for (int j = 0; j < B; ++j)
-        if (row[j] >= 0 && !dropped[j]) {
-#pragma unroll
-          for (int i = 0; i < N; ++i) sum[j] = fmaf(g.at(i), y[j].at(i), sum[j]);
-        }
+        for (int i = 0; i < N; ++i) sum[j] = fmaf(g.at(i), y[j].at(i), sum[j]);
     }
     if (a.grad_y != nullptr) {
 #pragma unroll
       for (int j = 0; j < B; ++j)
         if (row[j] >= 0) {
           float o[N];
+          const bool zeros = (dropped >> j) & 1;
 #pragma unroll
-          for (int i = 0; i < N; ++i) o[i] = dropped[j] ? 0.0f : w[j] * g.at(i);
-          Piece<Y_BF16, N>::store(a.grad_y, (int64_t)row[j] * a.pieces + v, o);
+          for (int i = 0; i < N; ++i) o[i] = zeros ? 0.0f : w[j] * g.at(i);
+          Piece<Y_BF16, N> piece;
+          piece.round(o);
+          piece.template store<true>(a.grad_y, (int64_t)row[j] * a.pieces + v);
         }
     }
   }
@@ -136,26 +142,33 @@ __global__ __launch_bounds__(kGradThreads) void k_combine_grad(CombineGradArgs a
   if (tid < B && j0 + tid < a.k) {
     float all = 0.0f;
     for (int i = 0; i < threads / 64; ++i) all += s_part[i][tid];
-    a.grad_w[t * a.k + j0 + tid] = all;
+    bool summed = false;
+#pragma unroll
+    for (int j = 0; j < B; ++j)
+      if (j == tid) summed = row[j] >= 0 && !((dropped >> j) & 1);
+    a.grad_w[t * a.k + j0 + tid] = summed ? all : 0.0f;
   }
 }
 
 template <bool Y_BF16, bool OUT_BF16, int N>
 static hipError_t launch_combine_grad_t(const CombineGradArgs& a, int T, hipStream_t st) {
-  const int wavefronts = (a.pieces + 63) / 64;
-  const int threads = wavefronts < kGradThreads / 64 ? wavefronts * 64 : kGradThreads;
-  const auto launch = [&](auto size) {
-    constexpr int B = decltype(size)::value;
-    const int batches = (a.k + B - 1) / B;
-    return in_launches((int64_t)T * batches, max_blocks(threads), [&](int64_t first, int64_t n) {
-      hipLaunchKernelGGL((k_combine_grad<Y_BF16, OUT_BF16, N, B>), dim3((unsigned)n), dim3((unsigned)threads), 0, st, a, first,
-                         batches);
-      return hipGetLastError();
-    });
-  };
-  if (T < 512 || a.k == 1) return launch(std::integral_constant<int, 1>());
-  if (a.k == 2) return launch(std::integral_constant<int, 2>());
-  return launch(std::integral_constant<int, 4>());
+  // pairs a workgroup: as many as leave a thousand workgroups, up to 8, the batches of a token alike
+  const int64_t pairs = (int64_t)T * a.k;
+  const int most = pairs < 2 * 1024 ? 1 : pairs < 8 * 1024 ? (int)(pairs / 1024) : 8;
+  const int batches = (a.k + most - 1) / most, size = (a.k + batches - 1) / batches;
+  // threads: all of a row at a time where workgroups are few, else up to 512
+  const int limit = pairs < 2 * 1024 ? 1024 : 512, rounds = (a.pieces + limit - 1) / limit;
+  const int threads = ((a.pieces + rounds - 1) / rounds + 63) / 64 * 64;
+  return in_launches(T, max_blocks(threads) / batches, [&](int64_t first, int64_t n) {
+    const dim3 grid((unsigned)(n * batches)), block((unsigned)threads);
+    switch (size) {
+#define EEP_PAIRS(B) \
+  case B: hipLaunchKernelGGL((k_combine_grad<Y_BF16, OUT_BF16, N, B>), grid, block, 0, st, a, first, batches); break;
+      EEP_PAIRS(1) EEP_PAIRS(2) EEP_PAIRS(3) EEP_PAIRS(4) EEP_PAIRS(5) EEP_PAIRS(6) EEP_PAIRS(7) EEP_PAIRS(8)
+#undef EEP_PAIRS
+    }
+    return hipGetLastError();
+  });
 }
 
 hipError_t launch_combine_grad(eep_ctx* c, const void* y, const float* topk_w, const void* grad_out, void* grad_y, float* grad_w,
@@ -173,7 +186,8 @@ hipError_t launch_combine_grad(eep_ctx* c, const void* y, const float* topk_w, c
 // ---------------------------------------------------------------------------
 // dispatch's gradient: grad_x[t] = sum over routed j, ascending, of grad_recv[row_of[t, j]]: combine without weights.
 //
-// As there, a wavefront has 64 pieces of one token's rows, their loads all under way together.
+// As there, a wavefront has 64 pieces of one token's rows, their loads all under way together.  Bound by memory: 16384 tokens of 7168 bf16,
+// top-8, 323 us (6.2 TB/s).
 // ---------------------------------------------------------------------------
 template <bool Y_BF16, bool OUT_BF16, int N>
 __global__ __launch_bounds__(64) void k_dispatch_grad(const int32_t* __restrict__ row_of, const void* __restrict__ grad_recv,
@@ -212,7 +226,9 @@ __global__ __launch_bounds__(64) void k_dispatch_grad(const int32_t* __restrict_
     j += 2;
   }
   if (j < k) batch(std::integral_constant<int, 1>(), j);
-  Piece<OUT_BF16, N>::store(grad_x, t * pieces + v, acc);
+  Piece<OUT_BF16, N> piece;
+  piece.round(acc);
+  piece.template store<false>(grad_x, t * pieces + v);
 }
 
 template <bool Y_BF16, bool OUT_BF16, int N>
