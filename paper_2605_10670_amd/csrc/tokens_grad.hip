@@ -31,16 +31,15 @@ struct Piece {
       for (int i = 0; i < N; ++i) d[i >> 2][i & 3] = __float_as_uint(v[i]);
     }
   }
-  // THROUGH: as receive rows are stored (rows.hpp), else non-temporal
-  template <bool THROUGH>
-  __device__ __forceinline__ void store(void* base, int64_t at) const {
+  // through: as receive rows are stored (rows.hpp), else non-temporal
+  __device__ __forceinline__ void store(void* base, int64_t at, bool through) const {
     u32x4* to = (u32x4*)base + at * (BF16 ? 1 : N / 4);
+    if (through) {
 #pragma unroll
-    for (int i = 0; i < (BF16 ? 1 : N / 4); ++i) {
-      if constexpr (THROUGH)
-        store_row(to + i, d[i]);
-      else
-        __builtin_nontemporal_store(d[i], to + i);
+      for (int i = 0; i < (BF16 ? 1 : N / 4); ++i) store_row(to + i, d[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < (BF16 ? 1 : N / 4); ++i) __builtin_nontemporal_store(d[i], to + i);
     }
   }
 };
@@ -52,6 +51,7 @@ struct CombineGradArgs {
   void* grad_y;
   float* grad_w;
   int k, pieces;  // of N values, of a row
+  bool through;   // how rows are stored
 };
 
 // The row of a pair that lost its row_of entry when failure detection dropped its rank within the step (-1: it never had
@@ -76,11 +76,14 @@ __device__ __forceinline__ int row_of_dropped(const CombineGradArgs& a, int64_t 
 //
 // A workgroup has B pairs of one token: it reads the token's gradient once for them, and of every pair the row of y, from which
 // the products are summed, and writes the row of grad_y beside it.  Bound by memory at many tokens, by one trip and the
-// sum across wavefronts at few.  Measured, 5976 tokens of 2880, top-6, rows bf16, tokens fp32 / 16384 of 7168, top-8 / 512 / 128 of them,
-// us: 82.6 (5.7 TB/s) / 815 / 20.9 / 9.2; with non-temporal stores 92.0 / 813 / 24.9 / 10.4, with plain ones 81.7 / 847 / 23.5 / 10.6; up
-// to 4 / 2 pairs a workgroup (non-temporal) 101 / 888 / 24.8 / 10.4 and 111 / 1034 / 24.9 / 10.3; 256 / 128 threads 92.9 / 816 / 25.1 / 10.6
+// sum across wavefronts at few.  Measured on buffers that are used again and again, 5976 tokens of 2880, top-6, rows bf16, tokens fp32 /
+// 16384 of 7168, top-8 / 512 / 128 of them, us: non-temporal stores 92.0 / 813 / 24.9 / 10.4, write-through 82.6 / 815 / 20.9 / 9.2, plain
+// 81.7 / 847 / 23.5 / 10.6; on other buffers every time, where the large caches have none of them, 5976 tokens 92 (5.1 TB/s) / 95 / 98.
+// Up to 4 / 2 pairs a workgroup (non-temporal) 101 / 888 / 24.8 / 10.4 and 111 / 1034 / 24.9 / 10.3; 256 / 128 threads 92.9 / 816 / 25.1 / 10.6
 // and 94.2 / 822 / 26.6 / 10.5.
 // ---------------------------------------------------------------------------
+constexpr int64_t kThroughBytes = 128 << 20;  // of grad_y, half of what the memory-side cache holds
+
 template <bool Y_BF16, bool OUT_BF16, int N, int B>
 __global__ __launch_bounds__(1024) void k_combine_grad(CombineGradArgs a, int64_t first, int batches) {
   __shared__ float s_part[16][B];
@@ -128,7 +131,7 @@ __global__ __launch_bounds__(1024) void k_combine_grad(CombineGradArgs a, int64_
           for (int i = 0; i < N; ++i) o[i] = zeros ? 0.0f : w[j] * g.at(i);
           Piece<Y_BF16, N> piece;
           piece.round(o);
-          piece.template store<true>(a.grad_y, (int64_t)row[j] * a.pieces + v);
+          piece.store(a.grad_y, (int64_t)row[j] * a.pieces + v, a.through);
         }
     }
   }
@@ -173,10 +176,11 @@ static hipError_t launch_combine_grad_t(const CombineGradArgs& a, int T, hipStre
 
 hipError_t launch_combine_grad(eep_ctx* c, const void* y, const float* topk_w, const void* grad_out, void* grad_y, float* grad_w,
                                int T, hipStream_t st) {
-  CombineGradArgs a = {c->row_of, c->slot_of, c->src_of, c->offset, grad_out, y, topk_w, grad_y, grad_w, c->k, 0};
+  CombineGradArgs a = {c->row_of, c->slot_of, c->src_of, c->offset, grad_out, y, topk_w, grad_y, grad_w, c->k, 0, false};
   const bool yb = c->cfg.y_dtype == EEP_BF16, ob = c->cfg.out_dtype == EEP_BF16;
   const int n = yb || ob ? 8 : 4;
   a.pieces = c->H / n;
+  a.through = (int64_t)T * c->k * c->y_row_bytes <= kThroughBytes;
   if (yb && ob) return launch_combine_grad_t<true, true, 8>(a, T, st);
   if (yb) return launch_combine_grad_t<true, false, 8>(a, T, st);
   if (ob) return launch_combine_grad_t<false, true, 8>(a, T, st);
@@ -228,7 +232,7 @@ __global__ __launch_bounds__(64) void k_dispatch_grad(const int32_t* __restrict_
   if (j < k) batch(std::integral_constant<int, 1>(), j);
   Piece<OUT_BF16, N> piece;
   piece.round(acc);
-  piece.template store<false>(grad_x, t * pieces + v);
+  piece.store(grad_x, t * pieces + v, false);
 }
 
 template <bool Y_BF16, bool OUT_BF16, int N>

@@ -13,7 +13,7 @@ pytestmark = pytest.mark.gpu
 
 
 @pytest.mark.parametrize("T,E,k", [(1, 1, 1), (3, 8, 8), (5, 60, 6), (33, 256, 8), (7, 257, 1), (4, 510, 32), (2, 4096, 32), (9000, 64, 6),
-                                   (2, 4093, 7)])
+                                   (4096, 256, 8), (4100, 252, 16), (4099, 512, 1), (4100, 100, 17), (4097, 4, 4), (2, 4093, 7)])
 @pytest.mark.parametrize("x", ["f32", "bf16"])
 @pytest.mark.parametrize("over_all", [False, True])
 def test_route_grad(T, E, k, x, over_all):
@@ -53,13 +53,14 @@ def test_rows_with_nothing_to_choose_and_odd_addresses():
         gr.check("grad_logits", got, want, err)
 
 
-def test_an_index_twice_gets_both():
-    idx = torch.tensor([[2, 2]], dtype=torch.int32, device="cuda")
-    w, gw = torch.tensor([[0.25, 0.75]], device="cuda"), torch.tensor([[1.0, -2.0]], device="cuda")
-    out = torch.empty((1, 4), device="cuda")
-    layer.Router(num_logical=4, topk=2).grad(idx, w, gw, out, 1)
+@pytest.mark.parametrize("T", [1, 5000])
+def test_an_index_twice_gets_both_and_one_out_of_range_nothing(T):
+    idx = torch.tensor([[2, 2, 4]], dtype=torch.int32, device="cuda").repeat(T, 1)
+    w, gw = torch.tensor([[0.25, 0.75, 0.0]], device="cuda").repeat(T, 1), torch.tensor([[1.0, -2.0, 3.0]], device="cuda").repeat(T, 1)
+    out = torch.empty((T, 4), device="cuda")
+    layer.Router(num_logical=4, topk=3).grad(idx, w, gw, out, T)
     inner = 0.25 - 1.5
-    assert out.cpu().tolist() == [[0, 0, 0.25 * (1 - inner) + 0.75 * (-2 - inner), 0]]
+    assert out.unique(dim=0).cpu().tolist() == [[0, 0, 0.25 * (1 - inner) + 0.75 * (-2 - inner), 0]]
 
 
 def test_against_differences():
