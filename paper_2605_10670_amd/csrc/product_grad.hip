@@ -242,15 +242,27 @@ __global__ __launch_bounds__(64 * grad_waves(TT), 2) void k_grad_tiled(TileArgs 
     items = (int64_t)map.total * a.feature_tiles;
   }
   // The items go to the XCDs in turn, as many neighbouring ones at a time as one has workgroups, which share rows of the
-  // operands in its L2.
+  // operands in its L2; what is left over for a last turn is divided between them.
   const int xcds = gridDim.x % 8 == 0 ? 8 : 1;
-  const int xcd = blockIdx.x % xcds, seats = gridDim.x / xcds;
-  const int64_t first_item = (int64_t)xcd * seats + blockIdx.x / xcds;
-  const auto find = [&](int64_t item) {
+  const int xcd = blockIdx.x % xcds, seat = blockIdx.x / xcds, seats = gridDim.x / xcds;
+  const int64_t whole_turns = items / gridDim.x, over = items - whole_turns * gridDim.x;
+  const int over_from = (int)(over * xcd / xcds), over_to = (int)(over * (xcd + 1) / xcds);
+  const int64_t turns = whole_turns + (seat < over_to - over_from ? 1 : 0);
+  const auto item_of = [&](int64_t turn) {
+    return turn * gridDim.x + (turn < whole_turns ? xcd * seats : over_from) + seat;
+  };
+  // Where a walk over the items is: OF_W, the slot and the place among its tiles (without a division, which 64 bits make long).
+  struct Walk {
+    int64_t turn, at;
+    int slot;
+  };
+  const auto find = [&](Walk& w) {
     Tile t;
     if constexpr (OF_W) {
-      t.slot = (int)(item / per_slot);
-      int at = (int)(item - t.slot * per_slot);
+      const int64_t item = item_of(w.turn);
+      for (; item - w.at >= per_slot; w.at += per_slot) ++w.slot;
+      t.slot = w.slot;
+      int at = (int)(item - w.at);
       // four tiles of weight rows by all of in_features, then the next four
       const int four = at / (4 * a.feature_tiles), tall = a.row_tiles - 4 * four < 4 ? a.row_tiles - 4 * four : 4;
       at -= four * 4 * a.feature_tiles;
@@ -267,7 +279,7 @@ __global__ __launch_bounds__(64 * grad_waves(TT), 2) void k_grad_tiled(TileArgs 
       t.terms = t.end > t.first ? t.end - t.first : 0;
     } else {
       int feature_tile;
-      map.find(a, item, &t.slot, &feature_tile, &t.first, &t.end);
+      map.find(a, item_of(w.turn), &t.slot, &feature_tile, &t.first, &t.end);
       t.column0 = feature_tile * kGradCols;
       t.row0 = t.first;
       t.terms = a.n;
@@ -280,7 +292,7 @@ __global__ __launch_bounds__(64 * grad_waves(TT), 2) void k_grad_tiled(TileArgs 
   const int load_row = lane >> 2, load_chunk = (lane & 3) ^ ((load_row >> 2) & 3);
 
   // The stream of steps: the tile that is fetched, its terms left, where its operands are and the lane's places there.
-  int64_t fetch_item = first_item;
+  Walk ahead = {-1, 0, 0};
   int fetch_left = 0;
   const uint8_t *other_at = nullptr, *grads_at[kGradLoads] = {};
   uint32_t other_off[Other::kLoads] = {}, grads_off[kGradLoads] = {};
@@ -319,12 +331,11 @@ __global__ __launch_bounds__(64 * grad_waves(TT), 2) void k_grad_tiled(TileArgs 
     // (behind the stream's end nothing new: the last step again, so that as many loads are under way as ever)
     if (fetch_left <= 0 && more) {
       for (;;) {
-        fetch_item += gridDim.x;
-        if (fetch_item >= items) {
+        if (++ahead.turn >= turns) {
           more = false;
           break;
         }
-        const Tile t = find(fetch_item);
+        const Tile t = find(ahead);
         if (t.terms == 0) continue;
         aim(t);
         break;
@@ -373,14 +384,13 @@ __global__ __launch_bounds__(64 * grad_waves(TT), 2) void k_grad_tiled(TileArgs 
       return *(const u32x4*)(stage + kOtherStage + (wn * kB + j) * 16 * kGradStep + read_at);
   };
 
-  if (first_item >= items) return;
   // the first tile that has terms at all
-  fetch_item = first_item - (int64_t)gridDim.x;
 #pragma unroll
   for (int s = 0; s < kStages; ++s) fetch();
   const uint8_t* stage = lds;
   // What a step begins with: all of g's operands, the first ones of the other.
-  constexpr int kAhead = 3;
+  constexpr int kAhead = 2, kBefore = kA - 2;
+  static_assert(kBefore + kAhead >= kA, "all of the stage is read");
   u32x4 b_head[kB], a_head[kAhead];
   const auto read_heads = [&]() {
     a_head[0] = read_other(stage, 0);
@@ -400,13 +410,29 @@ __global__ __launch_bounds__(64 * grad_waves(TT), 2) void k_grad_tiled(TileArgs 
   constexpr int kStores = kA * kB / (OT == EEP_F32 ? 1 : 2);  // of a whole tile, a wavefront's
   static_assert((kStages - 2) * kLoads + kStores < 64, "what the counter holds");
   int behind_stores = kStages;  // steps since a whole tile was stored
-  for (int64_t item = first_item; item < items; item += gridDim.x) {
-    const Tile t = find(item);
+  for (Walk here = {0, 0, 0}; here.turn < turns; ++here.turn) {
+    const Tile t = find(here);
+    const int rows_end = OF_W ? a.n : t.end;
     f32x4 acc[kA][kB];
 #pragma unroll
     for (int f = 0; f < kA; ++f)
 #pragma unroll
       for (int j = 0; j < kB; ++j) acc[f][j] = f32x4{0, 0, 0, 0};
+    // All wavefronts have read what they need of the stage and the next step's rows are there (no more than the fetches behind them are
+    // under way): the stage may be filled again and the next step's first operands are read.
+    const auto turn_over = [&](bool heads) {
+      // (Loads and stores count together, in order: the last tile's stores are newer than the rows of the next kStages - 1 steps.)
+      if (behind_stores < kStages - 1)
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kStages - 2) * kLoads + kStores) : "memory");
+      else
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kStages - 2) * kLoads) : "memory");
+      ++behind_stores;
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      stage = stage + kStage < lds + kStages * kStage ? stage + kStage : lds;
+      if (heads) read_heads();
+      fetch();
+    };
     const auto step = [&](int left, auto is_cut) {
       const auto ready = [&](u32x4 f) {
         if constexpr (decltype(is_cut)::value) cut<DT>(f, part, left);
@@ -424,31 +450,23 @@ __global__ __launch_bounds__(64 * grad_waves(TT), 2) void k_grad_tiled(TileArgs 
         __builtin_amdgcn_sched_barrier(0);
       };
 #pragma unroll
-      for (int f = 0; f < kA - 2; ++f) {
+      for (int f = 0; f < kBefore; ++f) {
         if (f + kAhead < kA) v[f + kAhead] = read_other(stage, f + kAhead);
         multiply(f);
       }
-      // This wavefront has read all it needs of the stage.  Once all have, and the next step's rows are there (no more than
-      // the fetches behind them are under way), the stage may be filled again and the next step's first operands are read.
-      // (Loads and stores count together, in order: the last tile's stores are newer than the rows of the next kStages - 1 steps.)
-      if (behind_stores < kStages - 1)
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kStages - 2) * kLoads + kStores) : "memory");
-      else
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kStages - 2) * kLoads) : "memory");
-      ++behind_stores;
-      __builtin_amdgcn_s_barrier();
-      asm volatile("" ::: "memory");
-      stage = stage + kStage < lds + kStages * kStage ? stage + kStage : lds;
-      read_heads();
-      fetch();
-      multiply(kA - 2);
-      multiply(kA - 1);
+      turn_over(true);
+#pragma unroll
+      for (int f = kBefore; f < kA; ++f) multiply(f);
     };
     int left = t.terms;
-    for (; left >= kDepth; left -= kDepth) step(left, std::false_type());
-    if (left > 0) step(left, std::true_type());
+    if (OF_W || t.row0 + wn * kB * 16 < rows_end) {
+      for (; left >= kDepth; left -= kDepth) step(left, std::false_type());
+      if (left > 0) step(left, std::true_type());
+    } else {
+      // (none of this wavefront's rows is one: it only takes part in the fetches)
+      for (; left > 0; left -= kDepth) turn_over(left <= kDepth);
+    }
 
-    const int rows_end = OF_W ? a.n : t.end;
     uint8_t* out = OF_W ? a.out + t.slot * a.stride : a.out;
     const int n0 = t.column0 + wm * (kA * 16);
     if (OF_W && a.accumulate != 0 && t.terms == 0) continue;  // (nothing to add)
