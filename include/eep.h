@@ -742,7 +742,8 @@ int eep_route_grad(const eep_router_shape* shape, const void* logits, const int3
  *   grad_x   device [rows, in_features] or NULL;  grad_w  device, slot p's begins p * grad_stride bytes in, or NULL.  Results may not
  *            overlap an operand; with a gate both may be NULL.
  * Row sizes, strides, limits and offsets are treated as eep_product_create and eep_expert_product treat them; rows 0 with grad_w
- * writes its zeros.  Calls with one handle may overlap. */
+ * writes its zeros.  The handle owns a workspace (64 MiB) for sums that are made in parts: calls with it share that, and may not
+ * overlap (one stream, or events between).  eep_product_grad_destroy waits for the device. */
 typedef struct {
   int32_t num_slots, in_features, out_features;
   int32_t dtype, grad_w_dtype;

@@ -91,7 +91,7 @@ class ExpertProductGrad(_Handle):
     """eep_product_grad: the gradients of an ExpertProduct of fp32 or bf16 operands (dtype: of grad_y, sums, grad_sums, x, w and
     grad_x).  gate: of one with a gate; `sums` then is what an ExpertProduct without one and 2 * out_features gives for the same x
     and w.  slot_stride and grad_stride: bytes from one slot's weights / gradients to the next one's (None: packed).  It belongs to
-    the device that is current here."""
+    the device that is current here.  Its calls share a workspace: they may not overlap (one stream, or events between)."""
 
     _destroy = "eep_product_grad_destroy"
 

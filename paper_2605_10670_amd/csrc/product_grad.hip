@@ -18,6 +18,7 @@ struct eep_product_grad {
   eep_product_grad_config cfg;
   int64_t slot_stride, grad_stride;  // bytes
   int cus;                           // of the device
+  float* partial;                    // kPartialBytes of sums over parts of the terms
 };
 
 namespace eep {
@@ -92,7 +93,9 @@ struct TileArgs {
   int n, k;           // weight rows (features of g), in_features
   int feature_tiles;  // of in_features
   int row_tiles;      // OF_W: of weight rows
-  int64_t stride;     // bytes, from one slot's weights (or gradients) to the next one's
+  int64_t stride;     // bytes, from one slot's weights to the next one's
+  int64_t out_stride; // OF_W: and of their gradients
+  int64_t plane;      // bytes, from one part's results to the next one's, where the terms are divided between gridDim.y
   int accumulate;
 };
 
@@ -230,7 +233,17 @@ __global__ __launch_bounds__(64 * grad_waves(TT), 2) void k_grad_tiled(TileArgs 
   const int col = lane & 15, part = lane >> 4;
 
   struct Tile {
-    int slot, column0, row0, first, end, terms;  // row0: of the result; first, end: the slot's rows (OF_W) or the tile's
+    int slot, column0, row0, first, end;  // row0: of the result; first, end: the slot's rows (OF_W) or the tile's
+    int start, terms;                     // of the sum: this part's
+  };
+  const auto divide = [&](Tile& t) {
+    t.start = 0;
+    if (gridDim.y > 1) {
+      const int64_t steps = (t.terms + kDepth - 1) / kDepth;
+      const int end = (int)(steps * (blockIdx.y + 1) / gridDim.y) * kDepth;
+      t.start = (int)(steps * blockIdx.y / gridDim.y) * kDepth;
+      t.terms = (end < t.terms ? end : t.terms) - t.start;
+    }
   };
   TileMap<kRows> map;
   int64_t items, per_slot = 0;
@@ -284,6 +297,7 @@ __global__ __launch_bounds__(64 * grad_waves(TT), 2) void k_grad_tiled(TileArgs 
       t.row0 = t.first;
       t.terms = a.n;
     }
+    divide(t);
     return t;
   };
 
@@ -301,7 +315,7 @@ __global__ __launch_bounds__(64 * grad_waves(TT), 2) void k_grad_tiled(TileArgs 
   // (terms past the end are read as the last ones, and cut off in the registers; columns likewise, and not stored)
   const auto aim = [&](const Tile& t) {
     fetch_left = t.terms;
-    other_at = OF_W ? a.other + t.first * k_bytes : a.other + t.slot * a.stride;
+    other_at = (OF_W ? a.other + t.first * k_bytes : a.other + t.slot * a.stride) + t.start * k_bytes;
     other_at += (int64_t)t.column0 * kSize;
 #pragma unroll
     for (int i = 0; i < Other::kLoads; ++i) {
@@ -312,7 +326,7 @@ __global__ __launch_bounds__(64 * grad_waves(TT), 2) void k_grad_tiled(TileArgs 
 #pragma unroll
       for (int i = 0; i < kGradLoads; ++i) {
         const int r = Grads::row(wave, lane, i), c = Grads::column(wave, lane, i), most = a.n - t.row0 - 16 / kSize;
-        grads_at[i] = a.g + t.first * n_bytes + (int64_t)t.row0 * kSize;
+        grads_at[i] = a.g + (t.first + t.start) * n_bytes + (int64_t)t.row0 * kSize;
         grads_off[i] = (uint32_t)r * (uint32_t)n_bytes + (uint32_t)(c < most ? c : most) * kSize;
       }
     } else {
@@ -321,7 +335,7 @@ __global__ __launch_bounds__(64 * grad_waves(TT), 2) void k_grad_tiled(TileArgs 
         // (16 rows at a time are within 32 bits, all of them may not be)
         const int r0 = (wave * kGradLoads + i) * 16, most = t.end > t.first ? t.end - 1 - t.first : 0;
         const int from = r0 < most ? r0 : most, r = r0 + load_row < most ? r0 + load_row : most;
-        grads_at[i] = a.g + (t.first + from) * n_bytes;
+        grads_at[i] = a.g + (t.first + from) * n_bytes + (int64_t)t.start * kSize;
         grads_off[i] = (uint32_t)(r - from) * (uint32_t)n_bytes + load_chunk * 16;
       }
     }
@@ -467,7 +481,7 @@ __global__ __launch_bounds__(64 * grad_waves(TT), 2) void k_grad_tiled(TileArgs 
       for (; left > 0; left -= kDepth) turn_over(left <= kDepth);
     }
 
-    uint8_t* out = OF_W ? a.out + t.slot * a.stride : a.out;
+    uint8_t* out = a.out + blockIdx.y * a.plane + (OF_W ? t.slot * a.out_stride : 0);
     const int n0 = t.column0 + wm * (kA * 16);
     if (OF_W && a.accumulate != 0 && t.terms == 0) continue;  // (nothing to add)
     constexpr int kOut = OT == EEP_F32 ? 4 : 2;
@@ -532,45 +546,119 @@ __global__ __launch_bounds__(64 * grad_waves(TT), 2) void k_grad_tiled(TileArgs 
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // nothing may still write to LDS when the workgroup is gone
 }
 
+// The parts' sums, added in their order: of rows of `width` values, of which those of the slots alone (offset NULL: all).
+struct PartArgs {
+  const float* partial;
+  const int32_t* offset;
+  uint8_t* out;
+  int64_t plane, slot_values, out_stride;  // values of a part and of a slot (0: one array), bytes from one slot's results to the next one's
+  int width, rows, slots, parts, accumulate;
+};
+template <bool BF16>
+__global__ __launch_bounds__(256) void k_grad_parts(PartArgs a) {
+  int64_t from = 0, to = a.plane;
+  if (a.offset != nullptr) {
+    from = (int64_t)clamp_row(a.offset[0], a.rows) * a.width;
+    to = (int64_t)clamp_row(a.offset[a.slots], a.rows) * a.width;
+  }
+  for (int64_t at = from + ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; at < to; at += (int64_t)gridDim.x * 1024) {
+    f32x4 sum = *(const f32x4*)(a.partial + at);
+    for (int p = 1; p < a.parts; ++p) sum += *(const f32x4*)(a.partial + p * a.plane + at);
+    const int64_t slot = a.slot_values != 0 ? at / a.slot_values : 0;
+    uint8_t* to_slot = a.out + slot * a.out_stride;
+    const int64_t in_slot = at - slot * a.slot_values;
+    if constexpr (BF16) {
+      u32x2* p = (u32x2*)to_slot + in_slot / 4;
+      if (a.accumulate != 0) {
+        const u32x2 d = *p;
+        sum += f32x4{bf16_lo(d[0]), bf16_hi(d[0]), bf16_lo(d[1]), bf16_hi(d[1])};
+      }
+      *p = u32x2{pack_bf16x2(sum[0], sum[1]), pack_bf16x2(sum[2], sum[3])};
+    } else {
+      f32x4* p = (f32x4*)to_slot + in_slot / 4;
+      if (a.accumulate != 0) sum += *p;
+      *p = sum;
+    }
+  }
+}
+
+// Where tiles are few, the terms of each are divided between several workgroups, whose sums are left in the workspace: into as many
+// parts as leave every CU something to do, of four steps at least.
+constexpr int64_t kPartialBytes = 64 << 20;  // (256 CUs' tiles of 256 by 256)
+static int grad_parts(int64_t work, int64_t most, int64_t steps, int64_t values) {
+  if (work <= 0 || 2 * work > most) return 1;
+  int64_t parts = most / work;
+  if (parts > steps / 4) parts = steps / 4;
+  if (parts > kPartialBytes / (values * (int64_t)sizeof(float))) parts = kPartialBytes / (values * (int64_t)sizeof(float));
+  return parts < 2 ? 1 : (int)parts;
+}
+
+// values, width: of the result, of one of its rows; terms: of a sum, about.
 template <int DT, int OT, bool OF_W, int TT>
-static hipError_t launch_grad_tiled(const TileArgs& a, int64_t work, int cus, hipStream_t st) {
-  const int64_t most = (int64_t)cus * grad_per_cu(TT);
-  hipLaunchKernelGGL((k_grad_tiled<DT, OT, OF_W, TT>), dim3((unsigned)(work < most ? work : most)), dim3(64 * grad_waves(TT)),
-                     grad_lds_bytes(TT), st, a);
+static hipError_t launch_grad_tiled(const TileArgs& a, const eep_product_grad& g, int64_t work, int64_t values, int64_t terms,
+                                    hipStream_t st) {
+  constexpr int kDepth = kGradStep / (DT == EEP_BF16 ? 2 : 4);
+  const int64_t most = (int64_t)g.cus * grad_per_cu(TT);
+  const unsigned grid = (unsigned)(work < most ? work : most);
+  const int parts = grad_parts(work, most, (terms + kDepth - 1) / kDepth, values);
+  if (parts == 1) {
+    hipLaunchKernelGGL((k_grad_tiled<DT, OT, OF_W, TT>), dim3(grid), dim3(64 * grad_waves(TT)), grad_lds_bytes(TT), st, a);
+    return hipGetLastError();
+  }
+  TileArgs part = a;
+  part.out = (uint8_t*)g.partial;
+  part.out_stride = (int64_t)a.n * a.k * (int64_t)sizeof(float);
+  part.plane = values * (int64_t)sizeof(float);
+  part.accumulate = 0;
+  hipLaunchKernelGGL((k_grad_tiled<DT, EEP_F32, OF_W, TT>), dim3(grid, (unsigned)parts), dim3(64 * grad_waves(TT)), grad_lds_bytes(TT), st,
+                     part);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const PartArgs sum = {g.partial, OF_W ? nullptr : a.offset, a.out, values, OF_W ? (int64_t)a.n * a.k : 0, a.out_stride, a.k,
+                        a.rows, a.slots, parts, OF_W ? a.accumulate : 0};
+  const int64_t blocks = (values / 4 + 255) / 256;
+  hipLaunchKernelGGL((k_grad_parts<OT == EEP_BF16>), dim3((unsigned)(blocks < 4 * g.cus ? blocks : 4 * g.cus)), dim3(256), 0, st, sum);
   return hipGetLastError();
 }
 
-// What the tiles of 64 * tt tokens cost, in time: what a step of one takes (us), as often as a CU has one.  A slot's last tile is half
-// empty on average.  Where there are two workgroups to a CU, a step of both.
-static float grad_x_cost(int tt, int64_t rows, int64_t slots, int64_t feature_tiles, int cus) {
-  const int64_t touched = rows < slots ? rows : slots;
-  float tiles = (float)rows / touched / (64 * tt) + 0.5f;
-  if (touched == 1) tiles = (float)((rows + 64 * tt - 1) / (64 * tt));
-  const float rounds = (tiles < 1.0f ? 1.0f : tiles) * touched * feature_tiles / (cus * grad_per_cu(tt));
-  const float step = tt == 4 ? 0.8f : tt == 2 ? 1.06f : 0.55f;
-  if (grad_per_cu(tt) == 2 && rounds <= 0.5f) return tt == 2 ? 0.62f : 0.4f;
-  return step * (rounds < 4.0f ? ceilf(rounds) : rounds);
+// What the tiles of 64 * tt tokens cost, us: what a step of one takes, as often as a CU has one, and the sum of parts.  A slot's last
+// tile is half empty on average.  Where there are two workgroups to a CU, a step of both, or of one alone.  (fp32 steps take four times
+// as long whatever the tile; the parts' sum then weighs less than it should.)
+static float grad_x_cost(int tt, const TileArgs& a, int64_t steps, int cus) {
+  const int64_t touched = a.rows < a.slots ? a.rows : a.slots, most = (int64_t)cus * grad_per_cu(tt);
+  float tiles = (float)a.rows / touched / (64 * tt) + 0.5f;
+  if (touched == 1) tiles = (float)((a.rows + 64 * tt - 1) / (64 * tt));
+  const float work = (tiles < 1.0f ? 1.0f : tiles) * touched * a.feature_tiles;
+  const int64_t values = (int64_t)a.rows * a.k;
+  const int parts = grad_parts((int64_t)work, most, steps, values);
+  const float rounds = work * parts / most;
+  float step = tt == 4 ? 0.8f : tt == 2 ? 1.06f : 0.55f;
+  if (grad_per_cu(tt) == 2 && rounds <= 0.5f) step = tt == 2 ? 0.62f : 0.4f;
+  const float time = step * steps / parts * (rounds < 4.0f ? ceilf(rounds) : rounds);
+  return parts == 1 ? time : time + 4.0f + parts * values * 8 / 5e6f;
 }
 
 template <int DT>
-static hipError_t launch_grad_x(TileArgs a, int cus, hipStream_t st) {
+static hipError_t launch_grad_x(TileArgs a, const eep_product_grad& g, hipStream_t st) {
   a.feature_tiles = (a.k + kGradCols - 1) / kGradCols;
   const int64_t touched = a.rows < a.slots ? a.rows : a.slots;
   const auto tiled = [&](auto tt) {
     constexpr int TT = decltype(tt)::value;
-    return launch_grad_tiled<DT, DT, false, TT>(a, (a.rows + touched * (64 * TT - 1)) / (64 * TT) * a.feature_tiles, cus, st);
+    return launch_grad_tiled<DT, DT, false, TT>(a, g, (a.rows + touched * (64 * TT - 1)) / (64 * TT) * a.feature_tiles,
+                                                (int64_t)a.rows * a.k, a.n, st);
   };
-  const float one = grad_x_cost(1, a.rows, a.slots, a.feature_tiles, cus), two = grad_x_cost(2, a.rows, a.slots, a.feature_tiles, cus),
-              four = grad_x_cost(4, a.rows, a.slots, a.feature_tiles, cus);
+  const int64_t steps = (a.n + kGradStep / (DT == EEP_BF16 ? 2 : 4) - 1) / (kGradStep / (DT == EEP_BF16 ? 2 : 4));
+  const float one = grad_x_cost(1, a, steps, g.cus), two = grad_x_cost(2, a, steps, g.cus), four = grad_x_cost(4, a, steps, g.cus);
   if (four <= one && four <= two) return tiled(std::integral_constant<int, 4>());
   return two <= one ? tiled(std::integral_constant<int, 2>()) : tiled(std::integral_constant<int, 1>());
 }
 
 template <int DT, int OT>
-static hipError_t launch_grad_w(TileArgs a, int cus, hipStream_t st) {
+static hipError_t launch_grad_w(TileArgs a, const eep_product_grad& g, hipStream_t st) {
   a.feature_tiles = (a.k + kGradCols - 1) / kGradCols;
   a.row_tiles = (a.n + 255) / 256;
-  return launch_grad_tiled<DT, OT, true, 4>(a, (int64_t)a.row_tiles * a.feature_tiles * a.slots, cus, st);
+  return launch_grad_tiled<DT, OT, true, 4>(a, g, (int64_t)a.row_tiles * a.feature_tiles * a.slots, (int64_t)a.slots * a.n * a.k,
+                                            a.rows / a.slots, st);
 }
 
 // More LDS than a kernel may have by default, on the current device.
@@ -580,6 +668,9 @@ static hipError_t allow_grad_lds() {
     return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, grad_lds_bytes(tt));
   };
   hipError_t e = allow((const void*)k_grad_tiled<DT, DT, false, 1>, 1);
+  if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, EEP_F32, false, 1>, 1);
+  if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, EEP_F32, false, 2>, 2);
+  if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, EEP_F32, false, 4>, 4);
   if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, DT, false, 2>, 2);
   if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, DT, false, 4>, 4);
   if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, EEP_F32, true, 4>, 4);
@@ -623,7 +714,8 @@ int eep_product_grad_create(const eep_product_grad_config* cfg, eep_product_grad
   int device = 0;
   if (hipGetDevice(&device) != hipSuccess ||
       hipDeviceGetAttribute(&g->cus, hipDeviceAttributeMultiprocessorCount, device) != hipSuccess ||
-      (f.dtype == EEP_BF16 ? allow_grad_lds<EEP_BF16>() : allow_grad_lds<EEP_F32>()) != hipSuccess) {
+      (f.dtype == EEP_BF16 ? allow_grad_lds<EEP_BF16>() : allow_grad_lds<EEP_F32>()) != hipSuccess ||
+      hipMalloc((void**)&g->partial, kPartialBytes) != hipSuccess) {
     (void)hipGetLastError();
     delete g;
     return EEP_ERR_HIP;
@@ -634,9 +726,9 @@ int eep_product_grad_create(const eep_product_grad_config* cfg, eep_product_grad
 
 int eep_product_grad_destroy(eep_product_grad* grad) {
   if (!grad) return EEP_OK;
-  const hipError_t e = hipDeviceSynchronize();
+  const hipError_t e = hipDeviceSynchronize(), e2 = hipFree(grad->partial);
   delete grad;
-  return e == hipSuccess ? EEP_OK : EEP_ERR_HIP;
+  return e == hipSuccess && e2 == hipSuccess ? EEP_OK : EEP_ERR_HIP;
 }
 
 int eep_product_grad_run(eep_product_grad* grad, const void* grad_y, const void* sums, const void* x, const void* w,
@@ -691,15 +783,15 @@ int eep_product_grad_run(eep_product_grad* grad, const void* grad_y, const void*
     a.other = (const uint8_t*)w;
     a.out = (uint8_t*)grad_x;
     a.stride = grad->slot_stride;
-    e = bf16 ? launch_grad_x<EEP_BF16>(a, grad->cus, st) : launch_grad_x<EEP_F32>(a, grad->cus, st);
+    e = bf16 ? launch_grad_x<EEP_BF16>(a, *grad, st) : launch_grad_x<EEP_F32>(a, *grad, st);
   }
   if (e == hipSuccess && grad_w) {
     a.other = (const uint8_t*)x;
     a.out = (uint8_t*)grad_w;
-    a.stride = grad->grad_stride;
+    a.out_stride = grad->grad_stride;
     const bool out16 = f.grad_w_dtype == EEP_BF16;
-    e = bf16 ? (out16 ? launch_grad_w<EEP_BF16, EEP_BF16>(a, grad->cus, st) : launch_grad_w<EEP_BF16, EEP_F32>(a, grad->cus, st))
-             : (out16 ? launch_grad_w<EEP_F32, EEP_BF16>(a, grad->cus, st) : launch_grad_w<EEP_F32, EEP_F32>(a, grad->cus, st));
+    e = bf16 ? (out16 ? launch_grad_w<EEP_BF16, EEP_BF16>(a, *grad, st) : launch_grad_w<EEP_BF16, EEP_F32>(a, *grad, st))
+             : (out16 ? launch_grad_w<EEP_F32, EEP_BF16>(a, *grad, st) : launch_grad_w<EEP_F32, EEP_F32>(a, *grad, st));
   }
   return e == hipSuccess ? EEP_OK : EEP_ERR_HIP;
 }

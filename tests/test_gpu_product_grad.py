@@ -229,7 +229,19 @@ def test_against_differences(gate):
         assert abs(slope - want) < 80 * 4 * 2.0 ** -20 / step + 80 * step ** 2, name
 
 
-@pytest.mark.parametrize("counts", [[40, 0, 300, 2], [2, 1, 0, 3]], ids=str)
+@pytest.mark.parametrize("dtype,w_dtype", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32")])
+@pytest.mark.parametrize("counts,K,I", [([1], 64, 4096), ([700], 264, 1032), ([2000, 0, 1500], 72, 64), ([3, 0, 1, 9, 0], 520, 2048)], ids=str)
+def test_sums_in_parts(dtype, w_dtype, counts, K, I):
+    """Few tiles of many terms: divided between workgroups."""
+    c = Case(len(counts), counts, K, I, dtype=dtype, spare=2)
+    h = c.handle(w_dtype)
+    c.check(c.run(h, w_dtype))
+    old = lu.randn(lu.gen(8), c.P, c.N, c.K).to(TORCH_OF[w_dtype])
+    c.check(c.run(h, w_dtype, old=old, wanted="w"), old=old)
+    h.destroy()
+
+
+@pytest.mark.parametrize("counts", [[40, 0, 300, 2], [2, 1, 0, 3], [900, 500, 0, 0]], ids=str)
 def test_captured_and_replayed(counts):
     """One graph for all row counts: the offsets are read on the device."""
     c = Case(10, counts, 264, 72, gate=True)
