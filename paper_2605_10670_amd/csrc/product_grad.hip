@@ -563,21 +563,29 @@ __global__ __launch_bounds__(256) void k_grad_parts(PartArgs a) {
   }
   for (int64_t at = from + ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; at < to; at += (int64_t)gridDim.x * 1024) {
     f32x4 sum = *(const f32x4*)(a.partial + at);
-    for (int p = 1; p < a.parts; ++p) sum += *(const f32x4*)(a.partial + p * a.plane + at);
+    int p = 1;
+    for (; p + 8 <= a.parts; p += 8) {  // eight under way together
+      f32x4 v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = *(const f32x4*)(a.partial + (p + i) * a.plane + at);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum += v[i];
+    }
+    for (; p < a.parts; ++p) sum += *(const f32x4*)(a.partial + p * a.plane + at);
     const int64_t slot = a.slot_values != 0 ? at / a.slot_values : 0;
     uint8_t* to_slot = a.out + slot * a.out_stride;
     const int64_t in_slot = at - slot * a.slot_values;
     if constexpr (BF16) {
-      u32x2* p = (u32x2*)to_slot + in_slot / 4;
+      u32x2* o = (u32x2*)to_slot + in_slot / 4;
       if (a.accumulate != 0) {
-        const u32x2 d = *p;
+        const u32x2 d = *o;
         sum += f32x4{bf16_lo(d[0]), bf16_hi(d[0]), bf16_lo(d[1]), bf16_hi(d[1])};
       }
-      *p = u32x2{pack_bf16x2(sum[0], sum[1]), pack_bf16x2(sum[2], sum[3])};
+      *o = u32x2{pack_bf16x2(sum[0], sum[1]), pack_bf16x2(sum[2], sum[3])};
     } else {
-      f32x4* p = (f32x4*)to_slot + in_slot / 4;
-      if (a.accumulate != 0) sum += *p;
-      *p = sum;
+      f32x4* o = (f32x4*)to_slot + in_slot / 4;
+      if (a.accumulate != 0) sum += *o;
+      *o = sum;
     }
   }
 }
