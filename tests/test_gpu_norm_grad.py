@@ -92,6 +92,39 @@ def test_no_rows_give_zeros_or_leave_what_is_there():
     assert (gg == 0).all() and (gb == 0).all()
 
 
+def test_values_of_both_signs_at_the_end_of_fp32():
+    """Sums of neighbours vanish, of others overflow; the squares do everywhere."""
+    T, H = 2, 1024
+    g = lu.gen(12)
+    h = 3e38 * (1 - 2 * (torch.arange(H) % 2).float()).expand(T, H) * (0.5 + 0.5 * torch.rand((T, H), generator=g))
+    h[1] = h[1].sort().values
+    gain, gy = torch.ones(H), lu.randn(g, T, H)
+    y = torch.empty((T, H), device="cuda")
+    layer.LayerNorm(hidden=H, in_dtype="f32", gain_dtype="f32", out_dtype="f32").run(h.cuda(), gain.cuda(), T, y=y)
+    _, want, err = gr.layer_norm(h, None, gain, None, 1e-5)
+    gr.check("y", y, want, err)
+    for centred in (False, True):
+        gg = torch.empty(H, device="cuda")
+        layer.NormGrad(hidden=H, in_dtype="f32", gain_dtype="f32", out_dtype="f32", centred=centred, epsilon=1e-5).run(
+            h.cuda(), gain.cuda(), gy.cuda(), T, grad_gain=gg)
+        gr.check("grad_gain", gg, *gr.norm_grad(h, gain, gy, None, centred, 1e-5)["grad_gain"])
+
+
+def test_infinities_and_nans_stay_in_their_rows():
+    T, H = 6, 2048
+    g = lu.gen(13)
+    h, gy = lu.randn(g, T, H), lu.randn(g, T, H)
+    h[1, 3], h[2, 4], h[3, 5] = float("inf"), float("nan"), -float("inf")
+    gy[4, 7] = float("nan")
+    gain = torch.ones(H, device="cuda")
+    y, out = torch.empty((T, H), device="cuda"), torch.empty((T, H), device="cuda")
+    layer.LayerNorm(hidden=H, in_dtype="f32", gain_dtype="f32", out_dtype="f32").run(h.cuda(), gain, T, y=y)
+    assert (~y.isfinite()).any(dim=1).tolist() == [False, True, True, True, False, False]
+    for centred in (False, True):
+        layer.NormGrad(hidden=H, in_dtype="f32", gain_dtype="f32", out_dtype="f32", centred=centred).run(h.cuda(), gain, gy.cuda(), T, grad_h=out)
+        assert (~out.isfinite()).any(dim=1).tolist() == [False, True, True, True, True, False]
+
+
 @pytest.mark.parametrize("scale", [1e-30, 1e25, 1e37])
 @pytest.mark.parametrize("centred", [False, True])
 def test_rows_whose_squares_leave_fp32(scale, centred):
@@ -116,10 +149,11 @@ def test_rows_whose_squares_leave_fp32(scale, centred):
         gr.check("y", y, want, err)
 
 
-def test_rows_of_one_value():
+@pytest.mark.parametrize("value", [3.0, 0.0, 2.0 ** 126])
+def test_rows_of_one_value(value):
     """d is nothing: the layer norm is its bias, and the gradient that of a row of zeros."""
     T, H = 2, 512
-    h = torch.full((T, H), 3.0, device="cuda")
+    h = torch.full((T, H), value, device="cuda")
     gain, bias = torch.full((H,), 2.0, device="cuda"), torch.arange(H, device="cuda").float()
     y = torch.empty((T, H), device="cuda")
     layer.LayerNorm(hidden=H, in_dtype="f32", gain_dtype="f32", out_dtype="f32").run(h, gain, T, bias=bias, y=y)
