@@ -78,7 +78,7 @@ __global__ __launch_bounds__(256) void k_gate_grad(GateGradArgs a, int64_t first
 }
 
 // ---------------------------------------------------------------------------
-// tiles: 256 in_features by 64 * TT rows of the result, which are tokens (OF_W false: the rows' gradient, summed over the
+// tiles: 256 in_features by 64 * TT rows (TT 0: 16) of the result, which are tokens (OF_W false: the rows' gradient, summed over the
 // weights' rows) or weight rows (OF_W: the weights' gradient, summed over a slot's tokens).
 //
 // As in product.hip the in_features are the matrix cores' rows, so that a lane has four neighbouring ones of one row of the
@@ -100,10 +100,11 @@ struct TileArgs {
 };
 
 constexpr int kGradCols = 256, kGradStep = 64;  // bytes along the sum
+constexpr int grad_rows(int tt) { return tt == 0 ? 16 : 64 * tt; }
 constexpr int grad_waves(int tt) { return tt == 4 ? 8 : 4; }
-constexpr int grad_across(int tt) { return tt == 1 ? 4 : 2; }  // wavefronts side by side on the columns
+constexpr int grad_across(int tt) { return tt <= 1 ? 4 : 2; }  // wavefronts side by side on the columns
 constexpr int grad_stages(int tt) { return tt == 2 ? 3 : 4; }
-constexpr int grad_stage_bytes(int tt) { return (kGradCols + 64 * tt) * kGradStep; }
+constexpr int grad_stage_bytes(int tt) { return (kGradCols + grad_rows(tt)) * kGradStep; }
 constexpr int grad_lds_bytes(int tt) { return grad_stages(tt) * grad_stage_bytes(tt); }
 constexpr int grad_per_cu(int tt) { return tt == 4 ? 1 : 2; }  // workgroups
 
@@ -217,13 +218,13 @@ __device__ __forceinline__ void cut(u32x4& f, int part, int left) {
 template <int DT, int OT, bool OF_W, int TT>
 __global__ __launch_bounds__(64 * grad_waves(TT), 2) void k_grad_tiled(TileArgs a) {
   constexpr int kWaves = grad_waves(TT), kWM = grad_across(TT), kWN = kWaves / kWM;
-  constexpr int kA = kGradCols / 16 / kWM, kB = 4 * TT / kWN;  // tiles of 16 columns and of 16 rows a wavefront
-  constexpr int kRows = 64 * TT, kStages = grad_stages(TT), kStage = grad_stage_bytes(TT);
+  constexpr int kRows = grad_rows(TT), kStages = grad_stages(TT), kStage = grad_stage_bytes(TT);
+  constexpr int kA = kGradCols / 16 / kWM, kB = kRows / 16 / kWN;  // tiles of 16 columns and of 16 rows a wavefront
   typedef Across<DT, kGradCols, kWaves> Other;
   typedef Across<DT, OF_W ? kRows : kGradCols, kWaves> Grads;  // (where they lie across too)
   constexpr int kSize = Other::kSize, kDepth = Other::kDepth;
   constexpr int kOtherStage = kGradCols * kGradStep;
-  constexpr int kGradLoads = OF_W ? Grads::kLoads : kRows / 16 / kWaves;  // of g, a wavefront's; 16 rows each where they lie along
+  constexpr int kGradLoads = OF_W ? Grads::kLoads : TT == 0 ? 1 : kRows / 16 / kWaves;  // of g, a wavefront's; 16 rows each where they lie along
   constexpr int kLoads = Other::kLoads + kGradLoads;  // of a step
   extern __shared__ __align__(1024) uint8_t lds[];
 
@@ -333,7 +334,7 @@ __global__ __launch_bounds__(64 * grad_waves(TT), 2) void k_grad_tiled(TileArgs 
 #pragma unroll
       for (int i = 0; i < kGradLoads; ++i) {
         // (16 rows at a time are within 32 bits, all of them may not be)
-        const int r0 = (wave * kGradLoads + i) * 16, most = t.end > t.first ? t.end - 1 - t.first : 0;
+        const int r0 = TT == 0 ? 0 : (wave * kGradLoads + i) * 16, most = t.end > t.first ? t.end - 1 - t.first : 0;
         const int from = r0 < most ? r0 : most, r = r0 + load_row < most ? r0 + load_row : most;
         grads_at[i] = a.g + (t.first + from) * n_bytes + (int64_t)t.start * kSize;
         grads_off[i] = (uint32_t)(r - from) * (uint32_t)n_bytes + load_chunk * 16;
@@ -378,7 +379,8 @@ __global__ __launch_bounds__(64 * grad_waves(TT), 2) void k_grad_tiled(TileArgs 
     for (int i = 0; i < Other::kLoads; ++i) load_to_lds(other_at, other_off[i], to + wave * (Other::kLoads - 1) * 1024 + i * 1024);
 #pragma unroll
     for (int i = 0; i < kGradLoads; ++i)
-      load_to_lds(grads_at[i], grads_off[i], to + kOtherStage + wave * (kGradLoads - 1) * 1024 + i * 1024);
+      // (of 16 rows all wavefronts bring the same)
+      load_to_lds(grads_at[i], grads_off[i], to + kOtherStage + (TT == 0 ? -wave * 1024 : wave * (kGradLoads - 1) * 1024 + i * 1024));
     stage_at = stage_at + 1 < kStages ? stage_at + 1 : 0;
     if (!again) {
       fetch_left -= kDepth;
@@ -629,19 +631,20 @@ static hipError_t launch_grad_tiled(const TileArgs& a, const eep_product_grad& g
   return hipGetLastError();
 }
 
-// What the tiles of 64 * tt tokens cost, us: what a step of one takes, as often as a CU has one, and the sum of parts.  A slot's last
-// tile is half empty on average.  Where there are two workgroups to a CU, a step of both, or of one alone.  (fp32 steps take four times
-// as long whatever the tile; the parts' sum then weighs less than it should.)
-static float grad_x_cost(int tt, const TileArgs& a, int64_t steps, int cus) {
-  const int64_t touched = a.rows < a.slots ? a.rows : a.slots, most = (int64_t)cus * grad_per_cu(tt);
-  float tiles = (float)a.rows / touched / (64 * tt) + 0.5f;
-  if (touched == 1) tiles = (float)((a.rows + 64 * tt - 1) / (64 * tt));
+// What the tiles of so many tokens cost, us: what a step of one takes, as often as a CU has one, and the sum of parts.  A slot's last
+// tile is half empty on average.  Where there are two workgroups to a CU, a step of both, or of one alone.  fp32 products take the matrix
+// cores 16 times as long as bf16 ones, on half as many terms a step.
+static float grad_x_cost(int tt, bool f32, const TileArgs& a, int64_t steps, int cus) {
+  const int64_t touched = a.rows < a.slots ? a.rows : a.slots, most = (int64_t)cus * grad_per_cu(tt), rows = grad_rows(tt);
+  float tiles = (float)a.rows / touched / rows + 0.5f;
+  if (touched == 1) tiles = (float)((a.rows + rows - 1) / rows);
   const float work = (tiles < 1.0f ? 1.0f : tiles) * touched * a.feature_tiles;
   const int64_t values = (int64_t)a.rows * a.k;
   const int parts = grad_parts((int64_t)work, most, steps, values);
   const float rounds = work * parts / most;
-  float step = tt == 4 ? 0.8f : tt == 2 ? 1.06f : 0.55f;
-  if (grad_per_cu(tt) == 2 && rounds <= 0.5f) step = tt == 2 ? 0.62f : 0.4f;
+  const bool alone = grad_per_cu(tt) == 2 && rounds <= 0.5f;
+  float step = tt == 4 ? 0.8f : tt == 2 ? (alone ? 0.62f : 1.06f) : tt == 1 ? (alone ? 0.4f : 0.55f) : (alone ? 0.35f : 0.5f);
+  if (f32) step = tt == 4 ? 4.1f : tt == 2 ? (alone ? 2.1f : 4.1f) : tt == 1 ? (alone ? 1.1f : 2.1f) : (alone ? 0.4f : 0.6f);
   const float time = step * steps / parts * (rounds < 4.0f ? ceilf(rounds) : rounds);
   return parts == 1 ? time : time + 4.0f + parts * values * 8 / 5e6f;
 }
@@ -652,13 +655,26 @@ static hipError_t launch_grad_x(TileArgs a, const eep_product_grad& g, hipStream
   const int64_t touched = a.rows < a.slots ? a.rows : a.slots;
   const auto tiled = [&](auto tt) {
     constexpr int TT = decltype(tt)::value;
-    return launch_grad_tiled<DT, DT, false, TT>(a, g, (a.rows + touched * (64 * TT - 1)) / (64 * TT) * a.feature_tiles,
+    return launch_grad_tiled<DT, DT, false, TT>(a, g, (a.rows + touched * (grad_rows(TT) - 1)) / grad_rows(TT) * a.feature_tiles,
                                                 (int64_t)a.rows * a.k, a.n, st);
   };
-  const int64_t steps = (a.n + kGradStep / (DT == EEP_BF16 ? 2 : 4) - 1) / (kGradStep / (DT == EEP_BF16 ? 2 : 4));
-  const float one = grad_x_cost(1, a, steps, g.cus), two = grad_x_cost(2, a, steps, g.cus), four = grad_x_cost(4, a, steps, g.cus);
-  if (four <= one && four <= two) return tiled(std::integral_constant<int, 4>());
-  return two <= one ? tiled(std::integral_constant<int, 2>()) : tiled(std::integral_constant<int, 1>());
+  constexpr int kDepth = kGradStep / (DT == EEP_BF16 ? 2 : 4);
+  const int sizes[] = {4, 2, 1, 0};
+  int best = 4;
+  float least = INFINITY;
+  for (const int tt : sizes) {
+    const float cost = grad_x_cost(tt, DT == EEP_F32, a, (a.n + kDepth - 1) / kDepth, g.cus);
+    if (cost < least) {
+      least = cost;
+      best = tt;
+    }
+  }
+  switch (best) {
+    case 4: return tiled(std::integral_constant<int, 4>());
+    case 2: return tiled(std::integral_constant<int, 2>());
+    case 1: return tiled(std::integral_constant<int, 1>());
+    default: return tiled(std::integral_constant<int, 0>());
+  }
 }
 
 template <int DT, int OT>
@@ -675,7 +691,9 @@ static hipError_t allow_grad_lds() {
   const auto allow = [](const void* kernel, int tt) {
     return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, grad_lds_bytes(tt));
   };
-  hipError_t e = allow((const void*)k_grad_tiled<DT, DT, false, 1>, 1);
+  hipError_t e = allow((const void*)k_grad_tiled<DT, DT, false, 0>, 0);
+  if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, EEP_F32, false, 0>, 0);
+  if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, DT, false, 1>, 1);
   if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, EEP_F32, false, 1>, 1);
   if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, EEP_F32, false, 2>, 2);
   if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, EEP_F32, false, 4>, 4);
