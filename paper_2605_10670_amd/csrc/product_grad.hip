@@ -100,12 +100,12 @@ struct TileArgs {
 };
 
 constexpr int kGradCols = 256, kGradStep = 64;  // bytes along the sum
+constexpr int kGradStages = 4;
 constexpr int grad_rows(int tt) { return tt == 0 ? 16 : 64 * tt; }
 constexpr int grad_waves(int tt) { return tt == 4 ? 8 : 4; }
-constexpr int grad_across(int tt) { return tt <= 1 ? 4 : 2; }  // wavefronts side by side on the columns
-constexpr int grad_stages(int tt) { return tt == 2 ? 3 : 4; }
+constexpr int grad_across(int tt) { return tt == 4 ? 2 : 4; }  // wavefronts side by side on the columns
 constexpr int grad_stage_bytes(int tt) { return (kGradCols + grad_rows(tt)) * kGradStep; }
-constexpr int grad_lds_bytes(int tt) { return grad_stages(tt) * grad_stage_bytes(tt); }
+constexpr int grad_lds_bytes(int tt) { return kGradStages * grad_stage_bytes(tt); }
 constexpr int grad_per_cu(int tt) { return tt == 4 ? 1 : 2; }  // workgroups
 
 // One step of 16 rows (columns): lane l has four dwords of row l % 16, terms from 16 * (l / 16) bytes on.
@@ -218,7 +218,7 @@ __device__ __forceinline__ void cut(u32x4& f, int part, int left) {
 template <int DT, int OT, bool OF_W, int TT>
 __global__ __launch_bounds__(64 * grad_waves(TT), 2) void k_grad_tiled(TileArgs a) {
   constexpr int kWaves = grad_waves(TT), kWM = grad_across(TT), kWN = kWaves / kWM;
-  constexpr int kRows = grad_rows(TT), kStages = grad_stages(TT), kStage = grad_stage_bytes(TT);
+  constexpr int kRows = grad_rows(TT), kStages = kGradStages, kStage = grad_stage_bytes(TT);
   constexpr int kA = kGradCols / 16 / kWM, kB = kRows / 16 / kWN;  // tiles of 16 columns and of 16 rows a wavefront
   typedef Across<DT, kGradCols, kWaves> Other;
   typedef Across<DT, OF_W ? kRows : kGradCols, kWaves> Grads;  // (where they lie across too)
@@ -631,9 +631,12 @@ static hipError_t launch_grad_tiled(const TileArgs& a, const eep_product_grad& g
   return hipGetLastError();
 }
 
-// What the tiles of so many tokens cost, us: what a step of one takes, as often as a CU has one, and the sum of parts.  A slot's last
-// tile is half empty on average.  Where there are two workgroups to a CU, a step of both, or of one alone.  fp32 products take the matrix
-// cores 16 times as long as bf16 ones, on half as many terms a step.
+// What the tiles of 256, 64 or 16 tokens cost, us: what a step of one takes, as often as a CU has one, and the sum of parts.  A slot's
+// last tile is half empty on average.  Where there are two workgroups to a CU, a step of both, or of one alone.  fp32 products take the
+// matrix cores 16 times as long as bf16 ones, on half as many terms a step.  Measured, 16 / 64 / 256 tokens a tile, us, bf16: 144 slots
+// 1024 -> 4096, 64 tokens by top-8 217 / 226 / 247, 300 242 / 240 / 262, 1200 406 / 271 / 272, 2400 708 / 342 / 339; 120 slots 2880 -> 2816,
+// top-6, 400 tokens 408 / 357 / 379, 1600 814 / 480 / 456, 5976 - / 973 / 800; one matrix 2048 -> 7168, 64 rows 19 / 26 / 24, 256 35 / 29 / 41,
+// 2048 211 / 90 / 83, 8192 785 / 282 / 224.  (Tiles of 128 were between the two, and best nowhere.)
 static float grad_x_cost(int tt, bool f32, const TileArgs& a, int64_t steps, int cus) {
   const int64_t touched = a.rows < a.slots ? a.rows : a.slots, most = (int64_t)cus * grad_per_cu(tt), rows = grad_rows(tt);
   float tiles = (float)a.rows / touched / rows + 0.5f;
@@ -643,8 +646,8 @@ static float grad_x_cost(int tt, bool f32, const TileArgs& a, int64_t steps, int
   const int parts = grad_parts((int64_t)work, most, steps, values);
   const float rounds = work * parts / most;
   const bool alone = grad_per_cu(tt) == 2 && rounds <= 0.5f;
-  float step = tt == 4 ? 0.8f : tt == 2 ? (alone ? 0.62f : 1.06f) : tt == 1 ? (alone ? 0.4f : 0.55f) : (alone ? 0.35f : 0.5f);
-  if (f32) step = tt == 4 ? 4.1f : tt == 2 ? (alone ? 2.1f : 4.1f) : tt == 1 ? (alone ? 1.1f : 2.1f) : (alone ? 0.4f : 0.6f);
+  float step = tt == 4 ? 0.95f : tt == 1 ? (alone ? 0.4f : 0.75f) : (alone ? 0.35f : 0.5f);
+  if (f32) step = tt == 4 ? 4.1f : tt == 1 ? (alone ? 1.1f : 2.1f) : (alone ? 0.4f : 0.6f);
   const float time = step * steps / parts * (rounds < 4.0f ? ceilf(rounds) : rounds);
   return parts == 1 ? time : time + 4.0f + parts * values * 8 / 5e6f;
 }
@@ -659,7 +662,7 @@ static hipError_t launch_grad_x(TileArgs a, const eep_product_grad& g, hipStream
                                                 (int64_t)a.rows * a.k, a.n, st);
   };
   constexpr int kDepth = kGradStep / (DT == EEP_BF16 ? 2 : 4);
-  const int sizes[] = {4, 2, 1, 0};
+  const int sizes[] = {4, 1, 0};
   int best = 4;
   float least = INFINITY;
   for (const int tt : sizes) {
@@ -671,7 +674,6 @@ static hipError_t launch_grad_x(TileArgs a, const eep_product_grad& g, hipStream
   }
   switch (best) {
     case 4: return tiled(std::integral_constant<int, 4>());
-    case 2: return tiled(std::integral_constant<int, 2>());
     case 1: return tiled(std::integral_constant<int, 1>());
     default: return tiled(std::integral_constant<int, 0>());
   }
@@ -695,9 +697,7 @@ static hipError_t allow_grad_lds() {
   if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, EEP_F32, false, 0>, 0);
   if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, DT, false, 1>, 1);
   if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, EEP_F32, false, 1>, 1);
-  if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, EEP_F32, false, 2>, 2);
   if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, EEP_F32, false, 4>, 4);
-  if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, DT, false, 2>, 2);
   if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, DT, false, 4>, 4);
   if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, EEP_F32, true, 4>, 4);
   if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, EEP_BF16, true, 4>, 4);

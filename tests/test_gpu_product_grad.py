@@ -241,6 +241,18 @@ def test_sums_in_parts(dtype, w_dtype, counts, K, I):
     h.destroy()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("counts,K,I", [([2990, 3003, 1, 2816], 2056, 72), ([60] * 39 + [61], 2056, 72), ([3, 0, 17, 1] * 60, 1032, 136),
+                                        ([10700], 1288, 72)], ids=["256", "64", "16", "one"])
+def test_tiles_of_every_size(dtype, counts, K, I):
+    """Enough tokens a slot, and slots, for tiles of 256, 64 and 16 tokens, several to a workgroup."""
+    c = Case(sum(counts), counts, K, I, dtype=dtype)
+    h = c.handle("bf16")
+    c.check(c.run(h, wanted="x"))
+    c.check(c.run(h, wanted="w"))
+    h.destroy()
+
+
 @pytest.mark.parametrize("counts", [[40, 0, 300, 2], [2, 1, 0, 3], [900, 500, 0, 0]], ids=str)
 def test_captured_and_replayed(counts):
     """One graph for all row counts: the offsets are read on the device."""
