@@ -14,7 +14,7 @@ namespace eep {
 
 constexpr int kNormMaxWidth = 65536;
 
-// Sums over the workgroup of K values, in every thread, added in the order of the wavefronts.  Successive sums take the two buffers
+// Sums over the workgroup of K values, in every thread, always added in the same order.  Successive sums take the two buffers
 // in turn, so that one barrier each is enough.
 constexpr int kSums = 4;
 struct BlockSums {
@@ -31,12 +31,9 @@ __device__ __forceinline__ void block_sum(float (&v)[K], BlockSums& s, int& turn
     for (int i = 0; i < K; ++i) s.part[turn][threadIdx.x >> 6][i] = v[i];
   }
   __syncthreads();
+  const int w = threadIdx.x & 15;
 #pragma unroll
-  for (int i = 0; i < K; ++i) v[i] = 0.0f;
-  for (int w = 0; w < threads / 64; ++w) {
-#pragma unroll
-    for (int i = 0; i < K; ++i) v[i] += s.part[turn][w][i];
-  }
+  for (int i = 0; i < K; ++i) v[i] = lane_sum<16>(w < threads / 64 ? s.part[turn][w][i] : 0.0f);
   turn ^= 1;
 }
 
@@ -202,8 +199,9 @@ static hipError_t launch_layer_norm(const LayerNormArgs& a, int T, hipStream_t s
 //
 // A workgroup goes over every so manieth row; a thread has the same channels of each, whose gain and bias sums stay in its
 // registers, and the next row's loads are under way while this one's sums cross the workgroup.  The sums of the workgroups
-// are left in the workspace and added up, in their order, by a second kernel.  Bound by memory: 16384 rows of 7168 bf16 with grad_sum 174 us
-// (5.4 TB/s; with four exchanges a row, the gain from memory and one workgroup to a CU 242); 64 centred rows 7 + 3.3 us, latency.
+// are left in the workspace and added up, in their order, by a second kernel.  Bound by memory: 16384 rows of 7168 bf16 with grad_sum 159 to 174 us
+// (5.4 to 5.9 TB/s; with four exchanges a row, the gain from memory and one workgroup to a CU 242; 1 / 4 / 8 workgroups a CU 233 / 165 / 192; up
+// to 1024 / 256 threads 167 / 257; plain stores 170); 64 centred rows 10.1, latency (12.2 with two vectors a thread).
 // ---------------------------------------------------------------------------
 struct NormGradArgs {
   const void *h, *gain, *grad_y, *grad_sum;
@@ -231,8 +229,8 @@ struct Raw8 {
 };
 
 // Workgroups to a CU: as many as registers allow; the rows of fp32 inputs are twice as many bytes under way.
-constexpr int norm_grad_threads(int nv) { return nv == 8 ? 1024 : 512; }
-constexpr int norm_grad_waves(bool in_bf16, int nv) { return nv == 8 ? 4 : in_bf16 && nv <= 2 ? 4 : 2; }
+constexpr int norm_grad_threads(int nv) { return nv == 8 || nv == 1 ? 1024 : 512; }
+constexpr int norm_grad_waves(bool in_bf16, int nv) { return nv == 8 || nv == 1 || (in_bf16 && nv <= 2) ? 4 : 2; }
 
 template <bool IN_BF16, bool OUT_BF16, bool CENTRED, int NV>
 __global__ __launch_bounds__(norm_grad_threads(NV), norm_grad_waves(IN_BF16, NV)) void k_norm_grad(NormGradArgs a) {
@@ -403,10 +401,11 @@ __global__ __launch_bounds__(64 * kColumnRuns) void k_norm_columns(const float* 
 }
 
 template <bool IN_BF16, bool OUT_BF16, bool CENTRED>
-static hipError_t launch_norm_grad(const NormGradArgs& a, int groups, hipStream_t st) {
+static hipError_t launch_norm_grad(const NormGradArgs& a, int groups, int most_groups, hipStream_t st) {
   const int vecs = a.H / 8;
-  int nv = 1;
-  while (nv < 8 && vecs > nv * 512) nv *= 2;
+  int nv = 1;  // vectors a thread: one where rows are fewer than CUs and latency counts, else so many that threads are up to 512
+  if (a.T > most_groups / 2 || vecs > 1024)
+    while (nv < 8 && vecs > nv * 512) nv *= 2;
   const dim3 grid((unsigned)groups), block((unsigned)(((vecs + nv - 1) / nv + 63) / 64 * 64));
   const size_t lds = nv <= 2 ? (size_t)a.H * sizeof(float) : 0;
   switch (nv) {
@@ -495,14 +494,14 @@ int eep_norm_grad_run(eep_norm_grad* grad, const void* h, const void* gain, cons
   hipError_t e = hipSuccess;
   if (T > 0) {
     switch ((f.in_dtype == EEP_BF16) * 4 + (f.out_dtype == EEP_BF16) * 2 + f.centred) {
-      case 0: e = launch_norm_grad<false, false, false>(a, groups, st); break;
-      case 1: e = launch_norm_grad<false, false, true>(a, groups, st); break;
-      case 2: e = launch_norm_grad<false, true, false>(a, groups, st); break;
-      case 3: e = launch_norm_grad<false, true, true>(a, groups, st); break;
-      case 4: e = launch_norm_grad<true, false, false>(a, groups, st); break;
-      case 5: e = launch_norm_grad<true, false, true>(a, groups, st); break;
-      case 6: e = launch_norm_grad<true, true, false>(a, groups, st); break;
-      default: e = launch_norm_grad<true, true, true>(a, groups, st);
+      case 0: e = launch_norm_grad<false, false, false>(a, groups, grad->groups, st); break;
+      case 1: e = launch_norm_grad<false, false, true>(a, groups, grad->groups, st); break;
+      case 2: e = launch_norm_grad<false, true, false>(a, groups, grad->groups, st); break;
+      case 3: e = launch_norm_grad<false, true, true>(a, groups, grad->groups, st); break;
+      case 4: e = launch_norm_grad<true, false, false>(a, groups, grad->groups, st); break;
+      case 5: e = launch_norm_grad<true, false, true>(a, groups, grad->groups, st); break;
+      case 6: e = launch_norm_grad<true, true, false>(a, groups, grad->groups, st); break;
+      default: e = launch_norm_grad<true, true, true>(a, groups, grad->groups, st);
     }
   }
   if (e == hipSuccess && columns) {  // (of no rows: zeros)
