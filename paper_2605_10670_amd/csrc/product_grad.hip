@@ -136,13 +136,16 @@ __device__ __forceinline__ void load_to_lds(const uint8_t* base, uint32_t offset
 }
 #pragma clang diagnostic pop
 
-// 16 bytes a lane to `offset` behind base: one store, whatever the compiler makes of what is around it.  (The distances are those
-// to the scalar registers before it and from its data, as rows.hpp has them.)
-__device__ __forceinline__ void store_counted(uint8_t* base, uint32_t offset, u32x4 v) {
+// 16 bytes a lane to `offset` behind base: one store, whatever the compiler makes of what is around it.  past: the caches, non-temporal,
+// for lines that are written whole.  (The distances are those to the scalar registers before it and from its data, as rows.hpp has them.)
+__device__ __forceinline__ void store_counted(uint8_t* base, uint32_t offset, u32x4 v, bool past) {
   const uint32_t low = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)base);
   const uint32_t high = __builtin_amdgcn_readfirstlane((uint32_t)((uintptr_t)base >> 32));
   const uint64_t to = (uint64_t)high << 32 | low;
-  asm volatile("s_nop 4\n\tglobal_store_dwordx4 %0, %1, %2 nt\n\ts_nop 1" ::"v"(offset), "v"(v), "s"(to) : "memory");
+  if (past)
+    asm volatile("s_nop 4\n\tglobal_store_dwordx4 %0, %1, %2 nt\n\ts_nop 1" ::"v"(offset), "v"(v), "s"(to) : "memory");
+  else
+    asm volatile("s_nop 4\n\tglobal_store_dwordx4 %0, %1, %2\n\ts_nop 1" ::"v"(offset), "v"(v), "s"(to) : "memory");
 }
 
 // 64 bytes each of 16 rows in p, lane l a piece of row l % 16, and the next 64 of them in q: afterwards p has 128 of the first
@@ -515,6 +518,7 @@ __global__ __launch_bounds__(64 * grad_waves(TT), 2) void k_grad_tiled(TileArgs 
       constexpr int kPiece = OT == EEP_F32 ? 1 : 2;  // tiles of 16 columns that make 64 bytes of a row
       uint8_t* base = out + ((int64_t)t.row0 * a.k + n0) * kOut;
       uint8_t* base8 = base + (int64_t)8 * a.k * kOut;
+      const bool past = (((uintptr_t)base | (uint32_t)a.k * kOut) & 127u) == 0;
 #pragma unroll
       for (int j = 0; j < kB; ++j) {
         const int row = (wn * kB + j) * 16 + (col & 7);
@@ -532,8 +536,8 @@ __global__ __launch_bounds__(64 * grad_waves(TT), 2) void k_grad_tiled(TileArgs 
           }
           whole_lines(p[0], p[1]);
           const bool in = kWhole || n0 + f * 16 + (int)(in_row / kOut) < a.k;
-          if (in && (kWhole || t.row0 + row < rows_end)) store_counted(base, at + f * 16 * kOut, p[0]);
-          if (in && (kWhole || t.row0 + row + 8 < rows_end)) store_counted(base8, at + f * 16 * kOut, p[1]);
+          if (in && (kWhole || t.row0 + row < rows_end)) store_counted(base, at + f * 16 * kOut, p[0], past);
+          if (in && (kWhole || t.row0 + row + 8 < rows_end)) store_counted(base8, at + f * 16 * kOut, p[1], past);
         }
       }
     };
@@ -592,15 +596,27 @@ __global__ __launch_bounds__(256) void k_grad_parts(PartArgs a) {
   }
 }
 
-// Where tiles are few, the terms of each are divided between several workgroups, whose sums are left in the workspace: into as many
-// parts as leave every CU something to do, of four steps at least.
+// What a step of a tile takes, us: of 256 rows; of 64 and 16, of which a CU has two, a step of both, or of one alone.  fp32 products take
+// the matrix cores 16 times as long as bf16 ones, on half as many terms a step.
+static float grad_step_time(int tt, bool f32, bool alone) {
+  if (f32) return tt == 4 ? 4.1f : tt == 1 ? (alone ? 1.1f : 2.1f) : (alone ? 0.4f : 0.6f);
+  return tt == 4 ? (alone ? 0.8f : 0.95f) : tt == 1 ? (alone ? 0.4f : 0.75f) : (alone ? 0.35f : 0.5f);
+}
+
+// Where tiles are few, the terms of each are divided between several workgroups, whose sums are left in the workspace and added up by a
+// launch more: into as many parts as there are CUs for, of four steps at least, unless writing and reading that many sums takes
+// longer than the steps that it saves.  (664 rows 1720 x 1368: the weights' gradient in 5 parts 36 us, undivided 27; 14373 rows 392 x 696
+// in 42 parts 43, in 22)
 constexpr int64_t kPartialBytes = 64 << 20;  // (256 CUs' tiles of 256 by 256)
-static int grad_parts(int64_t work, int64_t most, int64_t steps, int64_t values) {
-  if (work <= 0 || 2 * work > most) return 1;
-  int64_t parts = most / work;
-  if (parts > steps / 4) parts = steps / 4;
-  if (parts > kPartialBytes / (values * (int64_t)sizeof(float))) parts = kPartialBytes / (values * (int64_t)sizeof(float));
-  return parts < 2 ? 1 : (int)parts;
+static float grad_parts_time(int64_t parts, int64_t values) { return parts == 1 ? 0.0f : 6.0f + parts * values * 8 / 4.5e6f; }
+static int grad_parts(int64_t work, int64_t most, int64_t steps, int64_t values, float step) {
+  int64_t limit = work > 0 ? most / work : 1;
+  if (limit > steps / 4) limit = steps / 4;
+  if (limit > kPartialBytes / (values * (int64_t)sizeof(float))) limit = kPartialBytes / (values * (int64_t)sizeof(float));
+  if (limit < 2) return 1;
+  const float best = sqrtf(step * steps / (values * 8 / 4.5e6f));
+  const int64_t parts = best < limit ? (int64_t)best : limit;
+  return parts >= 2 && step * steps / parts + grad_parts_time(parts, values) < step * steps ? (int)parts : 1;
 }
 
 // values, width: of the result, of one of its rows; terms: of a sum, about.
@@ -610,7 +626,7 @@ static hipError_t launch_grad_tiled(const TileArgs& a, const eep_product_grad& g
   constexpr int kDepth = kGradStep / (DT == EEP_BF16 ? 2 : 4);
   const int64_t most = (int64_t)g.cus * grad_per_cu(TT);
   const unsigned grid = (unsigned)(work < most ? work : most);
-  const int parts = grad_parts(work, most, (terms + kDepth - 1) / kDepth, values);
+  const int parts = grad_parts(work, most, (terms + kDepth - 1) / kDepth, values, grad_step_time(TT, DT == EEP_F32, true));
   if (parts == 1) {
     hipLaunchKernelGGL((k_grad_tiled<DT, OT, OF_W, TT>), dim3(grid), dim3(64 * grad_waves(TT)), grad_lds_bytes(TT), st, a);
     return hipGetLastError();
@@ -631,9 +647,8 @@ static hipError_t launch_grad_tiled(const TileArgs& a, const eep_product_grad& g
   return hipGetLastError();
 }
 
-// What the tiles of 256, 64 or 16 tokens cost, us: what a step of one takes, as often as a CU has one, and the sum of parts.  A slot's
-// last tile is half empty on average.  Where there are two workgroups to a CU, a step of both, or of one alone.  fp32 products take the
-// matrix cores 16 times as long as bf16 ones, on half as many terms a step.  Measured, 16 / 64 / 256 tokens a tile, us, bf16: 144 slots
+// What the tiles of 256, 64 or 16 tokens cost, us: their steps, as often as a CU has one, and the sum of parts.  A slot's last tile is half
+// empty on average.  Measured, 16 / 64 / 256 tokens a tile, us, bf16: 144 slots
 // 1024 -> 4096, 64 tokens by top-8 217 / 226 / 247, 300 242 / 240 / 262, 1200 406 / 271 / 272, 2400 708 / 342 / 339; 120 slots 2880 -> 2816,
 // top-6, 400 tokens 408 / 357 / 379, 1600 814 / 480 / 456, 5976 - / 973 / 800; one matrix 2048 -> 7168, 64 rows 19 / 26 / 24, 256 35 / 29 / 41,
 // 2048 211 / 90 / 83, 8192 785 / 282 / 224.  (Tiles of 128 were between the two, and best nowhere.)
@@ -643,13 +658,9 @@ static float grad_x_cost(int tt, bool f32, const TileArgs& a, int64_t steps, int
   if (touched == 1) tiles = (float)((a.rows + rows - 1) / rows);
   const float work = (tiles < 1.0f ? 1.0f : tiles) * touched * a.feature_tiles;
   const int64_t values = (int64_t)a.rows * a.k;
-  const int parts = grad_parts((int64_t)work, most, steps, values);
-  const float rounds = work * parts / most;
-  const bool alone = grad_per_cu(tt) == 2 && rounds <= 0.5f;
-  float step = tt == 4 ? 0.95f : tt == 1 ? (alone ? 0.4f : 0.75f) : (alone ? 0.35f : 0.5f);
-  if (f32) step = tt == 4 ? 4.1f : tt == 1 ? (alone ? 1.1f : 2.1f) : (alone ? 0.4f : 0.6f);
-  const float time = step * steps / parts * (rounds < 4.0f ? ceilf(rounds) : rounds);
-  return parts == 1 ? time : time + 4.0f + parts * values * 8 / 5e6f;
+  const int parts = grad_parts((int64_t)work, most, steps, values, grad_step_time(tt, f32, true));
+  const float rounds = work * parts / most, step = grad_step_time(tt, f32, rounds <= 0.5f);
+  return step * steps / parts * (rounds < 4.0f ? ceilf(rounds) : rounds) + grad_parts_time(parts, values);
 }
 
 template <int DT>
