@@ -404,7 +404,7 @@ __global__ __launch_bounds__(64 * grad_waves(TT), 2) void k_grad_tiled(TileArgs 
   };
 
   // the first tile that has terms at all
-#pragma unroll
+#pragma nounroll  // (its code comes three times as it is)
   for (int s = 0; s < kStages; ++s) fetch();
   const uint8_t* stage = lds;
   // What a step begins with: all of g's operands, the first ones of the other.
