@@ -306,8 +306,13 @@ __global__ __launch_bounds__(64 * grad_waves(TT), 2) void k_grad_tiled(TileArgs 
   };
 
   const int64_t k_bytes = (int64_t)a.k * kSize, n_bytes = (int64_t)a.n * kSize;
-  // what the lane loads of g where its rows lie along the sum: 16 bytes of row `lane / 4` of 16
-  const int load_row = lane >> 2, load_chunk = (lane & 3) ^ ((load_row >> 2) & 3);
+  // What the lane loads of g where its rows lie along the sum: 16 bytes of row `lane / 4` of 16.  A row's four chunks change places there so
+  // that reads of 16 bytes meet in no bank: lanes 0 to 3, 12 to 15 and 20 to 27 take theirs at a time, 4 to 11, 16 to 19 and 28 to 31.
+  const auto places = [](int row) {
+    const int four = (row >> 2) & 3;
+    return ((four & 1) << 1) ^ (four >> 1) ^ (four & 2);
+  };
+  const int load_row = lane >> 2, load_chunk = (lane & 3) ^ places(load_row);
 
   // The stream of steps: the tile that is fetched, its terms left, where its operands are and the lane's places there.
   Walk ahead = {-1, 0, 0};
@@ -394,7 +399,7 @@ __global__ __launch_bounds__(64 * grad_waves(TT), 2) void k_grad_tiled(TileArgs 
       }
     }
   };
-  const int read_at = col * kGradStep + ((part ^ ((col >> 2) & 3)) << 4);
+  const int read_at = col * kGradStep + ((part ^ places(col)) << 4);
   const auto read_other = [&](const uint8_t* stage, int f) { return Other::read(stage, lane, wm * kA + f); };
   const auto read_grads = [&](const uint8_t* stage, int j) {
     if constexpr (OF_W)
