@@ -609,14 +609,15 @@ static float grad_step_time(int tt, bool f32, bool alone) {
 }
 
 // Where tiles are few, the terms of each are divided between several workgroups, whose sums are left in the workspace and added up by a
-// launch more: into as many parts as there are CUs for, of four steps at least, unless writing and reading that many sums takes
+// launch more: into as many parts as there are CUs for, of four steps at least (one, where it takes so long), unless writing and reading that many sums takes
 // longer than the steps that it saves.  (664 rows 1720 x 1368: the weights' gradient in 5 parts 36 us, undivided 27; 14373 rows 392 x 696
 // in 42 parts 43, in 22)
 constexpr int64_t kPartialBytes = 64 << 20;  // (256 CUs' tiles of 256 by 256)
 static float grad_parts_time(int64_t parts, int64_t values) { return parts == 1 ? 0.0f : 6.0f + parts * values * 8 / 4.5e6f; }
 static int grad_parts(int64_t work, int64_t most, int64_t steps, int64_t values, float step) {
   int64_t limit = work > 0 ? most / work : 1;
-  if (limit > steps / 4) limit = steps / 4;
+  const int64_t shortest = step > 1.0f ? 1 : 4;
+  if (limit > steps / shortest) limit = steps / shortest;
   if (limit > kPartialBytes / (values * (int64_t)sizeof(float))) limit = kPartialBytes / (values * (int64_t)sizeof(float));
   if (limit < 2) return 1;
   const float best = sqrtf(step * steps / (values * 8 / 4.5e6f));
