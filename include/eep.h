@@ -740,7 +740,8 @@ int eep_route_grad(const eep_router_shape* shape, const void* logits, const int3
  *            (grad_sums may be sums itself)
  *   x        device [rows, in_features], needed for grad_w;  w  as eep_expert_product's, needed for grad_x
  *   grad_x   device [rows, in_features] or NULL;  grad_w  device, slot p's begins p * grad_stride bytes in, or NULL.  Results may not
- *            overlap an operand; with a gate both may be NULL.
+ *            overlap an operand or each other (slots' arrays: from the first slot's first byte to the last one's last); with a gate both
+ *            may be NULL.
  * Row sizes, strides, limits and offsets are treated as eep_product_create and eep_expert_product treat them; rows 0 with grad_w
  * writes its zeros.  The handle owns a workspace (64 MiB) for sums that are made in parts: calls with it share that, and may not
  * overlap (one stream, or events between).  eep_product_grad_destroy waits for the device. */

@@ -58,6 +58,16 @@ __device__ __forceinline__ float without(float mean_square, float mean) {
   return mean_square < INFINITY ? fmaxf(fmaf(-mean, mean, mean_square), 0.0f) : mean_square;
 }
 
+// What is still to be taken out of every value of a centred row: its mean, as roundings left it, where that outweighs what lies around it
+// (a row of equal values, mostly, whose mean square would else be a difference of roundings), and wherever the row is scaled.
+__device__ __forceinline__ float stray(float left, float mean_square, float epsilon, float by, float more) {
+  const bool out = more != 1.0f || left * left > mean_square + epsilon * by * by;
+  return out && fabsf(left) < INFINITY ? left : 0.0f;
+}
+// Times that a row is scaled or centred again: equal values near the largest number take seven, each of which leaves 2^-22 of their
+// mean; without that they would go back and forth between two scales, at one of which their squares leave fp32.
+constexpr int kRefits = 12;
+
 // ---------------------------------------------------------------------------
 // layer norm: h = x + r;  d = h - mean(h);  y = d / sqrt(mean(d^2) + eps) * g + b.
 //
@@ -147,12 +157,16 @@ __global__ __launch_bounds__(1024) void k_layer_norm(LayerNormArgs a, int64_t fi
     mean = without(sum[1] / (float)a.H, left);
   };
   mean_square();
-  for (float more; (more = fitting(mean, a.epsilon, by)) != 1.0f;) {
+  for (int fit = 0; fit < kRefits; ++fit) {
+    const float more = fitting(mean, a.epsilon, by), off = stray(left, mean, a.epsilon, by, more);
+    if (more == 1.0f && off == 0.0f) break;
     by *= more;
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
+    for (int j = 0; j < NV; ++j) {
+      if (j * threads + tid >= vecs) continue;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) h[j][i] *= more;
+      for (int i = 0; i < 8; ++i) h[j][i] = (h[j][i] - off) * more;
+    }
     mean_square();
   }
   const float inv = 1.0f / sqrtf(mean + a.epsilon * by * by);
@@ -329,12 +343,16 @@ __global__ __launch_bounds__(norm_grad_threads(NV), norm_grad_waves(IN_BF16, NV)
       }
     };
     sums();
-    for (float more; (more = fitting(mean_square(), a.epsilon, by)) != 1.0f;) {
+    for (int fit = 0; fit < kRefits; ++fit) {
+      const float more = fitting(mean_square(), a.epsilon, by);
+      float off = 0.0f;
+      if constexpr (CENTRED) off = stray(sum[2] / count, mean_square(), a.epsilon, by, more);
+      if (more == 1.0f && off == 0.0f) break;
       by *= more;
 #pragma unroll
       for (int j = 0; j < NV; ++j)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) d[j][i] *= more;
+        for (int i = 0; i < 8; ++i) d[j][i] = (d[j][i] - off) * more;  // (what lies past the row is used nowhere)
       sums();
     }
     const float inv = 1.0f / sqrtf(mean_square() + a.epsilon * by * by);

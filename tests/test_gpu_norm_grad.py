@@ -166,6 +166,53 @@ def test_rows_of_one_value(value):
     gr.check("grad_h", out, *want)
 
 
+@pytest.mark.parametrize("H", [2880, 7168, 8, 24])
+@pytest.mark.parametrize("value", [1e6 + 0.1, 1.1e20, 1.1 * 2.0 ** 90, 1.1 * 2.0 ** 100, 1.3 * 2.0 ** 110, 1.7 * 2.0 ** 126])
+def test_large_rows_of_one_value_whose_mean_is_rounded(value, H):
+    """What roundings leave of the mean is taken out too, however large its squares are.  (What is left of it then is at most 2^-19 of the root:
+    the sums of equal values are off by up to 24 roundings, and by no more than sqrt(mean square + epsilon) before the last of them.)"""
+    T = 3
+    h = torch.full((T, H), value)
+    h[1] = -h[1]
+    g = lu.gen(H)
+    gain, bias, gy = 1 + 0.2 * lu.randn(g, H), lu.randn(g, H), lu.randn(g, T, H)
+    y, out = torch.empty((T, H), device="cuda"), torch.empty((T, H), device="cuda")
+    gg = torch.empty(H, device="cuda")
+    layer.LayerNorm(hidden=H, in_dtype="f32", gain_dtype="f32", out_dtype="f32").run(h.cuda(), gain.cuda(), T, bias=bias.cuda(), y=y)
+    u = 2.0 ** -19
+    assert ((y.cpu().double() - bias.double()).abs() <= u * gain.abs() + 2.0 ** -24 * bias.abs()).all()
+    grad = layer.NormGrad(hidden=H, in_dtype="f32", gain_dtype="f32", out_dtype="f32", centred=True)
+    grad.run(h.cuda(), gain.cuda(), gy.cuda(), T, grad_h=out, grad_gain=gg)
+    v = gy.double() * gain.double()
+    root = 1e-5 ** 0.5
+    # u times mean(v * u) on top of that, the mean's own 24 roundings and the root's, half of u's
+    err = (v.abs() + 2 * v.abs().mean(dim=1, keepdim=True)) * u / root
+    assert ((out.cpu().double() - (v - v.mean(dim=1, keepdim=True)) / root).abs() <= err).all()
+    assert (gg.cpu().double().abs() <= u * gy.double().abs().sum(dim=0)).all()
+
+
+@pytest.mark.parametrize("value", [1e8, 1.1 * 2.0 ** 90, 1.7 * 2.0 ** 126])
+def test_rows_that_differ_in_their_last_bit(value):
+    """Every third value is the next one: the layer norm of 0, 0, 1 (times their distance, beside which epsilon is nothing)."""
+    T, H = 2, 2880
+    h = torch.full((T, H), value)
+    h[:, ::3] = torch.nextafter(h[:, ::3], torch.tensor(float("inf")))
+    ones, y, out = torch.ones(H), torch.empty((T, H), device="cuda"), torch.empty((T, H), device="cuda")
+    layer.LayerNorm(hidden=H, in_dtype="f32", gain_dtype="f32", out_dtype="f32").run(h.cuda(), ones.cuda(), T, y=y)
+    step = h[0, 0].double() - h[0, 1].double()
+    small = (torch.arange(H) % 3 == 0).double().expand(T, H) * step
+    d = small - small.mean(dim=1, keepdim=True)
+    root = ((d * d).mean(dim=1, keepdim=True) + 1e-5).sqrt()
+    # d and the mean square are of whole steps, but for the mean that is left: 24 roundings each
+    assert ((y.cpu().double() - d / root).abs() <= 2.0 ** -19 * 1.5).all()
+    gy = lu.randn(lu.gen(4), T, H)
+    layer.NormGrad(hidden=H, in_dtype="f32", gain_dtype="f32", out_dtype="f32", centred=True).run(h.cuda(), ones.cuda(), gy.cuda(), T, grad_h=out)
+    v, u = gy.double(), d / root
+    want = (v - u * (v * u).mean(dim=1, keepdim=True) - v.mean(dim=1, keepdim=True)) / root
+    err = 2.0 ** -19 * 8 * (v.abs() + v.abs().mean(dim=1, keepdim=True)) / root + 2.0 ** -149
+    assert ((out.cpu().double() - want).abs() <= err).all()
+
+
 def test_against_differences():
     """The gradient of a weighted sum of the layer norm's outputs, by central differences of the kernel itself in fp32."""
     T, H = 2, 64
