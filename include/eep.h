@@ -721,7 +721,7 @@ int eep_norm_grad_run(eep_norm_grad* grad, const void* h, const void* gain, cons
  *   over_all == 0: grad_logits[topk_idx[j]] = topk_w[j] * (grad_w[j] - inner), the others 0
  *   over_all != 0: grad_logits[e] = -p[e] * inner, and topk_w[j] * grad_w[j] more where e is chosen; p: the softmax over all logits
  * Logits of -infinity and NaN get 0.  logits: as eep_route's, only for over_all (else NULL); grad_w: device float [T, topk];
- * grad_logits: device [T, num_logical] in_dtype, all of it written. */
+ * grad_logits: device [T, num_logical] in_dtype, all of it written; it may be logits itself. */
 int eep_route_grad(const eep_router_shape* shape, const void* logits, const int32_t* topk_idx, const float* topk_w,
                    const float* grad_w, void* grad_logits, int32_t T, void* stream);
 

@@ -295,14 +295,14 @@ hipError_t launch_route(const eep_router_shape& s, const void* logits, int32_t* 
 // others nothing; over all logits every one gets -p * inner, p its share, and a chosen one w_j * grad_w_j more.
 //
 // A group of LANES lanes has a token, four neighbouring logits a lane at a time, to which the lane adds those of the k choices that are
-// among them.  Bound by memory at many tokens, by one trip at few.
+// among them; it reads them itself before it writes there, so that the gradient may take the logits' place.  Bound by memory at many tokens, by one trip at few.
 // ---------------------------------------------------------------------------
 constexpr int kRouteGradMany = 4096;  // tokens from which 16 lanes have one
 
 template <bool BF16, int LANES, bool FOURS>
-__global__ __launch_bounds__(256) void k_route_grad(const void* __restrict__ logits, const int32_t* __restrict__ topk_idx,
+__global__ __launch_bounds__(256) void k_route_grad(const void* logits, const int32_t* __restrict__ topk_idx,
                                                     const float* __restrict__ topk_w, const float* __restrict__ grad_w,
-                                                    void* __restrict__ grad_logits, int E, int k, int over_all, int64_t first,
+                                                    void* grad_logits, int E, int k, int over_all, int64_t first,
                                                     int64_t end) {
   constexpr int kTokens = 256 / LANES;
   const int lane = threadIdx.x & (LANES - 1);
@@ -405,9 +405,9 @@ __global__ __launch_bounds__(256) void k_route_grad(const void* __restrict__ log
 // Measured, 256 bf16 logits, top-8, over all of them, 16 lanes / a wavefront a token, us: 1024 tokens 5.3 / 4.7, 4096 5.6 / 5.7, 16384
 // 7.1 / 13.8; with every lane comparing its logits with every choice 9.4.
 template <bool BF16, int FOURS>
-__global__ __launch_bounds__(256) void k_route_grad_many(const void* __restrict__ logits, const int32_t* __restrict__ topk_idx,
+__global__ __launch_bounds__(256) void k_route_grad_many(const void* logits, const int32_t* __restrict__ topk_idx,
                                                          const float* __restrict__ topk_w, const float* __restrict__ grad_w,
-                                                         void* __restrict__ grad_logits, int E, int k, int over_all,
+                                                         void* grad_logits, int E, int k, int over_all,
                                                          int64_t first, int64_t end) {
   const int lane = threadIdx.x & 15;
   const int64_t t = first + (int64_t)blockIdx.x * 16 + threadIdx.x / 16;

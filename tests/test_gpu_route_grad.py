@@ -32,6 +32,9 @@ def test_route_grad(T, E, k, x, over_all):
     router.grad(idx, w, gw.cuda(), out, T, logits=logits if over_all else None)
     want, err = gr.route_grad(idx.cpu(), w.cpu(), gw, E, logits.cpu() if over_all else None)
     gr.check("grad_logits", out, want, err)
+    if over_all:
+        router.grad(idx, w, gw.cuda(), logits, T, logits=logits)   # in their place
+        assert torch.equal(logits, out)
 
 
 def test_rows_with_nothing_to_choose_and_odd_addresses():
