@@ -259,14 +259,16 @@ __global__ __launch_bounds__(64 * grad_waves(TT), 2) void k_grad_tiled(TileArgs 
     items = (int64_t)map.total * a.feature_tiles;
   }
   // The items go to the XCDs in turn, as many neighbouring ones at a time as one has workgroups, which share rows of the
-  // operands in its L2; what is left over for a last turn is divided between them.
+  // operands in its L2; what is left over for a last turn is divided between them.  Seats move on by one every turn: tiles of few rows
+  // take less time, and come at even distances (120 slots 2880 -> 2816 of 300 tokens 1078 us with seats that stay, now 894; of 256 642 both).
   const int xcds = gridDim.x % 8 == 0 ? 8 : 1;
   const int xcd = blockIdx.x % xcds, seat = blockIdx.x / xcds, seats = gridDim.x / xcds;
   const int64_t whole_turns = items / gridDim.x, over = items - whole_turns * gridDim.x;
   const int over_from = (int)(over * xcd / xcds), over_to = (int)(over * (xcd + 1) / xcds);
   const int64_t turns = whole_turns + (seat < over_to - over_from ? 1 : 0);
   const auto item_of = [&](int64_t turn) {
-    return turn * gridDim.x + (turn < whole_turns ? xcd * seats : over_from) + seat;
+    if (turn >= whole_turns) return turn * gridDim.x + over_from + seat;
+    return turn * gridDim.x + xcd * seats + (int)(((unsigned)seat + (unsigned)turn) % (unsigned)seats);
   };
   // Where a walk over the items is: OF_W, the slot and the place among its tiles (without a division, which 64 bits make long).
   struct Walk {
