@@ -136,28 +136,42 @@ __device__ __forceinline__ void load_to_lds(const uint8_t* base, uint32_t offset
 }
 #pragma clang diagnostic pop
 
-// 16 bytes a lane to `offset` behind base: one store, whatever the compiler makes of what is around it.  past: the caches, non-temporal,
-// for lines that are written whole.  (The distances are those to the scalar registers before it and from its data, as rows.hpp has them.)
-__device__ __forceinline__ void store_counted(uint8_t* base, uint32_t offset, u32x4 v, bool past) {
-  const uint32_t low = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)base);
-  const uint32_t high = __builtin_amdgcn_readfirstlane((uint32_t)((uintptr_t)base >> 32));
-  const uint64_t to = (uint64_t)high << 32 | low;
-  if (past)
-    asm volatile("s_nop 4\n\tglobal_store_dwordx4 %0, %1, %2 nt\n\ts_nop 1" ::"v"(offset), "v"(v), "s"(to) : "memory");
-  else
-    asm volatile("s_nop 4\n\tglobal_store_dwordx4 %0, %1, %2\n\ts_nop 1" ::"v"(offset), "v"(v), "s"(to) : "memory");
+// 16 or 8 bytes a lane: one store, whatever the compiler makes of what is around it.  past: the caches, non-temporal, for lines that are
+// written whole.  (Data of 16 bytes has to stay for a while.)
+template <class V>
+__device__ __forceinline__ void store_counted(uint8_t* to, V v, bool past) {
+  if constexpr (sizeof(V) == 16) {
+    if (past)
+      asm volatile("global_store_dwordx4 %0, %1, off nt\n\ts_nop 1" ::"v"(to), "v"(v) : "memory");
+    else
+      asm volatile("global_store_dwordx4 %0, %1, off\n\ts_nop 1" ::"v"(to), "v"(v) : "memory");
+  } else {
+    if (past)
+      asm volatile("global_store_dwordx2 %0, %1, off nt" ::"v"(to), "v"(v) : "memory");
+    else
+      asm volatile("global_store_dwordx2 %0, %1, off" ::"v"(to), "v"(v) : "memory");
+  }
 }
 
-// 64 bytes each of 16 rows in p, lane l a piece of row l % 16, and the next 64 of them in q: afterwards p has 128 of the first
-// eight rows and q of the last.  (With stores of 64 bytes of a row, and these not non-temporal: 144 slots of 1024 x 4096 bf16
-// of 512 rows 243 us, now 202.)
-__device__ __forceinline__ void whole_lines(u32x4& p, u32x4& q) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t a = p[i], b = q[i];  // lanes 8 away change places, in the upper half of a row of lanes, then in the lower
-    p[i] = __builtin_amdgcn_update_dpp(a, b, 0x128, 0xf, 0xc, false);
-    q[i] = __builtin_amdgcn_update_dpp(b, a, 0x128, 0xf, 0x3, false);
-  }
+// Lane p of every four has a, b, c, d; afterwards it has those of them that lanes 0 to 3 have at place p.  Every lane of the wavefront is there.
+// (Each of the eight instructions takes a lane's own value or another's; what another lane wrote is read two instructions later at the soonest.)
+__device__ __forceinline__ u32x4 turn_quads(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  uint32_t v, w, x, y, t, u;
+#define EEP_OTHERS(to, other, own, lanes) "v_cndmask_b32_dpp " to ", " other ", " own ", vcc quad_perm:" lanes " row_mask:0xf bank_mask:0xf\n\t"
+  asm volatile("s_nop 1\n\ts_mov_b64 vcc, %10\n\t"  // even lanes
+               EEP_OTHERS("%4", "%7", "%6", "[1,0,3,2]") EEP_OTHERS("%2", "%9", "%8", "[1,0,3,2]")
+               "s_mov_b64 vcc, %11\n\t"  // odd ones
+               EEP_OTHERS("%5", "%6", "%7", "[1,0,3,2]") EEP_OTHERS("%3", "%8", "%9", "[1,0,3,2]")
+               "s_mov_b64 vcc, %12\n\t"  // the lower two of four
+               EEP_OTHERS("%0", "%2", "%4", "[2,3,0,1]") EEP_OTHERS("%1", "%3", "%5", "[2,3,0,1]")
+               "s_mov_b64 vcc, %13\n\t"  // the upper two
+               EEP_OTHERS("%2", "%4", "%2", "[2,3,0,1]") EEP_OTHERS("%3", "%5", "%3", "[2,3,0,1]")
+               : "=&v"(v), "=&v"(w), "=&v"(x), "=&v"(y), "=&v"(t), "=&v"(u)
+               : "v"(a), "v"(b), "v"(c), "v"(d), "s"(0x5555555555555555ull), "s"(0xaaaaaaaaaaaaaaaaull), "s"(0x3333333333333333ull),
+                 "s"(0xccccccccccccccccull)
+               : "vcc");
+#undef EEP_OTHERS
+  return u32x4{v, w, x, y};
 }
 
 // An operand that lies across the sum: rows of COLS values, in LDS one behind the other.  Its 16-byte chunks change places within a
@@ -178,15 +192,22 @@ struct Across {
   __device__ __forceinline__ static int column(int wave, int lane, int i) {
     return ((lane % kChunks) ^ places(row(wave, lane, i))) * (16 / kSize);
   }
-  // 16 columns from `tile` * 16 on.
+  // Four neighbouring columns, counted in fours: those of lanes 4c to 4c + 3 of every 16 for the tile-th 16 columns.  spread: the columns of
+  // four tiles change places, so that the lanes' values of the four make, after turn_quads, 64 neighbouring ones.
+  template <bool SPREAD>
+  __device__ __forceinline__ static int four(int c, int tile) {
+    return SPREAD ? (tile >> 2) * 16 + c * 4 + ((tile & 3) ^ c) : tile * 4 + c;
+  }
+  // 16 columns of `tile`.
+  template <bool SPREAD>
   __device__ __forceinline__ static u32x4 read(const uint8_t* lds, int lane, int tile) {
     const int part = lane >> 4;
     u32x4 f;
     if constexpr (DT == EEP_BF16) {
       typedef int16_t i16x4 __attribute__((ext_vector_type(4)));
       typedef __attribute__((address_space(3))) i16x4 lds_quad;
-      const int row = 8 * part + ((lane >> 2) & 3);
-      const uint8_t* from = lds + row * kRowBytes + (((2 * tile + ((lane >> 1) & 1)) ^ places(row)) << 4) + (lane & 1) * 8;
+      const int row = 8 * part + ((lane >> 2) & 3), at = four<SPREAD>(lane & 3, tile);
+      const uint8_t* from = lds + row * kRowBytes + (((at >> 1) ^ places(row)) << 4) + (at & 1) * 8;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const u32x2 d =
@@ -196,7 +217,7 @@ struct Across {
       }
     } else {
       const uint8_t* from =
-          lds + 4 * part * kRowBytes + (((4 * tile + ((lane >> 2) & 3)) ^ places(4 * part)) << 4) + (lane & 3) * 4;
+          lds + 4 * part * kRowBytes + ((four<SPREAD>((lane >> 2) & 3, tile) ^ places(4 * part)) << 4) + (lane & 3) * 4;
 #pragma unroll
       for (int i = 0; i < 4; ++i) f[i] = *(const uint32_t*)(from + i * kRowBytes);
     }
@@ -402,10 +423,13 @@ __global__ __launch_bounds__(64 * grad_waves(TT), 2) void k_grad_tiled(TileArgs 
     }
   };
   const int read_at = col * kGradStep + ((part ^ places(col)) << 4);
-  const auto read_other = [&](const uint8_t* stage, int f) { return Other::read(stage, lane, wm * kA + f); };
+  // (a wavefront's four tiles at a time are 64 * kWM columns apart, which the places of chunks have no part in)
+  const auto read_other = [&](const uint8_t* stage, int f) {
+    return Other::template read<true>(stage + (f >> 2) * kWM * 64 * kSize, lane, wm * 4 + (f & 3));
+  };
   const auto read_grads = [&](const uint8_t* stage, int j) {
     if constexpr (OF_W)
-      return Grads::read(stage + kOtherStage, lane, wn * kB + j);
+      return Grads::template read<false>(stage + kOtherStage, lane, wn * kB + j);
     else
       return *(const u32x4*)(stage + kOtherStage + (wn * kB + j) * 16 * kGradStep + read_at);
   };
@@ -433,7 +457,8 @@ __global__ __launch_bounds__(64 * grad_waves(TT), 2) void k_grad_tiled(TileArgs 
     read_heads();
   }
 
-  constexpr int kStores = kA * kB / (OT == EEP_F32 ? 1 : 2);  // of a whole tile, a wavefront's
+  constexpr int kStores = kA * kB;  // of a whole tile, a wavefront's
+  static_assert(kA % 4 == 0, "four tiles change places");
   static_assert((kStages - 2) * kLoads + kStores < 64, "what the counter holds");
   int behind_stores = kStages;  // steps since a whole tile was stored
   for (Walk here = {0, 0, 0}; here.turn < turns; ++here.turn) {
@@ -472,7 +497,7 @@ __global__ __launch_bounds__(64 * grad_waves(TT), 2) void k_grad_tiled(TileArgs 
       const auto multiply = [&](int f) {
         const u32x4 now = ready(v[f]);
 #pragma unroll
-        for (int j = 0; j < kB; ++j) acc[f][j] = mma_step<DT>(now, b[j], acc[f][j]);
+        for (int j = 0; j < kB; ++j) acc[f][j] = mma_step<DT>(b[j], now, acc[f][j]);
         __builtin_amdgcn_sched_barrier(0);
       };
 #pragma unroll
@@ -494,59 +519,75 @@ __global__ __launch_bounds__(64 * grad_waves(TT), 2) void k_grad_tiled(TileArgs 
     }
 
     uint8_t* out = a.out + blockIdx.y * a.plane + (OF_W ? t.slot * a.out_stride : 0);
-    const int n0 = t.column0 + wm * (kA * 16);
     if (OF_W && a.accumulate != 0 && t.terms == 0) continue;  // (nothing to add)
-    constexpr int kOut = OT == EEP_F32 ? 4 : 2;
+    // The lane has, of rows row0 + 16 j + i, columns column + kNext * q to column + kNext * q + 3.
+    constexpr int kOut = OT == EEP_F32 ? 4 : 2, kNext = 64 * kWM;
+    const int column = t.column0 + wm * 64 + (col & 12) * 4 + (((col >> 2) ^ col) & 3) * 4;
+    const int row0 = t.row0 + wn * kB * 16 + part * 4;
+    // (the compiler, which keeps the matrix instructions' distance to what reads their results, does not look into turn_quads)
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    const auto values = [&](int j, int q, int i) {
+      return turn_quads(__float_as_uint(acc[4 * q][j][i]), __float_as_uint(acc[4 * q + 1][j][i]), __float_as_uint(acc[4 * q + 2][j][i]),
+                        __float_as_uint(acc[4 * q + 3][j][i]));
+    };
     if (OF_W && a.accumulate != 0) {
 #pragma unroll
-      for (int j = 0; j < kB; ++j) {
-        const int64_t row = (int64_t)t.row0 + (wn * kB + j) * 16 + col;
+      for (int j = 0; j < kB; ++j)
 #pragma unroll
-        for (int f = 0; f < kA; ++f) {
-          const int n = n0 + f * 16 + part * 4;
-          if (row >= rows_end || n >= a.k) continue;
-          uint8_t* to = out + (row * a.k + n) * kOut;
-          if constexpr (OT == EEP_F32) {
-            *(f32x4*)to = acc[f][j] + *(const f32x4*)to;
-          } else {
-            const u32x2 d = *(const u32x2*)to;
-            *(u32x2*)to = u32x2{pack_bf16x2(acc[f][j][0] + bf16_lo(d[0]), acc[f][j][1] + bf16_hi(d[0])),
-                                pack_bf16x2(acc[f][j][2] + bf16_lo(d[1]), acc[f][j][3] + bf16_hi(d[1]))};
+        for (int q = 0; q < kA / 4; ++q) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const f32x4 v = __builtin_bit_cast(f32x4, values(j, q, i));
+            const int row = row0 + j * 16 + i, n = column + q * kNext;
+            if (row >= rows_end || n >= a.k) continue;
+            uint8_t* to = out + ((int64_t)row * a.k + n) * kOut;
+            if constexpr (OT == EEP_F32) {
+              *(f32x4*)to = v + *(const f32x4*)to;
+            } else {
+              const u32x2 d = *(const u32x2*)to;
+              *(u32x2*)to = u32x2{pack_bf16x2(v[0] + bf16_lo(d[0]), v[1] + bf16_hi(d[0])),
+                                  pack_bf16x2(v[2] + bf16_lo(d[1]), v[3] + bf16_hi(d[1]))};
+            }
           }
+          __builtin_amdgcn_sched_barrier(0);
         }
-        __builtin_amdgcn_sched_barrier(0);
-      }
       behind_stores = kStages;
       continue;
     }
     // A whole tile is stored by a number of stores that the steps behind them count on.
     const auto store = [&](auto is_whole) {
       constexpr bool kWhole = decltype(is_whole)::value;
-      constexpr int kPiece = OT == EEP_F32 ? 1 : 2;  // tiles of 16 columns that make 64 bytes of a row
-      uint8_t* base = out + ((int64_t)t.row0 * a.k + n0) * kOut;
-      uint8_t* base8 = base + (int64_t)8 * a.k * kOut;
-      const bool past = (((uintptr_t)base | (uint32_t)a.k * kOut) & 127u) == 0;
+      int64_t pitch = (int64_t)a.k * kOut;
+      asm volatile("" : "+s"(pitch));  // (else all rows' distances are kept from tile to tile, in registers that are not there)
+      uint8_t* to = out + row0 * pitch + (int64_t)column * kOut;
+      const bool past = (((uintptr_t)out | (uint64_t)pitch) & 127u) == 0;
 #pragma unroll
-      for (int j = 0; j < kB; ++j) {
-        const int row = (wn * kB + j) * 16 + (col & 7);
-        const uint32_t in_row = (col >> 3) * 64 + (OT == EEP_F32 ? part * 16 : (part & 1) * 32 + (part >> 1) * 16);
-        const uint32_t at = (uint32_t)row * (uint32_t)a.k * kOut + in_row;
+      for (int j = 0; j < kB; ++j)
 #pragma unroll
-        for (int f = 0; f < kA; f += 2 * kPiece) {
-          u32x4 p[2];
+        for (int q = 0; q < kA / 4; ++q) {
+          const auto put = [&](int i, auto v) {
+            if (kWhole || (row0 + j * 16 + i < rows_end && column + q * kNext < a.k))
+              store_counted(to + ((j * 16 + i) * pitch + q * kNext * kOut), v, past);
+          };
+          if constexpr (OT == EEP_F32) {
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            if constexpr (OT == EEP_F32)
-              p[h] = __builtin_bit_cast(u32x4, acc[f + h][j]);
-            else
-              p[h] = side_by_side(acc[f + 2 * h][j], acc[f + 2 * h + 1][j]);
+            for (int i = 0; i < 4; ++i) put(i, values(j, q, i));
+          } else {
+            // (two rows' values are turned together)
+#pragma unroll
+            for (int i = 0; i < 4; i += 2) {
+              uint32_t p[4];
+#pragma unroll
+              for (int f = 0; f < 4; ++f) p[f] = pack_bf16x2(acc[4 * q + f][j][i], acc[4 * q + f][j][i + 1]);
+              const u32x4 v = turn_quads(p[0], p[1], p[2], p[3]);
+              put(i, u32x2{__builtin_amdgcn_perm(v[1], v[0], 0x05040100), __builtin_amdgcn_perm(v[3], v[2], 0x05040100)});
+              put(i + 1, u32x2{__builtin_amdgcn_perm(v[1], v[0], 0x07060302), __builtin_amdgcn_perm(v[3], v[2], 0x07060302)});
+            }
           }
-          whole_lines(p[0], p[1]);
-          const bool in = kWhole || n0 + f * 16 + (int)(in_row / kOut) < a.k;
-          if (in && (kWhole || t.row0 + row < rows_end)) store_counted(base, at + f * 16 * kOut, p[0], past);
-          if (in && (kWhole || t.row0 + row + 8 < rows_end)) store_counted(base8, at + f * 16 * kOut, p[1], past);
+          __builtin_amdgcn_sched_barrier(0);
         }
-      }
     };
     if (t.row0 + kRows <= rows_end && t.column0 + kGradCols <= a.k) {
       store(std::true_type());
