@@ -26,7 +26,7 @@ namespace eep {
 // ---------------------------------------------------------------------------
 // the gate's gradient: with e = exp(-|a|), s = 1 / (1 + exp(-a)),
 //   of a: grad_y * b * s * (1 + a * (1 - s)),  of b: grad_y * a * s.
-// A thread has eight (fp32: four) neighbouring features of a row.  Bound by memory.
+// A thread has eight (fp32: four) neighbouring features of a row.  Bound by memory: 131072 rows of 2 x 2048 bf16 429 us (6.3 TB/s).
 // ---------------------------------------------------------------------------
 struct GateGradArgs {
   const void *grad_y, *sums;
@@ -81,9 +81,16 @@ __global__ __launch_bounds__(256) void k_gate_grad(GateGradArgs a, int64_t first
 // tiles: 256 in_features by 64 * TT rows (TT 0: 16) of the result, which are tokens (OF_W false: the rows' gradient, summed over the
 // weights' rows) or weight rows (OF_W: the weights' gradient, summed over a slot's tokens).
 //
-// As in product.hip the in_features are the matrix cores' rows, so that a lane has four neighbouring ones of one row of the
-// result.  Eight wavefronts; the steps of all tiles are one stream, of which some are under way to LDS while one is
+// The in_features are the matrix cores' columns: a lane has one of them in four rows of the result, and they are dealt out to the lanes so
+// that after an exchange among every four lanes it has four neighbouring ones of a row, and the 16 lanes beside one another 64 of them.
+// (A CU stores 64 bytes at a time of what four neighbouring lanes have: where these are on different rows, a tile of 256 KB takes 8.0 us, now 2.0.)
+// Eight wavefronts; the steps of all tiles are one stream, of which some are under way to LDS while one is
 // multiplied, and the operands that a step begins with are read while the one before ends.
+// A step is 64 bytes deep, half of what is common, since the next tile's first steps are to be under way beside the stores of the last one: four
+// stages instead of two (with stores that the waits count, 64 tokens 522 -> 490 us); five, which just fit, change nothing.  A step of 256 x 256 takes 0.76 us on few CUs,
+// 0.87 to 1.05 on all, where the card's power bounds it (1.06 PFLOP/s on normal random numbers; torch's product of 8192 x 8192 1.13);
+// where stores are as many as products, one waits for the other: 120 slots 2880 -> 2816 of 304 tokens, fp32 gradients, 16 us a tile, of which
+// the stores alone are 12.
 // ---------------------------------------------------------------------------
 struct TileArgs {
   const uint8_t *g, *other;  // g: of the sums; other: the weights, or the rows x
@@ -653,8 +660,8 @@ static float grad_step_time(int tt, bool f32, bool alone) {
 
 // Where tiles are few, the terms of each are divided between several workgroups, whose sums are left in the workspace and added up by a
 // launch more: into as many parts as there are CUs for, of four steps at least (one, where it takes so long), unless writing and reading that many sums takes
-// longer than the steps that it saves.  (664 rows 1720 x 1368: the weights' gradient in 5 parts 36 us, undivided 27; 14373 rows 392 x 696
-// in 42 parts 43, in 22)
+// longer than the steps that it saves.  (664 rows 1720 x 1368: the weights' gradient in 5 parts 36 us, undivided 27; 249 rows 256 -> 1264 in
+// fp32, both gradients, 47 us with four steps at least, 41 with one.)
 constexpr int64_t kPartialBytes = 64 << 20;  // (256 CUs' tiles of 256 by 256)
 static float grad_parts_time(int64_t parts, int64_t values) { return parts == 1 ? 0.0f : 6.0f + parts * values * 8 / 4.5e6f; }
 static int grad_parts(int64_t work, int64_t most, int64_t steps, int64_t values, float step) {
