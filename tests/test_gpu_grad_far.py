@@ -1,5 +1,7 @@
 """Gradients of arrays of more than 4 GiB.  Their values are -1, 0 and 1, whose sums fp32 holds exactly: results are compared
 to the bit, at both ends and at rows between."""
+import gc
+
 import pytest
 import torch
 
@@ -7,6 +9,14 @@ from paper_2605_10670_amd import binding, layer, synth
 
 pytestmark = pytest.mark.gpu
 PAST = 2 ** 32
+
+
+@pytest.fixture(autouse=True)
+def nothing_large_stays_cached():
+    """(What a later test allocates would be cut from these blocks, which it then holds.)"""
+    yield
+    gc.collect()
+    torch.cuda.empty_cache()
 
 
 def small_integers(seed, *shape, dtype=torch.bfloat16):
