@@ -12,8 +12,11 @@ PAST = 2 ** 32
 
 
 @pytest.fixture(autouse=True)
-def nothing_large_stays_cached():
-    """(What a later test allocates would be cut from these blocks, which it then holds.)"""
+def nothing_large_stays():
+    """What lasts and is made by the way, the library's workspace for products, is made before anything large is: cut from a freed large
+    block it would hold the whole of that, and later tests' allocations would come from there."""
+    one = torch.ones((64, 64), device="cuda")
+    (one @ one).sum().item()
     yield
     gc.collect()
     torch.cuda.empty_cache()
