@@ -15,6 +15,8 @@ PAST = 2 ** 32
 def nothing_large_stays():
     """What lasts and is made by the way, the library's workspace for products, is made before anything large is: cut from a freed large
     block it would hold the whole of that, and later tests' allocations would come from there."""
+    gc.collect()
+    torch.cuda.empty_cache()
     one = torch.ones((64, 64), device="cuda")
     (one @ one).sum().item()
     yield
