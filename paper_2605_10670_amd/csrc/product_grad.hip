@@ -78,8 +78,8 @@ __global__ __launch_bounds__(256) void k_gate_grad(GateGradArgs a, int64_t first
 }
 
 // ---------------------------------------------------------------------------
-// tiles: 256 in_features by 64 * TT rows (TT 0: 16) of the result, which are tokens (OF_W false: the rows' gradient, summed over the
-// weights' rows) or weight rows (OF_W: the weights' gradient, summed over a slot's tokens).
+// tiles: 256 in_features by 64 * TT rows (TT 0: 16; OF_W has 4 and 1) of the result, which are tokens (OF_W false: the rows' gradient, summed
+// over the weights' rows) or weight rows (OF_W: the weights' gradient, summed over a slot's tokens).
 //
 // The in_features are the matrix cores' columns: a lane has one of them in four rows of the result, and they are dealt out to the lanes so
 // that after an exchange among every four lanes it has four neighbouring ones of a row, and the 16 lanes beside one another 64 of them.
@@ -188,9 +188,12 @@ struct Across {
   static constexpr int kSize = DT == EEP_BF16 ? 2 : 4, kDepth = kGradStep / kSize;
   static constexpr int kRowBytes = COLS * kSize, kChunks = kRowBytes / 16;
   static constexpr int kLoads = kDepth * kRowBytes / 1024 / WAVES;  // a wavefront's, of 1 KiB
-  static_assert(kChunks >= 16 && kLoads >= 1, "");
+  static_assert(kChunks >= 8 && kLoads >= 1, "");
   __device__ __forceinline__ static int places(int row) {
-    return DT == EEP_BF16 ? 2 * ((row & 3) | ((row >> 1) & 4)) : 4 * ((row >> 2) & 3);
+    if constexpr (kChunks == 8)  // (of which two rows make one of all banks)
+      return 2 * (((row >> 1) & 1) | ((row >> 2) & 2));
+    else
+      return DT == EEP_BF16 ? 2 * ((row & 3) | ((row >> 1) & 4)) : 4 * ((row >> 2) & 3);
   }
   // The row and the first column that this lane brings in the i-th load.
   __device__ __forceinline__ static int row(int wave, int lane, int i) {
@@ -654,7 +657,7 @@ __global__ __launch_bounds__(256) void k_grad_parts(PartArgs a) {
 // What a step of a tile takes, us: of 256 rows; of 64 and 16, of which a CU has two, a step of both, or of one alone.  fp32 products take
 // the matrix cores 16 times as long as bf16 ones, on half as many terms a step.
 static float grad_step_time(int tt, bool f32, bool alone) {
-  if (f32) return tt == 4 ? 4.1f : tt == 1 ? (alone ? 1.1f : 2.1f) : (alone ? 0.4f : 0.6f);
+  if (f32) return tt == 4 ? 4.1f : tt == 1 ? (alone ? 1.1f : 2.2f) : (alone ? 0.4f : 0.6f);
   return tt == 4 ? (alone ? 0.8f : 0.95f) : tt == 1 ? (alone ? 0.4f : 0.75f) : (alone ? 0.35f : 0.5f);
 }
 
@@ -746,12 +749,31 @@ static hipError_t launch_grad_x(TileArgs a, const eep_product_grad& g, hipStream
   }
 }
 
+// The same for tiles of 256 or 64 weight rows.  Measured, 256 / 64, us, bf16: one matrix 256 x 7168, 64 rows 9.6 / 6.8, 512 20.2 / 13.0, 16384
+// 89.8 / 98.1; 2048 x 2048, 2048 rows 44.7 / 35.1; 2048 x 7168, 128 rows 13.5 / 14.4; eight slots 512 x 2048 of 1000 rows 32.9 / 25.7, 1024 x 2048 of 300
+// 19.0 / 21.5; 144 slots 4096 x 1024 of 4 rows 202 / 260; fp32: 520 x 1032, 300 rows 32.3 / 19.4, 1024 x 1024, 8192 rows 156 / 149.
+static float grad_w_cost(int tt, bool f32, const TileArgs& a, int64_t work, int64_t steps, int cus) {
+  const int64_t most = (int64_t)cus * grad_per_cu(tt), values = (int64_t)a.slots * a.n * a.k;
+  const float alone = grad_step_time(tt, f32, true), both = grad_step_time(tt, f32, false);
+  const int parts = grad_parts(work, most, steps, values, alone);
+  const float rounds = (float)work * parts / most, more = rounds < 0.5f ? 0.0f : rounds > 1.0f ? 1.0f : 2.0f * rounds - 1.0f;
+  return (alone + (both - alone) * more) * steps / parts * (rounds < 4.0f ? ceilf(rounds) : rounds) + grad_parts_time(parts, values);
+}
+
 template <int DT, int OT>
 static hipError_t launch_grad_w(TileArgs a, const eep_product_grad& g, hipStream_t st) {
+  constexpr int kDepth = kGradStep / (DT == EEP_BF16 ? 2 : 4);
   a.feature_tiles = (a.k + kGradCols - 1) / kGradCols;
-  a.row_tiles = (a.n + 255) / 256;
-  return launch_grad_tiled<DT, OT, true, 4>(a, g, (int64_t)a.row_tiles * a.feature_tiles * a.slots, (int64_t)a.slots * a.n * a.k,
-                                            a.rows / a.slots, st);
+  const int64_t terms = a.rows / a.slots, steps = terms < kDepth ? 1 : (terms + kDepth - 1) / kDepth;
+  const auto work = [&](int tt) { return (int64_t)((a.n + grad_rows(tt) - 1) / grad_rows(tt)) * a.feature_tiles * a.slots; };
+  const auto tiled = [&](auto tt) {
+    constexpr int TT = decltype(tt)::value;
+    a.row_tiles = (a.n + grad_rows(TT) - 1) / grad_rows(TT);
+    return launch_grad_tiled<DT, OT, true, TT>(a, g, work(TT), (int64_t)a.slots * a.n * a.k, terms, st);
+  };
+  if (grad_w_cost(1, DT == EEP_F32, a, work(1), steps, g.cus) < grad_w_cost(4, DT == EEP_F32, a, work(4), steps, g.cus))
+    return tiled(std::integral_constant<int, 1>());
+  return tiled(std::integral_constant<int, 4>());
 }
 
 // More LDS than a kernel may have by default, on the current device.
@@ -766,6 +788,8 @@ static hipError_t allow_grad_lds() {
   if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, EEP_F32, false, 1>, 1);
   if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, EEP_F32, false, 4>, 4);
   if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, DT, false, 4>, 4);
+  if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, EEP_F32, true, 1>, 1);
+  if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, EEP_BF16, true, 1>, 1);
   if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, EEP_F32, true, 4>, 4);
   if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, EEP_BF16, true, 4>, 4);
   return e;

@@ -253,6 +253,19 @@ def test_tiles_of_every_size(dtype, counts, K, I):
     h.destroy()
 
 
+@pytest.mark.parametrize("dtype,w_dtype", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32"), ("f32", "bf16")])
+@pytest.mark.parametrize("counts,K,I", [([0, 1, 33, 70, 64, 96, 2] * 8, 520, 264), ([5, 0, 40] * 60, 264, 72), ([3000], 264, 520), ([31, 65, 0, 32], 1288, 136)],
+                         ids=lambda v: f"{len(v)} slots" if isinstance(v, list) else str(v))
+def test_weights_tiles_of_every_size(dtype, w_dtype, counts, K, I):
+    """Many and few tiles of 256 and 64 weight rows, with ends in every direction; also added to what is there."""
+    case = Case(K + I, counts, K, I, dtype)
+    handle = case.handle(w_dtype)
+    case.check(case.run(handle, w_dtype, wanted="w"))
+    old = lu.randn(lu.gen(9), case.P, case.N, case.K).to(TORCH_OF[w_dtype])
+    case.check(case.run(handle, w_dtype, wanted="w", old=old), old)
+    handle.destroy()
+
+
 @pytest.mark.parametrize("counts", [[40, 0, 300, 2], [2, 1, 0, 3], [900, 500, 0, 0]], ids=str)
 def test_captured_and_replayed(counts):
     """One graph for all row counts: the offsets are read on the device."""
