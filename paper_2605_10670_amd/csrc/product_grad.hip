@@ -657,7 +657,7 @@ __global__ __launch_bounds__(256) void k_grad_parts(PartArgs a) {
 // What a step of a tile takes, us: of 256 rows; of 64 and 16, of which a CU has two, a step of both, or of one alone.  fp32 products take
 // the matrix cores 16 times as long as bf16 ones, on half as many terms a step.
 static float grad_step_time(int tt, bool f32, bool alone) {
-  if (f32) return tt == 4 ? 4.1f : tt == 1 ? (alone ? 1.1f : 2.2f) : (alone ? 0.4f : 0.6f);
+  if (f32) return tt == 4 ? 4.1f : tt == 1 ? (alone ? 1.1f : 2.2f) : (alone ? 0.4f : 0.8f);
   return tt == 4 ? (alone ? 0.8f : 0.95f) : tt == 1 ? (alone ? 0.4f : 0.75f) : (alone ? 0.35f : 0.5f);
 }
 
