@@ -215,7 +215,7 @@ static hipError_t launch_layer_norm(const LayerNormArgs& a, int T, hipStream_t s
 // registers, and the next row's loads are under way while this one's sums cross the workgroup.  The sums of the workgroups
 // are left in the workspace and added up, in their order, by a second kernel.  Bound by memory: 16384 rows of 7168 bf16 with grad_sum 159 to 174 us
 // (5.4 to 5.9 TB/s; with four exchanges a row, the gain from memory and one workgroup to a CU 242; 1 / 4 / 8 workgroups a CU 233 / 165 / 192; up
-// to 1024 / 256 threads 167 / 257; plain stores 170); 64 centred rows 10.1, latency (12.2 with two vectors a thread).
+// to 1024 / 256 threads 167 / 257; plain stores 170); 64 centred rows 9.6, latency (12.2 with two vectors a thread).
 // ---------------------------------------------------------------------------
 struct NormGradArgs {
   const void *h, *gain, *grad_y, *grad_sum;

@@ -727,10 +727,10 @@ static hipError_t launch_grad_tiled(const TileArgs& a, const eep_product_grad& g
 }
 
 // What the tiles of 256, 64 or 16 tokens cost, us: their steps, as often as a CU has one, and the sum of parts.  A slot's last tile is half
-// empty on average.  Measured, 16 / 64 / 256 tokens a tile, us, bf16: 144 slots
-// 1024 -> 4096, 64 tokens by top-8 217 / 226 / 247, 300 242 / 240 / 262, 1200 406 / 271 / 272, 2400 708 / 342 / 339; 120 slots 2880 -> 2816,
-// top-6, 400 tokens 408 / 357 / 379, 1600 814 / 480 / 456, 5976 - / 973 / 800; one matrix 2048 -> 7168, 64 rows 19 / 26 / 24, 256 35 / 29 / 41,
-// 2048 211 / 90 / 83, 8192 785 / 282 / 224.  (Tiles of 128 were between the two, and best nowhere.)
+// empty on average.  Measured, 16 / 64 / 256 tokens a tile, us, bf16: one matrix 256 x 7168, 64 tokens 9.6 / 11.2 / 15.2, 512 18.6 / 12.2 / 17.1, 4096
+// 94 / 34.8 / 31.9; 2048 x 2048, 2048 tokens 68 / 37.9 / 49.5; 7168 x 2048, 512 64 / 37.4 / 44.4; eight slots 512 x 2048 of 1000 84 / 31.5 / 26.4; 120 slots
+// 2816 x 2880 of 4 334 / 343 / 361, of 20 462 / 359 / 364, of 50 676 / 365 / 371, of 100 1036 / 526 / 410; fp32: 2048 x 2048, 2048 tokens 201 / 155 / 159, 120
+// slots 2816 x 2880 of 4 686 / 1121 / 2286.  (Tiles of 128 were between the two, and best nowhere.)
 static float grad_x_cost(int tt, bool f32, const TileArgs& a, int64_t steps, int cus) {
   const int64_t touched = a.rows < a.slots ? a.rows : a.slots, most = (int64_t)cus * grad_per_cu(tt), rows = grad_rows(tt);
   float tiles = (float)a.rows / touched / rows + 0.5f;
