@@ -462,7 +462,7 @@ __global__ __launch_bounds__(256) void k_route_grad_many(const void* logits, con
 #pragma unroll
     for (int i = 0; i < FOURS; ++i)
 #pragma unroll
-      for (int n = 0; n < 4; ++n) v[i][n] *= by;
+      for (int n = 0; n < 4; ++n) v[i][n] = v[i][n] > 0.0f ? v[i][n] * by : 0.0f;  // (`by` may be infinite, or NaN)
   }
   // The choices' shares join their logits in LDS, each by its own lane; an index that comes several times (no router's choice does)
   // by the first of them, with the shares of all.
