@@ -459,10 +459,17 @@ __global__ __launch_bounds__(256) void k_route_grad_many(const void* logits, con
       }
     all = lane_sum<16>(all);
     const float by = all > 0.0f ? -inner / all : 0.0f;
+    if (fabsf(by) < INFINITY) {
 #pragma unroll
-    for (int i = 0; i < FOURS; ++i)
+      for (int i = 0; i < FOURS; ++i)
 #pragma unroll
-      for (int n = 0; n < 4; ++n) v[i][n] = v[i][n] > 0.0f ? v[i][n] * by : 0.0f;  // (`by` may be infinite, or NaN)
+        for (int n = 0; n < 4; ++n) v[i][n] *= by;
+    } else {  // (0 stays 0; asked of every value above too, 16384 x 256 bf16 take 7.2 us for 7.0)
+#pragma unroll
+      for (int i = 0; i < FOURS; ++i)
+#pragma unroll
+        for (int n = 0; n < 4; ++n) v[i][n] = v[i][n] > 0.0f ? by : 0.0f;
+    }
   }
   // The choices' shares join their logits in LDS, each by its own lane; an index that comes several times (no router's choice does)
   // by the first of them, with the shares of all.
