@@ -294,20 +294,19 @@ hipError_t launch_route(const eep_router_shape& s, const void* logits, int32_t* 
 // the router's gradient: with inner = sum over the chosen j of w_j * grad_w_j, a chosen logit gets w_j * (grad_w_j - inner) and the
 // others nothing; over all logits every one gets -p * inner, p its share, and a chosen one w_j * grad_w_j more.
 //
-// A group of LANES lanes has a token, four neighbouring logits a lane at a time, to which the lane adds those of the k choices that are
+// A wavefront has a token, four neighbouring logits a lane at a time, to which the lane adds those of the k choices that are
 // among them; it reads them itself before it writes there, so that the gradient may take the logits' place.  Bound by memory at many tokens, by one trip at few.
 // ---------------------------------------------------------------------------
 constexpr int kRouteGradMany = 4096;  // tokens from which 16 lanes have one
 
-template <bool BF16, int LANES, bool FOURS>
+template <bool BF16, bool FOURS>
 __global__ __launch_bounds__(256) void k_route_grad(const void* logits, const int32_t* __restrict__ topk_idx,
                                                     const float* __restrict__ topk_w, const float* __restrict__ grad_w,
                                                     void* grad_logits, int E, int k, int over_all, int64_t first,
                                                     int64_t end) {
-  constexpr int kTokens = 256 / LANES;
-  const int lane = threadIdx.x & (LANES - 1);
-  const int64_t t = first + (int64_t)blockIdx.x * kTokens + threadIdx.x / LANES;
-  if (t >= end) return;  // (a group's lanes go together)
+  const int lane = threadIdx.x & 63;
+  const int64_t t = first + (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
+  if (t >= end) return;
   const auto load4 = [&](int e, float (&v)[4]) {
     if constexpr (FOURS) {
       if constexpr (BF16) {
@@ -328,44 +327,34 @@ __global__ __launch_bounds__(256) void k_route_grad(const void* logits, const in
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = v[i] > -INFINITY ? v[i] : -INFINITY;  // (NaN weighs nothing either)
   };
-  // the choices, LANES of them at a time; top-32 of groups of 16 lanes takes two
-  constexpr int kRounds = 32 / LANES > 0 ? 32 / LANES : 1;
-  int idx[kRounds];
-  float part[kRounds], inner = 0.0f;
-#pragma unroll
-  for (int r = 0; r < kRounds; ++r) {
-    const int j = r * LANES + lane;
-    idx[r] = j < k ? topk_idx[t * k + j] : -1;
-    part[r] = 0.0f;
-    if (idx[r] >= 0) part[r] = topk_w[t * k + j] * grad_w[t * k + j];
-    inner += part[r];
+  static_assert(kMaxTopk <= 64, "a choice a lane");
+  const int idx = lane < k ? topk_idx[t * k + lane] : -1;
+  float w = 0.0f, gw = 0.0f;
+  if (idx >= 0) {
+    w = topk_w[t * k + lane];
+    gw = grad_w[t * k + lane];
   }
-  inner = lane_sum<LANES>(inner);
+  float part = idx >= 0 ? w * gw : 0.0f;
+  const float inner = lane_sum<64>(part);
   float top = -INFINITY, all = 0.0f;
   if (over_all == 0) {
-#pragma unroll
-    for (int r = 0; r < kRounds; ++r)
-      if (idx[r] >= 0) {
-        const int64_t at = t * k + r * LANES + lane;
-        part[r] = topk_w[at] * (grad_w[at] - inner);
-      }
+    part = idx >= 0 ? w * (gw - inner) : 0.0f;
   } else {
     float v[4];
-    for (int e = lane * 4; e < E; e += LANES * 4) {
+    for (int e = lane * 4; e < E; e += 256) {
       load4(e, v);
 #pragma unroll
       for (int i = 0; i < 4; ++i) top = fmaxf(top, v[i]);
     }
-    top = fold<LANES>(top, [](float a, float b) { return fmaxf(a, b); });
-    for (int e = lane * 4; e < E; e += LANES * 4) {
+    top = fold<64>(top, [](float a, float b) { return fmaxf(a, b); });
+    for (int e = lane * 4; e < E; e += 256) {
       load4(e, v);
 #pragma unroll
       for (int i = 0; i < 4; ++i) all += v[i] > -INFINITY ? exp_below(v[i], top) : 0.0f;
     }
-    all = lane_sum<LANES>(all);
+    all = lane_sum<64>(all);
   }
-  const int group = threadIdx.x & 63 & ~(LANES - 1);
-  for (int e = lane * 4; e < (E + LANES * 4 - 1) / (LANES * 4) * (LANES * 4); e += LANES * 4) {
+  for (int e = lane * 4; e < (E + 255) / 256 * 256; e += 256) {
     float g[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (over_all != 0 && e < E) {
       float v[4];
@@ -374,14 +363,12 @@ __global__ __launch_bounds__(256) void k_route_grad(const void* logits, const in
       for (int i = 0; i < 4; ++i) g[i] = v[i] > -INFINITY ? -(exp_below(v[i], top) / all) * inner : 0.0f;
     }
     // (all lanes take part: each brings its choices)
+    for (int j = 0; j < k; ++j) {
+      const int chosen = __shfl(idx, j, 64);
+      const float more = __shfl(part, j, 64);
 #pragma unroll
-    for (int r = 0; r < kRounds; ++r)
-      for (int j = 0; j < LANES && r * LANES + j < k; ++j) {
-        const int chosen = __shfl(idx[r], group + j, 64);
-        const float more = __shfl(part[r], group + j, 64);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) g[i] += chosen == e + i ? more : 0.0f;
-      }
+      for (int i = 0; i < 4; ++i) g[i] += chosen == e + i ? more : 0.0f;
+    }
     if (e >= E) continue;
     if constexpr (FOURS) {
       if constexpr (BF16)
@@ -510,10 +497,9 @@ __global__ __launch_bounds__(256) void k_route_grad_many(const void* logits, con
   }
 }
 
-template <bool BF16, int LANES>
+template <bool BF16>
 hipError_t launch_route_grad(const eep_router_shape& s, const void* logits, const int32_t* topk_idx, const float* topk_w,
                              const float* grad_w, void* grad_logits, int T, hipStream_t st) {
-  constexpr int kTokens = 256 / LANES;
   const uintptr_t four = 4 * dtype_bytes(s.in_dtype);
   const bool fours = s.num_logical % 4 == 0 && (uintptr_t)logits % four == 0 && (uintptr_t)grad_logits % four == 0;
   if (T >= kRouteGradMany && fours && s.num_logical <= 512 && s.topk <= 16) {
@@ -527,9 +513,9 @@ hipError_t launch_route_grad(const eep_router_shape& s, const void* logits, cons
       return hipGetLastError();
     });
   }
-  return in_launches(T, max_blocks(256) * kTokens, [&](int64_t first, int64_t n) {
-    hipLaunchKernelGGL((fours ? k_route_grad<BF16, LANES, true> : k_route_grad<BF16, LANES, false>),
-                       dim3((unsigned)((n + kTokens - 1) / kTokens)), dim3(256), 0, st, logits, topk_idx, topk_w, grad_w, grad_logits,
+  return in_launches(T, max_blocks(256) * 4, [&](int64_t first, int64_t n) {
+    hipLaunchKernelGGL((fours ? k_route_grad<BF16, true> : k_route_grad<BF16, false>),
+                       dim3((unsigned)((n + 3) / 4)), dim3(256), 0, st, logits, topk_idx, topk_w, grad_w, grad_logits,
                        s.num_logical, s.topk, s.over_all, first, first + n);
     return hipGetLastError();
   });
@@ -606,8 +592,8 @@ int eep_route_grad(const eep_router_shape* shape, const void* logits, const int3
     return EEP_ERR_ALIGN;
   hipStream_t st = (hipStream_t)stream;
   const hipError_t e = s.in_dtype == EEP_BF16
-                           ? launch_route_grad<true, 64>(s, logits, topk_idx, topk_w, grad_w, grad_logits, T, st)
-                           : launch_route_grad<false, 64>(s, logits, topk_idx, topk_w, grad_w, grad_logits, T, st);
+                           ? launch_route_grad<true>(s, logits, topk_idx, topk_w, grad_w, grad_logits, T, st)
+                           : launch_route_grad<false>(s, logits, topk_idx, topk_w, grad_w, grad_logits, T, st);
   return e == hipSuccess ? EEP_OK : EEP_ERR_HIP;
 }
 
