@@ -519,9 +519,11 @@ __global__ __launch_bounds__(64 * grad_waves(TT), 2) void k_grad_tiled(TileArgs 
 #pragma unroll
       for (int f = kBefore; f < kA; ++f) multiply(f);
     };
-    // fp32 products of few rows, whose roundings show, are added up 512 terms at a time and these sums then: over 5632 terms 1.3e-6 off in the
-    // 2-norm, now 0.4e-6.  (Tiles of 256 rows have no registers left for it.)
-    constexpr bool kFolds = DT == EEP_F32 && TT != 4;
+    // fp32 products, whose roundings show, are added up 512 terms at a time and these sums then: over 5632 terms 1.3e-6 off in the
+    // 2-norm, now 0.4e-6.  (Tiles of 256 rows have no registers left for it, so fp32 has none: 5632 rows 5632 x 2432, both gradients, 2.78 ms
+    // in such tiles, 2.95 in those of 64; tiles of 128, one to a CU, 3.03.)
+    constexpr bool kFolds = DT == EEP_F32;
+    static_assert(!kFolds || TT != 4, "two sets of sums");
     constexpr int kFoldSteps = 512 / kDepth;
     f32x4 total[kFolds ? kA : 1][kFolds ? kB : 1] = {};
     const auto fold_sums = [&](bool last) {
@@ -674,10 +676,10 @@ __global__ __launch_bounds__(256) void k_grad_parts(PartArgs a) {
   }
 }
 
-// What a step of a tile takes, us: of 256 rows; of 64 and 16, of which a CU has two, a step of both, or of one alone.  fp32 products take
+// What a step of a tile takes, us: of 256 rows (bf16 alone has them); of 64 and 16, of which a CU has two, a step of both, or of one alone.  fp32 products take
 // the matrix cores 16 times as long as bf16 ones, on half as many terms a step.
 static float grad_step_time(int tt, bool f32, bool alone) {
-  if (f32) return tt == 4 ? 4.1f : tt == 1 ? (alone ? 1.1f : 2.2f) : (alone ? 0.4f : 0.8f);
+  if (f32) return tt == 1 ? (alone ? 1.1f : 2.2f) : (alone ? 0.4f : 0.8f);
   return tt == 4 ? (alone ? 0.8f : 0.95f) : tt == 1 ? (alone ? 0.4f : 0.75f) : (alone ? 0.35f : 0.5f);
 }
 
@@ -729,8 +731,8 @@ static hipError_t launch_grad_tiled(const TileArgs& a, const eep_product_grad& g
 // What the tiles of 256, 64 or 16 tokens cost, us: their steps, as often as a CU has one, and the sum of parts.  A slot's last tile is half
 // empty on average.  Measured, 16 / 64 / 256 tokens a tile, us, bf16: one matrix 256 x 7168, 64 tokens 9.6 / 11.2 / 15.2, 512 18.6 / 12.2 / 17.1, 4096
 // 94 / 34.8 / 31.9; 2048 x 2048, 2048 tokens 68 / 37.9 / 49.5; 7168 x 2048, 512 64 / 37.4 / 44.4; eight slots 512 x 2048 of 1000 84 / 31.5 / 26.4; 120 slots
-// 2816 x 2880 of 4 334 / 343 / 361, of 20 462 / 359 / 364, of 50 676 / 365 / 371, of 100 1036 / 526 / 410; fp32: 2048 x 2048, 2048 tokens 201 / 155 / 159, 120
-// slots 2816 x 2880 of 4 686 / 1121 / 2286.  (Tiles of 128 were between the two, and best nowhere.)
+// 2816 x 2880 of 4 334 / 343 / 361, of 20 462 / 359 / 364, of 50 676 / 365 / 371, of 100 1036 / 526 / 410; fp32: 2048 x 2048, 2048 tokens 201 / 155, 120
+// slots 2816 x 2880 of 4 686 / 1121.  (Tiles of 128 were between the two, and best nowhere.)
 static float grad_x_cost(int tt, bool f32, const TileArgs& a, int64_t steps, int cus) {
   const int64_t touched = a.rows < a.slots ? a.rows : a.slots, most = (int64_t)cus * grad_per_cu(tt), rows = grad_rows(tt);
   float tiles = (float)a.rows / touched / rows + 0.5f;
@@ -758,28 +760,27 @@ static hipError_t launch_grad_x(TileArgs a, const eep_product_grad& g, hipStream
   };
   constexpr int kDepth = kGradStep / (DT == EEP_BF16 ? 2 : 4);
   const int sizes[] = {4, 1, 0};
-  int best = 4;
+  int best = 0;
   float least = INFINITY;
   for (const int tt : sizes) {
+    if (DT == EEP_F32 && tt == 4) continue;
     const float cost = grad_x_cost(tt, DT == EEP_F32, a, (a.n + kDepth - 1) / kDepth, g.cus);
     if (cost < least) {
       least = cost;
       best = tt;
     }
   }
-  switch (best) {
-    case 4: return tiled(std::integral_constant<int, 4>());
-    case 1: return tiled(std::integral_constant<int, 1>());
-    default: return tiled(std::integral_constant<int, 0>());
-  }
+  if constexpr (DT != EEP_F32)
+    if (best == 4) return tiled(std::integral_constant<int, 4>());
+  return best == 1 ? tiled(std::integral_constant<int, 1>()) : tiled(std::integral_constant<int, 0>());
 }
 
-// The same for tiles of 256 or 64 weight rows.  Measured, 256 / 64, us, bf16: one matrix 256 x 7168, 64 rows 9.6 / 6.8, 512 20.2 / 13.0, 16384
+// The same for tiles of 256 or 64 weight rows, for bf16 (fp32 has but the latter).  Measured, 256 / 64, us: one matrix 256 x 7168, 64 rows 9.6 / 6.8, 512 20.2 / 13.0, 16384
 // 89.8 / 98.1; 2048 x 2048, 2048 rows 44.7 / 35.1; 2048 x 7168, 128 rows 13.5 / 14.4; eight slots 512 x 2048 of 1000 rows 32.9 / 25.7, 1024 x 2048 of 300
-// 19.0 / 21.5; 144 slots 4096 x 1024 of 4 rows 202 / 260; fp32: 520 x 1032, 300 rows 32.3 / 19.4, 1024 x 1024, 8192 rows 156 / 149.
-static float grad_w_cost(int tt, bool f32, const TileArgs& a, int64_t work, int64_t steps, int cus) {
+// 19.0 / 21.5; 144 slots 4096 x 1024 of 4 rows 202 / 260.
+static float grad_w_cost(int tt, const TileArgs& a, int64_t work, int64_t steps, int cus) {
   const int64_t most = (int64_t)cus * grad_per_cu(tt), values = (int64_t)a.slots * a.n * a.k;
-  const float alone = grad_step_time(tt, f32, true), both = grad_step_time(tt, f32, false);
+  const float alone = grad_step_time(tt, false, true), both = grad_step_time(tt, false, false);
   const int parts = grad_parts(work, most, steps, values, alone);
   const float rounds = (float)work * parts / most, more = rounds < 0.5f ? 0.0f : rounds > 1.0f ? 1.0f : 2.0f * rounds - 1.0f;
   return (alone + (both - alone) * more) * steps / parts * (rounds < 4.0f ? ceilf(rounds) : rounds) + grad_parts_time(parts, values);
@@ -796,9 +797,10 @@ static hipError_t launch_grad_w(TileArgs a, const eep_product_grad& g, hipStream
     a.row_tiles = (a.n + grad_rows(TT) - 1) / grad_rows(TT);
     return launch_grad_tiled<DT, OT, true, TT>(a, g, work(TT), (int64_t)a.slots * a.n * a.k, terms, st);
   };
-  if (grad_w_cost(1, DT == EEP_F32, a, work(1), steps, g.cus) < grad_w_cost(4, DT == EEP_F32, a, work(4), steps, g.cus))
-    return tiled(std::integral_constant<int, 1>());
-  return tiled(std::integral_constant<int, 4>());
+  if constexpr (DT != EEP_F32)
+    if (!(grad_w_cost(1, a, work(1), steps, g.cus) < grad_w_cost(4, a, work(4), steps, g.cus)))
+      return tiled(std::integral_constant<int, 4>());
+  return tiled(std::integral_constant<int, 1>());
 }
 
 // More LDS than a kernel may have by default, on the current device.
@@ -811,12 +813,14 @@ static hipError_t allow_grad_lds() {
   if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, EEP_F32, false, 0>, 0);
   if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, DT, false, 1>, 1);
   if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, EEP_F32, false, 1>, 1);
-  if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, EEP_F32, false, 4>, 4);
-  if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, DT, false, 4>, 4);
   if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, EEP_F32, true, 1>, 1);
   if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, EEP_BF16, true, 1>, 1);
-  if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, EEP_F32, true, 4>, 4);
-  if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, EEP_BF16, true, 4>, 4);
+  if constexpr (DT != EEP_F32) {
+    if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, EEP_F32, false, 4>, 4);
+    if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, DT, false, 4>, 4);
+    if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, EEP_F32, true, 4>, 4);
+    if (e == hipSuccess) e = allow((const void*)k_grad_tiled<DT, EEP_BF16, true, 4>, 4);
+  }
   return e;
 }
 

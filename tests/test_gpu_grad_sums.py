@@ -36,7 +36,7 @@ def check(dtype, w_dtype, counts, K, I, wanted, folded):
 
 @pytest.mark.parametrize("counts,K,I", [([2] * 40, 520, 5632), ([54], 2432, 5632), ([2048], 2432, 5632), ([704] * 8, 520, 5632)],
                          ids=lambda v: f"{len(v)} of {v[0]}" if isinstance(v, list) else str(v))
-@pytest.mark.parametrize("dtype", ["bf16"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_rows(dtype, counts, K, I):
     check(dtype, dtype, counts, K, I, "x", 512 if dtype == "f32" else 0)
 
@@ -44,6 +44,6 @@ def test_rows(dtype, counts, K, I):
 @pytest.mark.parametrize("counts,K,I", [([10700], 1288, 72), ([10700], 2056, 2056), ([2990, 3003, 1, 2816], 2056, 72), ([5632], 2432, 1024),
                                         ([3000] * 8, 1032, 1032)],
                          ids=lambda v: f"{len(v)} of {v[0]}" if isinstance(v, list) else str(v))
-@pytest.mark.parametrize("dtype,w_dtype", [("bf16", "f32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("dtype,w_dtype", [("f32", "f32"), ("f32", "bf16"), ("bf16", "f32"), ("bf16", "bf16")])
 def test_weights(dtype, w_dtype, counts, K, I):
     check(dtype, w_dtype, counts, K, I, "w", 512 if dtype == "f32" else 0)
