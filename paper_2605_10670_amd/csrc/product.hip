@@ -27,6 +27,7 @@ struct eep_product {
 
 namespace eep {
 
+constexpr int kStepBytes = 128;  // along in_features
 constexpr int kScaleBlock = 128;
 
 struct ProductArgs {
@@ -42,6 +43,11 @@ struct ProductArgs {
   int64_t slot_stride, scale_stride;
 };
 
+// 32 bytes a lane of a 16-row operand: two chunks of 16.
+struct Frag {
+  u32x4 c[2];
+};
+
 // 16 e4m3 codes as bf16, which holds them exactly.
 __device__ __forceinline__ void widen(const u32x4& c, bf16x8 (&out)[2]) {
 #pragma unroll
@@ -53,6 +59,24 @@ __device__ __forceinline__ void widen(const u32x4& c, bf16x8 (&out)[2]) {
     out[i >> 1][4 * (i & 1) + 2] = hi[0];
     out[i >> 1][4 * (i & 1) + 3] = hi[1];
   }
+}
+
+// acc + a * b over the 128 bytes of a step.
+template <int DT>
+__device__ __forceinline__ f32x4 mma(const Frag& a, const Frag& b, f32x4 acc) {
+  if constexpr (DT == EEP_BF16) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a.c[j]),
+                                                    __builtin_bit_cast(bf16x8, b.c[j]), acc, 0, 0, 0);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.c[j][i]), __uint_as_float(b.c[j][i]), acc, 0, 0, 0);
+  }
+  return acc;
 }
 
 // Codes are multiplied as bf16, of which the matrix cores keep every product: their 8-bit forms line the products of
@@ -199,6 +223,25 @@ __device__ __forceinline__ bool find_tile(const ProductArgs& a, int64_t tile, in
   *first = __builtin_amdgcn_readlane(found[1], owner);
   *end = __builtin_amdgcn_readlane(found[2], owner);
   return true;
+}
+
+// Stores four neighbouring features of one token.
+template <int YT>
+__device__ __forceinline__ void store4(uint8_t* y, int64_t element, const float (&v)[4]) {
+  if constexpr (YT == EEP_F32)
+    *(f32x4*)(y + element * 4) = f32x4{v[0], v[1], v[2], v[3]};
+  else
+    *(u32x2*)(y + element * 2) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+}
+
+// Two tiles of 16 features side by side, of which a lane has four neighbouring ones each, as bf16: rows of lanes exchange halves,
+// and each stores 16 bytes, so that a row of y gets 64 at once.  n: the first of the 32 features.
+__device__ __forceinline__ void store_tiles(uint8_t* y, int64_t row, int features, int n, int part, bool in_rows,
+                                            const f32x4& a, const f32x4& b) {
+  const auto low = __builtin_amdgcn_permlane16_swap(pack_bf16x2(a[0], a[1]), pack_bf16x2(b[0], b[1]), false, false);
+  const auto high = __builtin_amdgcn_permlane16_swap(pack_bf16x2(a[2], a[3]), pack_bf16x2(b[2], b[3]), false, false);
+  n += (part & 1) * 16 + (part >> 1) * 8;
+  if (in_rows && n < features) *(u32x4*)(y + (row * features + n) * 2) = u32x4{low[0], high[0], low[1], high[1]};
 }
 
 // ---------------------------------------------------------------------------
@@ -535,6 +578,8 @@ __host__ __device__ constexpr int tiled_lds_bytes(bool codes, int tt) {
   return tiled_stages(tt) * (kWeightStage + 64 * tt * kStepBytes) +
          (codes ? kScaleBuffers * tiled_scale_bytes(tt) : 0) + tiled_across(tt) * 64 * tt * 4;
 }
+
+typedef const __attribute__((address_space(1))) void global_void;
 
 template <int DT, int YT, bool GATE, int TT>
 __global__ __launch_bounds__(kTiledThreads, 2) void k_product_tiled(ProductArgs a) {

@@ -2,9 +2,9 @@
 //
 // Both products have an operand whose rows lie across the sum: the weights, whose in_features are neighbours while the sum goes
 // over their rows; and for the weights' gradient both, since that sum goes over tokens.  Such an operand goes through LDS as it lies in
-// memory, a step of 128 bytes' worth of the sum deep, and is turned on the way to the registers: ds_read_b64_tr_b16 gives a lane four
-// values of ONE column from four rows (fp32 values are read one by one).  What a lane holds then is what product.hip's kernels have:
-// lane l has row (column) l % 16 and terms 16 * (l / 16) bytes into each half step.
+// memory, a step of 64 bytes' worth of the sum deep, and is turned on the way to the registers: ds_read_b64_tr_b16 gives a lane four
+// values of ONE column from four rows (fp32 values are read one by one).  Lane l then has row (column) l % 16 and the 16 bytes' worth of
+// terms from 16 * (l / 16) bytes into the step on.
 #include <math.h>
 
 #include <new>
@@ -78,17 +78,17 @@ __global__ __launch_bounds__(256) void k_gate_grad(GateGradArgs a, int64_t first
 }
 
 // ---------------------------------------------------------------------------
-// tiles: 256 in_features by 64 * TT rows (TT 0: 16; OF_W has 4 and 1) of the result, which are tokens (OF_W false: the rows' gradient, summed
+// tiles: 256 in_features by 64 * TT rows (TT 0: 16; OF_W has 4 and 1, fp32 no 4) of the result, which are tokens (OF_W false: the rows' gradient, summed
 // over the weights' rows) or weight rows (OF_W: the weights' gradient, summed over a slot's tokens).
 //
 // The in_features are the matrix cores' columns: a lane has one of them in four rows of the result, and they are dealt out to the lanes so
 // that after an exchange among every four lanes it has four neighbouring ones of a row, and the 16 lanes beside one another 64 of them.
 // (A CU stores 64 bytes at a time of what four neighbouring lanes have: where these are on different rows, a tile of 256 KB takes 8.0 us, now 2.0.)
-// Eight wavefronts; the steps of all tiles are one stream, of which some are under way to LDS while one is
+// Eight wavefronts, or two workgroups of four to a CU for 64 and 16 rows; the steps of all tiles are one stream, of which some are under way to LDS while one is
 // multiplied, and the operands that a step begins with are read while the one before ends.
 // A step is 64 bytes deep, half of what is common, since the next tile's first steps are to be under way beside the stores of the last one: four
 // stages instead of two (with stores that the waits count, 64 tokens 522 -> 490 us); five, which just fit, change nothing.  A step of 256 x 256 takes 0.76 us on few CUs,
-// 0.87 to 1.05 on all, where the card's power bounds it (1.06 PFLOP/s on normal random numbers; torch's product of 8192 x 8192 1.13);
+// 0.87 to 1.05 on all, where the card's power bounds it too (131072 rows 4096 x 4096 0.97 and 1.02 PFLOP/s on normal random numbers; torch's product of 8192 x 8192 1.13);
 // where stores are as many as products, one waits for the other: 120 slots 2880 -> 2816 of 304 tokens, fp32 gradients, 16 us a tile, of which
 // the stores alone are 12.
 // ---------------------------------------------------------------------------

@@ -1,5 +1,4 @@
-// What the kernels of the experts' products and of their gradients share: operands of the matrix cores, stores of their
-// results, the map of the slots' tiles.
+// What the kernels of the experts' products and of their gradients share: the map of the slots' tiles, and two types.
 #pragma once
 
 #include "eep_internal.hpp"
@@ -9,58 +8,7 @@ namespace eep {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-constexpr int kStepBytes = 128;  // along in_features
-
-// 32 bytes a lane of a 16-row operand: two chunks of 16.
-struct Frag {
-  u32x4 c[2];
-};
-
-// acc + a * b over the 128 bytes of a step.
-template <int DT>
-__device__ __forceinline__ f32x4 mma(const Frag& a, const Frag& b, f32x4 acc) {
-  if constexpr (DT == EEP_BF16) {
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a.c[j]),
-                                                    __builtin_bit_cast(bf16x8, b.c[j]), acc, 0, 0, 0);
-  } else {
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.c[j][i]), __uint_as_float(b.c[j][i]), acc, 0, 0, 0);
-  }
-  return acc;
-}
-
-// Stores four neighbouring features of one token.
-template <int YT>
-__device__ __forceinline__ void store4(uint8_t* y, int64_t element, const float (&v)[4]) {
-  if constexpr (YT == EEP_F32)
-    *(f32x4*)(y + element * 4) = f32x4{v[0], v[1], v[2], v[3]};
-  else
-    *(u32x2*)(y + element * 2) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-}
-
-// Two tiles of 16 features side by side, of which a lane has four neighbouring ones each, as bf16: rows of lanes exchange halves,
-// so that each has 16 bytes, the lanes of a row 64 at once: of feature (part & 1) * 16 + (part >> 1) * 8 on.
-__device__ __forceinline__ u32x4 side_by_side(const f32x4& a, const f32x4& b) {
-  const auto low = __builtin_amdgcn_permlane16_swap(pack_bf16x2(a[0], a[1]), pack_bf16x2(b[0], b[1]), false, false);
-  const auto high = __builtin_amdgcn_permlane16_swap(pack_bf16x2(a[2], a[3]), pack_bf16x2(b[2], b[3]), false, false);
-  return u32x4{low[0], high[0], low[1], high[1]};
-}
-
-// n: the first of the 32 features.
-__device__ __forceinline__ void store_tiles(uint8_t* y, int64_t row, int features, int n, int part, bool in_rows,
-                                            const f32x4& a, const f32x4& b) {
-  const u32x4 v = side_by_side(a, b);
-  n += (part & 1) * 16 + (part >> 1) * 8;
-  if (in_rows && n < features) *(u32x4*)(y + (row * features + n) * 2) = v;
-}
-
 typedef __attribute__((address_space(3))) void lds_void;
-typedef const __attribute__((address_space(1))) void global_void;
 
 // The tiles of the slots: what one wavefront has to remember to find any of them.  Args has the offsets (NULL: one slot), rows,
 // slots and feature_tiles.
