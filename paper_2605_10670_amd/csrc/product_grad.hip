@@ -731,7 +731,7 @@ static hipError_t launch_grad_tiled(const TileArgs& a, const eep_product_grad& g
 // What the tiles of 256, 64 or 16 tokens cost, us: their steps, as often as a CU has one, and the sum of parts.  A slot's last tile is half
 // empty on average.  Measured, 16 / 64 / 256 tokens a tile, us, bf16: one matrix 256 x 7168, 64 tokens 9.6 / 11.2 / 15.2, 512 18.6 / 12.2 / 17.1, 4096
 // 94 / 34.8 / 31.9; 2048 x 2048, 2048 tokens 68 / 37.9 / 49.5; 7168 x 2048, 512 64 / 37.4 / 44.4; eight slots 512 x 2048 of 1000 84 / 31.5 / 26.4; 120 slots
-// 2816 x 2880 of 4 334 / 343 / 361, of 20 462 / 359 / 364, of 50 676 / 365 / 371, of 100 1036 / 526 / 410; fp32: 2048 x 2048, 2048 tokens 201 / 155, 120
+// 2816 x 2880 of 4 334 / 343 / 361, of 16 388 / 355 / 364, of 50 641 / 375 / 371, of 100 1000 / 530 / 418; fp32: 2048 x 2048, 2048 tokens 201 / 155, 120
 // slots 2816 x 2880 of 4 686 / 1121.  (Tiles of 128 were between the two, and best nowhere.)
 static float grad_x_cost(int tt, bool f32, const TileArgs& a, int64_t steps, int cus) {
   const int64_t touched = a.rows < a.slots ? a.rows : a.slots, most = (int64_t)cus * grad_per_cu(tt), rows = grad_rows(tt);
@@ -742,8 +742,11 @@ static float grad_x_cost(int tt, bool f32, const TileArgs& a, int64_t steps, int
   const int parts = grad_parts((int64_t)work, most, steps, values, grad_step_time(tt, f32, true));
   const float rounds = work * parts / most, step = grad_step_time(tt, f32, rounds <= 0.5f);
   float time = step * steps / parts * (rounds < 4.0f ? ceilf(rounds) : rounds) + grad_parts_time(parts, values);
-  // Weights that no cache holds come from memory for every tile of a slot, since its tiles are seldom at the same place: 120 slots
-  // 2880 -> 2816 of 64 tokens on average 462 us in tiles of 64, 385 of 256, of 100 526 and 418, of 50 376 and 371.
+  // Weights that no cache holds come from memory for every tile of a slot, since its tiles are seldom at the same place; in tiles of 64 / 256,
+  // us: 120 slots 2880 -> 2816 of 50 tokens 375 / 371, of 64 460 / 387, of 100 530 / 418, of 200 776 / 570; 144 slots 4096 -> 4096 of 50 858 / 785,
+  // of 64 960 / 852, of 100 1111 / 914; 32 slots 7168 -> 2048 of 50 191 / 189, of 100 247 / 214; 144 slots 1024 -> 4096 of 50 238 / 263, of 100
+  // 283 / 280.  Of 48 points of six shapes beside the first (16 to 200 tokens, 0.26 to 4.8 GB) what is chosen took 1.034 times the best of the three in the
+  // mean, without this 1.065; either way 1.45 at most (16 slots 2880 -> 2816 of 80, 94 / 65).
   const float weights = (float)touched * a.n * a.k * (f32 ? 4 : 2), from_memory = (tiles < 1.0f ? 1.0f : tiles) * weights / 6.0e6f;
   if (weights > 256e6f) time = 0.05f * time + (time < from_memory ? from_memory : time);
   return time;
