@@ -701,7 +701,8 @@ int eep_layer_norm(const eep_norm_shape* shape, const void* x, const void* resid
  * grad_h is the gradient of x and of residual alike; grad_sum (or NULL) what reaches `sum` by itself.
  * h, grad_sum, grad_h: device [T, H] in_dtype; gain: device [H] gain_dtype; grad_y: device [T, H] out_dtype; grad_gain,
  * grad_bias: device float [H].  Any of the three results may be NULL.  grad_h may be h or grad_sum itself, or grad_y where the
- * types agree.  The sums over rows are added in an order that depends on T alone.
+ * types agree.  The sums over rows are added in an order that depends on T alone.  Squares, products and sums of a row that leave
+ * fp32's range, on either side, do no harm to results that do not.
  * The handle owns a workspace for the sums (up to 2 workgroups a CU by hidden floats, twice that for centred): calls with it
  * share that, and may not overlap (one stream, or events between).  eep_norm_grad_destroy waits for the device. */
 typedef struct {

@@ -313,6 +313,7 @@ __global__ __launch_bounds__(norm_grad_threads(NV), norm_grad_waves(IN_BF16, NV)
     float by = 1.0f;
     if constexpr (CENTRED) by = centre<NV>(d, a.H, vecs, s_sums, turn);
     // of d * d and v * d; centred, of d, which roundings have left, and of v
+    constexpr int kOfV = CENTRED ? 3 : 0;
     float sum[CENTRED ? 4 : 2];
     const auto sums = [&]() {
 #pragma unroll
@@ -329,7 +330,7 @@ __global__ __launch_bounds__(norm_grad_threads(NV), norm_grad_waves(IN_BF16, NV)
           sum[1] = fmaf(v, d[j][i], sum[1]);
           if constexpr (CENTRED) {
             sum[2] += d[j][i];
-            sum[3] += v;
+            sum[kOfV] += v;
           }
         }
       }
@@ -369,9 +370,30 @@ __global__ __launch_bounds__(norm_grad_threads(NV), norm_grad_waves(IN_BF16, NV)
     float left = 0.0f, mean = 0.0f;
     if constexpr (CENTRED) {
       left = sum[2] / count;
-      mean = sum[3] / count;
+      mean = sum[kOfV] / count;
     }
-    const float along = fmaf(-left, mean, sum[1] / count) * inv;  // mean(v * u)
+    float along = fmaf(-left, mean, sum[1] / count) * inv;  // mean(v * u)
+    // Where products of v and d leave fp32, on either side, those of v and u may not; nor has v to leave it where its sum does.
+    const bool within = fabsf(sum[1]) < INFINITY && (!CENTRED || fabsf(sum[kOfV]) < INFINITY);
+    if (__builtin_expect(!within || (sum[1] != 0.0f && fabsf(sum[1]) < 0x1p-100f), 0)) {
+      const float fits = within ? 1.0f : 0x1p-32f;
+      float again[2] = {0.0f, 0.0f};
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        if (j * threads + tid >= vecs) continue;
+        float g[8];
+        gain_of(j, g);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float v = grad[j].at(i) * g[i] * fits;
+          again[0] = fmaf(v, (d[j][i] - left) * inv, again[0]);
+          again[1] += v;
+        }
+      }
+      block_sum(again, s_sums, turn);
+      along = again[0] / count / fits;
+      if constexpr (CENTRED) mean = again[1] / count / fits;
+    }
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int at = j * threads + tid;
