@@ -704,7 +704,8 @@ int eep_layer_norm(const eep_norm_shape* shape, const void* x, const void* resid
  * types agree.  The sums over rows are added in an order that depends on T alone.  Squares, products and sums of a row that leave
  * fp32's range, on either side, do no harm to results that do not.
  * The handle owns a workspace for the sums (up to 2 workgroups a CU by hidden floats, twice that for centred): calls with it
- * share that, and may not overlap (one stream, or events between).  eep_norm_grad_destroy waits for the device. */
+ * share that, and may not overlap (one stream, or events between).  eep_norm_grad_destroy waits for the device.
+ * Made for rows of up to 8192 channels; a byte of longer ones takes up to twice as long, of more than 16384 channels about eight times. */
 typedef struct {
   int32_t hidden;
   int32_t in_dtype, gain_dtype, out_dtype; /* EEP_F32 or EEP_BF16 */
@@ -731,7 +732,7 @@ int eep_route_grad(const eep_router_shape* shape, const void* logits, const int3
  *   grad_w[p][n, k]  = round(sum over the slot's rows i of g[i, n] * x[i, k])   (0 for a slot without rows)
  *                      accumulate: round(that + what is there)
  *   gate EEP_GATE_SILU: with a = sums[i, n], b = sums[i, out_features + n], the product's sums before the gate (those of an
- *   eep_expert_product without a gate and 2 * out_features), s = 1 / (1 + exp(-a)),
+ *   eep_expert_product without a gate and 2 * out_features: no call with a gate leaves them, and they cost a product of that size more), s = 1 / (1 + exp(-a)),
  *     grad_sums[i, n] = round(grad_y[i, n] * b * s * (1 + a * (1 - s))), grad_sums[i, out_features + n] = round(grad_y[i, n] * a * s)
  *   and g is grad_sums, as rounded.
  * Rows outside every slot are left untouched in grad_sums and grad_x, and are read nowhere.

@@ -72,7 +72,7 @@ constexpr int kRefits = 12;
 // layer norm: h = x + r;  d = h - mean(h);  y = d / sqrt(mean(d^2) + eps) * g + b.
 //
 // A workgroup has a row, all of it in registers, as the residual norm's kernel does; the mean and the sum of squares are two
-// trips through LDS.  Bound by memory at many rows: 5976 rows of 2880 fp32 with residual and sum 38.5 us (5.4 TB/s).
+// trips through LDS.  Bound by memory at many rows: 5976 rows of 2880 fp32 with residual and sum 40 us (6.0 TB/s).
 // ---------------------------------------------------------------------------
 struct LayerNormArgs {
   const void *x, *residual, *gain, *bias;
@@ -215,7 +215,12 @@ static hipError_t launch_layer_norm(const LayerNormArgs& a, int T, hipStream_t s
 // registers, and the next row's loads are under way while this one's sums cross the workgroup.  The sums of the workgroups
 // are left in the workspace and added up, in their order, by a second kernel.  Bound by memory: 16384 rows of 7168 bf16 with grad_sum 159 to 174 us
 // (5.4 to 5.9 TB/s; with four exchanges a row, the gain from memory and one workgroup to a CU 242; 1 / 4 / 8 workgroups a CU 233 / 165 / 192; up
-// to 1024 / 256 threads 167 / 257; plain stores 170); 64 centred rows 9.6, latency (12.2 with two vectors a thread).
+// to 1024 / 256 threads 167 / 257; plain stores 170); centred 207 to 219; 64 centred rows 9.6, latency (12.2 with two vectors a thread).
+//
+// That is so for rows of up to 8192 channels, of which the main variants spill 32 registers a lane at most.  Up to 16384 fp32 rows spill 90 to
+// 142: 8192 rows of 16384 bf16 / fp32 4.6 / 3.0 TB/s (centred 3.9 / 2.8).  Above that neither the sums nor the next row fit: 738 to
+// 1285 registers a lane are spilled, 1.5 to 1.9 KB, and every row goes through scratch memory: 4096 rows of 16392 0.7 / 0.8 TB/s, 2048
+// of 65536 0.7 / 0.95 (centred 0.55 / 0.8 and 0.65 / 0.9).
 // ---------------------------------------------------------------------------
 struct NormGradArgs {
   const void *h, *gain, *grad_y, *grad_sum;
