@@ -521,7 +521,7 @@ __global__ __launch_bounds__(64 * grad_waves(TT), 2) void k_grad_tiled(TileArgs 
     };
     // fp32 products, whose roundings show, are added up 512 terms at a time and these sums then: over 5632 terms 1.3e-6 off in the
     // 2-norm, now 0.4e-6.  (Tiles of 256 rows have no registers left for it, so fp32 has none: 5632 rows 5632 x 2432, both gradients, 2.78 ms
-    // in such tiles, 2.95 in those of 64; tiles of 128, one to a CU, 3.03.)
+    // in such tiles, 2.95 in those of 64; tiles of 128, one to a CU, 3.03; of 43 other calls 0.82 to 1.12 of the time.)
     constexpr bool kFolds = DT == EEP_F32;
     static_assert(!kFolds || TT != 4, "two sets of sums");
     constexpr int kFoldSteps = 512 / kDepth;
@@ -700,6 +700,25 @@ static int grad_parts(int64_t work, int64_t most, int64_t steps, int64_t values,
   return parts >= 2 && step * steps / parts + grad_parts_time(parts, values) < step * steps ? (int)parts : 1;
 }
 
+// An fp32 step takes the matrix cores of a CU alike with one workgroup on it and with two: what counts is how many tiles the CU has that has
+// most, so that 200 tiles on 256 CUs take as long as 256, and 300 as long as 512.  Divided into 2 to 8 parts they are spread more evenly, undivided / so,
+// us: rows of 449 x 5760 -> 6400 392 / 329, weights 1024 x 5248 of 8311 rows with those rows' gradient 1884 / 1539, 9600 x 336 of 6620 1603 / 1295.
+static float grad_time_f32(int64_t work, int64_t parts, int64_t steps, int64_t values, float step, int cus) {
+  return (float)((work * parts + cus - 1) / cus) * step * steps / parts + grad_parts_time(parts, values);
+}
+static int grad_spread_f32(int64_t work, int parts, int64_t steps, int64_t values, float step, int cus) {
+  const float now = grad_time_f32(work, parts, steps, values, step, cus);
+  float least = 0.85f * now;  // (the tiles are an estimate)
+  for (int p = 2; p <= 8 && p <= steps && p * values * (int64_t)sizeof(float) <= kPartialBytes; ++p) {
+    const float time = grad_time_f32(work, p, steps, values, step, cus);
+    if (time < least) {
+      least = time;
+      parts = p;
+    }
+  }
+  return parts;
+}
+
 // values, width: of the result, of one of its rows; terms: of a sum, about.
 template <int DT, int OT, bool OF_W, int TT>
 static hipError_t launch_grad_tiled(const TileArgs& a, const eep_product_grad& g, int64_t work, int64_t values, int64_t terms,
@@ -707,7 +726,10 @@ static hipError_t launch_grad_tiled(const TileArgs& a, const eep_product_grad& g
   constexpr int kDepth = kGradStep / (DT == EEP_BF16 ? 2 : 4);
   const int64_t most = (int64_t)g.cus * grad_per_cu(TT);
   const unsigned grid = (unsigned)(work < most ? work : most);
-  const int parts = grad_parts(work, most, (terms + kDepth - 1) / kDepth, values, grad_step_time(TT, DT == EEP_F32, true));
+  const int64_t steps = (terms + kDepth - 1) / kDepth;
+  const float step = grad_step_time(TT, DT == EEP_F32, true);
+  int parts = grad_parts(work, most, steps, values, step);
+  if (DT == EEP_F32) parts = grad_spread_f32(work, parts, steps, values, step, g.cus);
   if (parts == 1) {
     hipLaunchKernelGGL((k_grad_tiled<DT, OT, OF_W, TT>), dim3(grid), dim3(64 * grad_waves(TT)), grad_lds_bytes(TT), st, a);
     return hipGetLastError();
@@ -739,9 +761,12 @@ static float grad_x_cost(int tt, bool f32, const TileArgs& a, int64_t steps, int
   if (touched == 1) tiles = (float)((a.rows + rows - 1) / rows);
   const float work = (tiles < 1.0f ? 1.0f : tiles) * touched * a.feature_tiles;
   const int64_t values = (int64_t)a.rows * a.k;
-  const int parts = grad_parts((int64_t)work, most, steps, values, grad_step_time(tt, f32, true));
+  const float alone = grad_step_time(tt, f32, true);
+  const int parts = grad_parts((int64_t)work, most, steps, values, alone);
   const float rounds = work * parts / most, step = grad_step_time(tt, f32, rounds <= 0.5f);
   float time = step * steps / parts * (rounds < 4.0f ? ceilf(rounds) : rounds) + grad_parts_time(parts, values);
+  const int spread = f32 ? grad_spread_f32((int64_t)work, parts, steps, values, alone, cus) : parts;
+  if (spread != parts) time = grad_time_f32((int64_t)work, spread, steps, values, alone, cus);
   // Weights that no cache holds come from memory for every tile of a slot, since its tiles are seldom at the same place; in tiles of 64 / 256,
   // us: 120 slots 2880 -> 2816 of 50 tokens 375 / 371, of 64 460 / 387, of 100 530 / 418, of 200 776 / 570; 144 slots 4096 -> 4096 of 50 858 / 785,
   // of 64 960 / 852, of 100 1111 / 914; 32 slots 7168 -> 2048 of 50 191 / 189, of 100 247 / 214; 144 slots 1024 -> 4096 of 50 238 / 263, of 100

@@ -47,3 +47,9 @@ def test_rows(dtype, counts, K, I):
 @pytest.mark.parametrize("dtype,w_dtype", [("f32", "f32"), ("f32", "bf16"), ("bf16", "f32"), ("bf16", "bf16")])
 def test_weights(dtype, w_dtype, counts, K, I):
     check(dtype, w_dtype, counts, K, I, "w", 512 if dtype == "f32" else 0)
+
+
+def test_more_parts_than_workgroups_at_a_time():
+    """Tiles that fill the CUs unevenly, divided: of 520 tiles two parts each, and of 200 five."""
+    check("f32", "f32", [12000] * 8, 1032, 832, "w", 512)
+    check("f32", "f32", [449], 6400, 5760, "x", 512)
